@@ -18,6 +18,9 @@
  *   arrol_score_mlp_kernels, arrol_score_mlp_tiles, arrol_logprob_kernel   test aids: which kernels a call takes
  *   arrol_token_confidence, arrol_trace_confidence             trace confidence (Sec. 3)
  *   arrol_grpo_advantage, arrol_grpo_objective                 group-relative advantage, clipped objective (Sec. 3)
+ *   arrol_attention, arrol_attention_grad                      attention over packed sequences (prompts, survivors) and its gradient
+ *   arrol_decode_attention                                     one token per rollout over the paged pool, a group's prompt read once
+ *   arrol_evict                                                rollouts' caches cut to a budget of tokens by their attention weight
  *
  * Conventions common to every call
  *   - Every data pointer is a DEVICE pointer owned by the caller (the library never
@@ -454,6 +457,40 @@ int arrol_adamw_step(float* param, const float* grad, float* m, float* v, int64_
  */
 int arrol_probe_mfma_rate(const void* a_bf16, int64_t n_a, const void* b_bf16, int64_t n_b, int32_t shape,
                           int32_t n_workgroups, int32_t iters, float* sink, double* flop_out, void* stream);
+
+/*
+ * ---- Attention on the rollouts: what a model runs between the stages above (the paper's backend and update take it as given) --------
+ * Packed sequences, as the log-prob pass has them: sequence s holds the rows [cu_seqlens[s], cu_seqlens[s+1]) (int64 [n_seq+1],
+ * ascending; clamped into [0, T]).  With nq queries and nk keys in a sequence, query head h reads kv head h / (n_heads / n_kv_heads):
+ *   z_ij = scale <q_i, k_j>,  j visible to i: all, or with causal != 0 those with j + nq <= i + nk (the ends aligned, so that the
+ *   queries may be the last rows of a longer context);  lse_i = log sum_j exp z_ij,  o_i = sum_j exp(z_ij - lse_i) v_j.
+ * A query that sees no key, and a row of no sequence, has o = 0 and lse = -inf.  Whatever lies in other sequences' rows (NaN, too) takes no part.
+ * q bf16, row t of head h at q + t*q_stride + h*head_dim (elements; k and v in the same way, n_kv_heads of them): slices of a
+ *   fused projection need no copy.  Strides multiples of 8 and at least heads*head_dim, bases 16-byte aligned.
+ * cu_seqlens_k NULL: the same as the queries'.   n_heads a multiple of n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0.
+ * out bf16 [T_q, n_heads, head_dim];  lse_out NULL or fp32 [n_heads, T_q].
+ * bf16 products, fp32 accumulation, maximum, sum and lse; the weights are rounded to bf16 for the product with v (2^-9 each).
+ * T_q == 0 is a no-op.  (T / 128 + n_seq + 2) * n_heads has to stay below 2^24, else ARROL_EINVAL.
+ */
+int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    const int64_t* cu_seqlens_q, const int64_t* cu_seqlens_k, int64_t T_q, int64_t T_k, int32_t n_seq,
+                    int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale, void* out,
+                    float* lse_out, void* stream);
+
+/*
+ * The gradient of the above, given out, lse (arrol_attention's of the same inputs) and grad_out = dL/dout bf16 [T_q, n_heads, head_dim]:
+ *   p_ij = exp(z_ij - lse_i),  ds_ij = p_ij (<do_i, v_j> - <do_i, o_i>)
+ *   dv_j = sum_i p_ij do_i,  dk_j = scale sum_i ds_ij q_i (sums over all query heads of the kv head),  dq_i = scale sum_j ds_ij k_j
+ * grad_q bf16 [T_q, n_heads, head_dim], grad_k and grad_v bf16 [T_k, n_kv_heads, head_dim], each rounded once from fp32 sums (p and ds are
+ * rounded to bf16 for their products).  No atomics: bit-reproducible run to run.  Rows of no sequence get zeros.
+ * workspace: arrol_attention_grad_workspace_bytes(T_q, n_heads) bytes, 16-byte aligned.
+ */
+size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int32_t n_heads);
+int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                         const void* out, const float* lse, const void* grad_out, const int64_t* cu_seqlens_q,
+                         const int64_t* cu_seqlens_k, int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads,
+                         int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale, void* grad_q, void* grad_k,
+                         void* grad_v, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -92,6 +92,11 @@ _SIGNATURES = {
     "arrol_calibrate": (ctypes.c_int, [_vp, _vp, _i32, Policy, _vp, _vp, _vp, _vp]),
     "arrol_calibrate_search": (ctypes.c_int, [_vp, _vp, _i32, Policy, _vp, _vp]),
     "arrol_prune_bernoulli": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "arrol_attention": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _i32, _i32, _i32, _f32,
+                                       _vp, _vp, _vp]),
+    "arrol_attention_grad_workspace_bytes": (_sz, [_i64, _i32]),
+    "arrol_attention_grad": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32,
+                                            _i32, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "arrol_probe_mfma_rate": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _vp]),
 }
 
@@ -720,6 +725,66 @@ def _py_prune_bernoulli(s_norm, uniforms, p_lut, want_p=False, stream=None):
                                      out["survivor_idx"].data_ptr(), out["n_survivors"].data_ptr(), _stream(stream))
     _check("arrol_prune_bernoulli", rc)
     return out
+
+
+def _heads(t, name):
+    """Row stride of a [rows, heads, head_dim] bf16 GPU tensor whose rows may be strided, as slices of a fused projection are."""
+    if t.dim() != 3 or t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise TypeError("%s must be a [rows, heads, head_dim] bf16 GPU tensor" % name)
+    rows, h, hd = t.shape
+    if (hd > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != hd):
+        raise ValueError("%s: the heads of a row must be contiguous" % name)
+    return t.stride(0) if rows > 1 else max(h * hd, t.stride(0) // 8 * 8)
+
+
+def _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale):
+    strides = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("k and v must be [T_k, n_kv_heads, head_dim] with the head_dim of q")
+    n = cu_seqlens.numel() - 1
+    if n < 0 or (cu_seqlens_k is not None and cu_seqlens_k.numel() != n + 1):
+        raise ValueError("cu_seqlens must hold at least one offset, cu_seqlens_k as many")
+    if cu_seqlens_k is None and k.shape[0] != q.shape[0]:
+        raise ValueError("k must have the rows of q where cu_seqlens_k is not given")
+    scale = q.shape[2] ** -0.5 if scale is None else scale
+    ends = (_ptr(cu_seqlens, torch.int64, "cu_seqlens"), _ptr(cu_seqlens_k, torch.int64, "cu_seqlens_k"), q.shape[0], k.shape[0], n,
+            q.shape[1], k.shape[1], q.shape[2], int(bool(causal)), float(scale))
+    return (q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2]), ends
+
+
+@_on_stream
+def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, stream=None):
+    """Attention over packed sequences: q bf16 [T_q, n_heads, head_dim], k and v bf16 [T_k, n_kv_heads, head_dim] (rows may be strided),
+    cu_seqlens int64 [n_seq+1] of the queries and, where they differ, cu_seqlens_k of the keys; scale None: head_dim ** -0.5.
+    -> (out bf16 [T_q, n_heads, head_dim], lse fp32 [n_heads, T_q])."""
+    head, ends = _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+    rc = lib().arrol_attention(*head, *ends, _ptr(out, torch.bfloat16, "out"), lse.data_ptr(), _stream(stream))
+    _check("arrol_attention", rc)
+    return out, lse
+
+
+@_on_stream
+def arrol_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, workspace=None, stream=None):
+    """Gradient of arrol_attention, given its out and lse and grad_out = dL/dout: -> dict(grad_q, grad_k, grad_v), bf16 in the shapes of
+    q, k and v."""
+    head, ends = _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale)
+    if out.shape != q.shape or grad_out.shape != q.shape or lse.shape != (q.shape[1], q.shape[0]):
+        raise ValueError("out and grad_out must have the shape of q, lse [n_heads, T_q]")
+    dev = q.device
+    if workspace is None:
+        workspace = torch.empty(max(lib().arrol_attention_grad_workspace_bytes(q.shape[0], q.shape[1]), 16), dtype=torch.uint8, device=dev)
+    grads = dict(grad_q=torch.empty(q.shape, dtype=torch.bfloat16, device=dev), grad_k=torch.empty(k.shape, dtype=torch.bfloat16, device=dev),
+                 grad_v=torch.empty(k.shape, dtype=torch.bfloat16, device=dev))
+    rc = lib().arrol_attention_grad(*head, _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"),
+                                    _ptr(grad_out, torch.bfloat16, "grad_out"), *ends, grads["grad_q"].data_ptr(), grads["grad_k"].data_ptr(),
+                                    grads["grad_v"].data_ptr(), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("arrol_attention_grad", rc)
+    return grads
 
 
 @_on_stream
