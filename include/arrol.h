@@ -492,6 +492,53 @@ int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t
                          int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale, void* grad_q, void* grad_k,
                          void* grad_v, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The same for one new token per rollout, on one layer of the paged pool (layout and block tables as in arrol_compact; the token's own key and value are
+ * in the pool already).  The rollouts of a prompt share its pages: rollouts [group_offsets[g], group_offsets[g+1]) (int64 [n_groups+1], ascending,
+ * clamped into [0, n]) see the prefix_len[g] tokens of prefix_table[g], which are read once for all of them, and then each its own
+ * seq_len[r] tokens of block_table[r]; a rollout of no group sees its own alone.  With t over all tokens that rollout r sees:
+ *   z_t = scale <q, k_t>,  lse = log sum_t exp z_t,  o = sum_t exp(z_t - lse) v_t;  no token: o = 0, lse = -inf
+ * q bf16 [n, n_heads, head_dim], 16-byte aligned; kv bf16, the whole pool; 0 <= layer < layout.n_layers.
+ * block_table int32 [n, max_pages_per_seq], seq_len int32 [n]; prefix_table int32 [n_groups, max_pages_per_prefix], prefix_len int32 [n_groups].
+ *   Lengths are clamped to what a row holds; a token on a page id outside [0, n_pages) does not exist.  n_groups == 0: no prefixes.
+ * out bf16 [n, n_heads, head_dim];  lse_out NULL or fp32 [n, n_heads].
+ * weight_out NULL or fp32 [n, max_pages_per_seq * page_tokens]: the attention weight gathered by every own token,
+ *   weight_out[r][t] = weight_in[r][t] (NULL: 0) + sum over the heads of exp(z_t - lse) for t < seq_len[r], 0 behind it (so that a token starts from 0);
+ *   prefix_weight_out, prefix_weight_in fp32 [n_groups, max_pages_per_prefix * page_tokens] in the same way, summed over the group's rollouts too.
+ *   The _out may be the _in.  Called for every layer with the same buffers they gather over the layers.
+ * n_heads a multiple of layout.n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0; n and n_groups at most 65535 with weights, n_groups always.
+ * fp32 scores, sums and lse; the weights are rounded to bf16 for the product with v.  No atomics: bit-reproducible run to run.
+ * workspace: arrol_decode_attention_workspace_bytes(...) bytes, 16-byte aligned (want_weight: 1 where weight_out or prefix_weight_out is given).
+ */
+size_t arrol_decode_attention_workspace_bytes(int32_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_tokens,
+                                              int32_t max_pages_per_seq, int32_t max_pages_per_prefix, int32_t n_groups,
+                                              int32_t want_weight);
+int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads, const void* kv, arrol_kv_layout layout, int32_t layer,
+                           const int32_t* block_table, const int32_t* seq_len, int32_t max_pages_per_seq,
+                           const int32_t* prefix_table, const int32_t* prefix_len, int32_t max_pages_per_prefix,
+                           const int64_t* group_offsets, int32_t n_groups, float scale, void* out, float* lse_out,
+                           const float* weight_in, const float* prefix_weight_in, float* weight_out,
+                           float* prefix_weight_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cuts every row's cache to `budget` tokens, in place and in every layer, by the weight that arrol_decode_attention gathers.  A row of
+ * len = seq_len (clamped to what its table holds) keeps n = min(len, budget) tokens: where len > budget the first n_first and the last n_recent, and of
+ * those between them the ones of the largest weight (ties: the lowest index; NaN counts as the smallest).  Kept tokens in slots >= n
+ * move, in ascending order, to the slots < n that come free, in ascending order; all others stay where they are (keys carry their
+ * own rotation, so the order in the cache means nothing to the attention).  A row's pages must be its own (rollouts' pages; a prefix is a row of its own).
+ *   block_table_out[r][p] = block_table[r][p] for p < ceil(n / page_tokens), -1 behind; seq_len_out[r] = n;
+ *   weight_out[r][t] = weight of the token now in slot t, 0 for t >= n;
+ *   position_out[r][t] = position[r][slot it came from] (position NULL: that slot itself), -1 for t >= n.
+ * weight, weight_out fp32 and position (NULL allowed), position_out int32, all [n_rows, max_pages_per_seq * page_tokens].  Each _out may be its input.
+ * A token on a page id outside [0, n_pages) is not copied.  n_kv_heads * head_dim a multiple of 8; n_first + n_recent <= budget.
+ * workspace: arrol_evict_workspace_bytes(...) bytes, 16-byte aligned.  n_rows == 0 is a no-op.
+ */
+size_t arrol_evict_workspace_bytes(int32_t n_rows, int32_t max_pages_per_seq, int32_t page_tokens, int32_t budget);
+int arrol_evict(void* kv, arrol_kv_layout layout, const int32_t* block_table, const int32_t* seq_len, int32_t n_rows,
+                int32_t max_pages_per_seq, const float* weight, const int32_t* position, int32_t budget, int32_t n_first,
+                int32_t n_recent, int32_t* block_table_out, int32_t* seq_len_out, float* weight_out, int32_t* position_out,
+                void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

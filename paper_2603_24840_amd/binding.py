@@ -97,6 +97,12 @@ _SIGNATURES = {
     "arrol_attention_grad_workspace_bytes": (_sz, [_i64, _i32]),
     "arrol_attention_grad": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32,
                                             _i32, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "arrol_decode_attention_workspace_bytes": (_sz, [_i32] * 9),
+    "arrol_decode_attention": (ctypes.c_int, [_vp, _i32, _i32, _vp, KVLayout, _i32, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _f32,
+                                              _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "arrol_evict_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "arrol_evict": (ctypes.c_int, [_vp, KVLayout, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz,
+                                   _vp]),
     "arrol_probe_mfma_rate": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _vp]),
 }
 
@@ -785,6 +791,84 @@ def arrol_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=N
                                     grads["grad_v"].data_ptr(), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
     _check("arrol_attention_grad", rc)
     return grads
+
+
+@_on_stream
+def arrol_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None, prefix_len=None, group_offsets=None, scale=None,
+                           want_weight=False, weight=None, prefix_weight=None, out_weight=None, out_prefix_weight=None, workspace=None,
+                           stream=None):
+    """Attention of one new token per rollout over one layer of the paged pool: q bf16 [n, n_heads, head_dim], kv the pool, block_table
+    int32 [n, pages] and seq_len int32 [n] of the rollouts' own tokens; with prefix_table int32 [groups, pages], prefix_len int32 [groups]
+    and group_offsets int64 [groups+1] the rollouts of a group share its prefix.  want_weight: the attention weight of every token is added to
+    weight fp32 [n, pages * page_tokens] and prefix_weight (None: zeros) into out_weight and out_prefix_weight (None: new; may be the inputs).
+    -> dict(out bf16 [n, n_heads, head_dim], lse fp32 [n, n_heads], weight, prefix_weight (None where not wanted or without prefixes))."""
+    if q.dim() != 3 or block_table.dim() != 2 or block_table.shape[0] != q.shape[0] or seq_len.numel() != q.shape[0]:
+        raise ValueError("q must be [n, n_heads, head_dim], block_table [n, pages], seq_len [n]")
+    n, H, hd = q.shape
+    lay = kv_layout_of(kv)
+    if lay.head_dim != hd:
+        raise ValueError("q and the KV pool disagree on head_dim")
+    given = [x is not None for x in (prefix_table, prefix_len, group_offsets)]
+    if any(given) and not all(given):
+        raise ValueError("prefix_table, prefix_len and group_offsets come together")
+    groups = prefix_len.numel() if all(given) else 0
+    if groups and (prefix_table.dim() != 2 or prefix_table.shape[0] != groups or group_offsets.numel() != groups + 1):
+        raise ValueError("prefix_table must be [groups, pages], prefix_len [groups], group_offsets [groups+1]")
+    if not want_weight and any(x is not None for x in (weight, prefix_weight, out_weight, out_prefix_weight)):
+        raise ValueError("weights are given but not wanted")
+    dev, width, prefix_width = q.device, block_table.shape[1], prefix_table.shape[1] if groups else 0
+    shapes = (n, width * lay.page_tokens), (groups, prefix_width * lay.page_tokens)
+    for t, shape in ((weight, shapes[0]), (out_weight, shapes[0]), (prefix_weight, shapes[1]), (out_prefix_weight, shapes[1])):
+        if t is not None and t.shape != shape:
+            raise ValueError("weights must be [rows, pages * page_tokens] of their table")
+    if want_weight and out_weight is None:
+        out_weight = torch.empty(shapes[0], dtype=torch.float32, device=dev)
+    if want_weight and groups and out_prefix_weight is None:
+        out_prefix_weight = torch.empty(shapes[1], dtype=torch.float32, device=dev)
+    if not groups:
+        prefix_weight = out_prefix_weight = None
+    if workspace is None:
+        need = lib().arrol_decode_attention_workspace_bytes(n, H, lay.n_kv_heads, hd, lay.page_tokens, width, prefix_width, groups, int(want_weight))
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    out = torch.empty((n, H, hd), dtype=torch.bfloat16, device=dev)
+    lse = torch.empty((n, H), dtype=torch.float32, device=dev)
+    rc = lib().arrol_decode_attention(
+        _ptr(q, torch.bfloat16, "q"), n, H, _ptr(kv, torch.bfloat16, "kv"), lay, int(layer), _ptr(block_table, torch.int32, "block_table"),
+        _ptr(seq_len, torch.int32, "seq_len"), width, _ptr(prefix_table if groups else None, torch.int32, "prefix_table"),
+        _ptr(prefix_len if groups else None, torch.int32, "prefix_len"), prefix_width, _ptr(group_offsets if groups else None, torch.int64, "group_offsets"),
+        groups, float(hd ** -0.5 if scale is None else scale), out.data_ptr(), lse.data_ptr(), _ptr(weight, torch.float32, "weight"),
+        _ptr(prefix_weight, torch.float32, "prefix_weight"), _ptr(out_weight, torch.float32, "out_weight"),
+        _ptr(out_prefix_weight, torch.float32, "out_prefix_weight"), _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("arrol_decode_attention", rc)
+    return dict(out=out, lse=lse, weight=out_weight, prefix_weight=out_prefix_weight)
+
+
+@_on_stream
+def arrol_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, position=None, out=None, workspace=None, stream=None):
+    """Cuts every row's cache to `budget` tokens by their gathered attention weight (kv is modified in place): block_table int32 [rows, pages],
+    seq_len int32 [rows], weight fp32 and position (None: the slots themselves) int32 [rows, pages * page_tokens].
+    -> dict(block_table, seq_len, weight, position); `out`: such a dict to write into, whose tensors may be the inputs."""
+    if block_table.dim() != 2 or seq_len.numel() != block_table.shape[0]:
+        raise ValueError("block_table must be [rows, pages], seq_len [rows]")
+    rows, width = block_table.shape
+    lay, dev = kv_layout_of(kv), kv.device
+    shape = (rows, width * lay.page_tokens)
+    if weight.shape != shape or (position is not None and position.shape != shape):
+        raise ValueError("weight and position must be [rows, pages * page_tokens]")
+    if out is None:
+        out = dict(block_table=torch.empty((rows, width), dtype=torch.int32, device=dev), seq_len=torch.empty(rows, dtype=torch.int32, device=dev),
+                   weight=torch.empty(shape, dtype=torch.float32, device=dev), position=torch.empty(shape, dtype=torch.int32, device=dev))
+    elif out["block_table"].shape != (rows, width) or out["seq_len"].numel() != rows or out["weight"].shape != shape or out["position"].shape != shape:
+        raise ValueError("the outputs must have the shapes of their inputs")
+    if workspace is None:
+        workspace = torch.empty(max(lib().arrol_evict_workspace_bytes(rows, width, lay.page_tokens, int(budget)), 16), dtype=torch.uint8, device=dev)
+    rc = lib().arrol_evict(_ptr(kv, torch.bfloat16, "kv"), lay, _ptr(block_table, torch.int32, "block_table"), _ptr(seq_len, torch.int32, "seq_len"), rows, width,
+                           _ptr(weight, torch.float32, "weight"), _ptr(position, torch.int32, "position"), int(budget), int(n_first), int(n_recent),
+                           _ptr(out["block_table"], torch.int32, "block_table"), _ptr(out["seq_len"], torch.int32, "seq_len"),
+                           _ptr(out["weight"], torch.float32, "weight"), _ptr(out["position"], torch.int32, "position"),
+                           _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check("arrol_evict", rc)
+    return out
 
 
 @_on_stream

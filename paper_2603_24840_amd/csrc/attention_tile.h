@@ -145,10 +145,10 @@ struct Packed {
 // many as it needs whatever the lengths, and at most one spare.  So the grid is T / rows + n + 2 without a look at the offsets, and a workgroup finds
 // its segment by a search that 64 lanes do together (two rounds for 4,096 sequences).  Offsets out of order give empty or misplaced tiles, all
 // within [0, T).
-template <unsigned ROWS>
-__device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
-    const auto start_of = [&](int s) { return static_cast<int64_t>(static_cast<uint64_t>(p.bound(s)) / ROWS) + s; };
-    int lo = 0, count = p.n + 2;
+template <unsigned ROWS, class Bound>
+__device__ __forceinline__ bool find_tile(const Bound& bound, int segments, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
+    const auto start_of = [&](int s) { return static_cast<int64_t>(static_cast<uint64_t>(bound(s)) / ROWS) + s; };
+    int lo = 0, count = segments;
     while (count > 1) {
         const int step = (count + 63) >> 6, at = lane * step;
         const bool before = at < count && start_of(lo + at) <= tile;
@@ -160,9 +160,13 @@ __device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lan
     }
     segment = __builtin_amdgcn_readfirstlane(lo);
     const int64_t start = start_of(segment);
-    end = p.bound(segment + 1);
-    first = p.bound(segment) + (tile - start) * ROWS;
+    end = bound(segment + 1);
+    first = bound(segment) + (tile - start) * ROWS;
     return tile >= start && first < end;
+}
+template <unsigned ROWS>
+__device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
+    return find_tile<ROWS>([&](int s) { return p.bound(s); }, p.n + 2, tile, lane, segment, first, end);
 }
 inline int64_t tile_bound(int64_t T, int n, int rows) { return T / rows + n + 2; }
 
