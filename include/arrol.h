@@ -466,7 +466,7 @@ int arrol_probe_mfma_rate(const void* a_bf16, int64_t n_a, const void* b_bf16, i
  *   queries may be the last rows of a longer context);  lse_i = log sum_j exp z_ij,  o_i = sum_j exp(z_ij - lse_i) v_j.
  * A query that sees no key, and a row of no sequence, has o = 0 and lse = -inf.  Whatever lies in other sequences' rows (NaN, too) takes no part.
  * q bf16, row t of head h at q + t*q_stride + h*head_dim (elements; k and v in the same way, n_kv_heads of them): slices of a
- *   fused projection need no copy.  Strides multiples of 8 and at least heads*head_dim, bases 16-byte aligned.
+ *   fused projection need no copy.  Strides multiples of 8, at least heads*head_dim and at most 2^24, bases 16-byte aligned.
  * cu_seqlens_k NULL: the same as the queries'.   n_heads a multiple of n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0.
  * out bf16 [T_q, n_heads, head_dim];  lse_out NULL or fp32 [n_heads, T_q].
  * bf16 products, fp32 accumulation, maximum, sum and lse; the weights are rounded to bf16 for the product with v (2^-9 each).

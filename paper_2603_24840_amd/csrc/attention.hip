@@ -13,7 +13,7 @@ namespace {
 using namespace attention;
 
 constexpr int kThreads = 256, kWaves = kThreads / ARROL_WAVE, kOwn = 32 * kWaves;   // 32 own rows a wavefront
-constexpr int64_t kDotBlocks = 1 << 20;
+constexpr int64_t kRowBlocks = 1 << 20;
 
 struct Problem {
     const uint16_t *q, *k, *v;
@@ -30,90 +30,111 @@ __device__ __forceinline__ void split_block(unsigned block, int kv_heads, int& k
     rest = block / static_cast<unsigned>(kv_heads);
 }
 
+__device__ __forceinline__ int clamp32(int64_t n) { return uniform(static_cast<int>(n < 0 ? 0 : n < 32 ? n : 32)); }
+
+// Where a workgroup's 128 queries of a head lie, and which keys they see.
+struct QueryBlock {
+    int64_t row0, k_begin;          // the wavefront's first row; the sequence's first key
+    int nk, own_valid;              // keys; rows of the wavefront that there are
+    int sees;                       // keys that this lane's row sees
+    int sees_least, sees_most;      // over the wavefront's rows (causal: its first and its last valid row)
+    int reach;                      // most over the workgroup's rows
+    __device__ __forceinline__ bool find(const Problem& a, int64_t tile, int wave, int lane) {
+        int segment;
+        int64_t first, end;
+        if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, end)) return false;
+        const int64_t q_begin = a.pq.bound(segment);
+        const int nq = uniform(static_cast<int>(end - q_begin));
+        k_begin = 0, nk = 0;
+        if (segment >= 1 && segment <= a.pq.n) {       // rows of no sequence see no keys: zeros
+            k_begin = a.pk.bound(segment);
+            const int64_t n = a.pk.bound(segment + 1) - k_begin;
+            nk = uniform(static_cast<int>(n < 0 ? 0 : n));
+        }
+        row0 = first + 32 * wave;
+        own_valid = clamp32(end - row0);
+        // query i of its sequence sees keys j < min(nk, i + 1 + nk - nq)
+        const auto seen_by = [&](int i) {
+            const int s = a.causal ? nk + (i + 1 - nq) : nk;
+            return s < 0 ? 0 : s < nk ? s : nk;
+        };
+        const int at = uniform(static_cast<int>(first - q_begin)), i0 = at + 32 * wave;
+        sees = seen_by(i0 + (lane & 31));
+        sees_least = seen_by(i0);
+        sees_most = own_valid > 0 ? seen_by(i0 + own_valid - 1) : 0;
+        reach = seen_by((nq - at < kOwn ? nq - at : kOwn) - 1 + at);
+        return true;
+    }
+};
+
 // Forward pass: a workgroup takes 128 queries of a head, a wavefront 32 of them, and walks over the keys in tiles of 64.
-// S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.
+// S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.  While a tile is worked on the next one is on its way into the
+// other half of the LDS.
 template <int HD>
 __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem a, int64_t tiles, uint16_t* __restrict__ out, float* __restrict__ lse_out) {
     constexpr int BK = 64;
     using T = Tile<HD>;
-    __shared__ __align__(16) unsigned char lds[2][2][BK * T::kRowBytes];
+    constexpr int kTileBytes = BK * T::kRowBytes;
+    __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads;
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
     const int head = kvh * per + static_cast<int>(rest % per);
-    const int64_t tile = tiles - 1 - rest / per;
-    int segment;
-    int64_t first, end;
-    if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, end)) return;
-    const int64_t q_begin = a.pq.bound(segment);
-    int64_t k_begin = 0, nk = 0;
-    if (segment >= 1 && segment <= a.pq.n) {       // rows of no sequence see no keys: zeros
-        k_begin = a.pk.bound(segment);
-        nk = a.pk.bound(segment + 1) - k_begin;
-        if (nk < 0) nk = 0;
-    }
-    const int64_t nq = end - q_begin;
-    // query at offset i of its sequence sees keys j < min(nk, i + 1 + nk - nq)
-    const int64_t shift = a.causal ? nk - nq : nk;
-    const int64_t row0 = first + 32 * wave;           // this wavefront's first row
-    const int own_valid = static_cast<int>(end - row0 < 32 ? (end - row0 < 0 ? 0 : end - row0) : 32);
-    const int64_t my_i = row0 - q_begin + (lane & 31);
-    int64_t sees = a.causal ? my_i + 1 + shift : nk;
-    sees = sees < 0 ? 0 : sees < nk ? sees : nk;
-    // keys that any of the workgroup's rows, and any / all of the wavefront's rows see
-    const int64_t last_i = (end - first < kOwn ? end - first : kOwn) - 1 + first - q_begin;
-    int64_t reach = a.causal ? last_i + 1 + shift : nk;
-    reach = reach < 0 ? 0 : reach < nk ? reach : nk;
-    const int n_tiles = static_cast<int>((reach + BK - 1) / BK);
+    QueryBlock w;
+    if (!w.find(a, tiles - 1 - rest / per, wave, lane)) return;
+    const int n_tiles = (w.reach + BK - 1) / BK;
 
     bf16x8 qf[HD / 16];
-    load_own<HD>(qf, a.q + row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, own_valid, a.hd, lane);
-    const uint16_t* kp = a.k + k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd;
-    const uint16_t* vp = a.v + k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd;
-
+    load_own<HD>(qf, a.q + w.row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, w.own_valid, a.hd, lane);
+    const uint16_t* kp = uniform(a.k + w.k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* vp = uniform(a.v + w.k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
     f32x16 o[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
     float m = -INFINITY, l = 0.f;                 // of z * log2 e; l is this lane's half of the row
     const float c = a.scale * kLog2e;
 
-    Staged<HD, BK, kThreads> ks, vs;
-    const auto fetch = [&](int t) {
-        const int64_t j0 = static_cast<int64_t>(t) * BK;
-        const int valid = static_cast<int>(nk - j0 < BK ? nk - j0 : BK);
-        ks.load(kp + j0 * a.k_stride, a.k_stride, valid, a.hd);
-        vs.load(vp + j0 * a.v_stride, a.v_stride, valid, a.hd);
+    Stream<HD, BK, kWaves> ks, vs;
+    const int whole = w.nk / BK;      // tiles of 64 keys that exist
+    const auto point = [&](int valid) {
+        ks.point(static_cast<unsigned>(a.k_stride) * 2, valid, a.hd, wave, lane);
+        vs.point(static_cast<unsigned>(a.v_stride) * 2, valid, a.hd, wave, lane);
     };
-    if (n_tiles > 0) {
-        fetch(0);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
-    }
-    __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        const int cur = t & 1;
-        if (t + 1 < n_tiles) fetch(t + 1);
-        const unsigned char *kt = lds[cur][0], *vt = lds[cur][1];
+    const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
+    const auto fetch = [&](int t) {
+        if (t == whole) point(w.nk - t * BK);
+        const unsigned to = lds0 + (t & 1) * 2 * kTileBytes;
+        ks.issue(kp, to, wave);
+        vs.issue(vp, to + kTileBytes, wave);
+        kp += BK * a.k_stride;
+        vp += BK * a.v_stride;
+    };
+    const int clear = w.sees_least / BK, needed = (w.sees_most + BK - 1) / BK;
+    const auto step = [&](int t) {
+        const unsigned slot = lds0 + (t & 1) * 2 * kTileBytes, rows = fresh(slot + row_at), columns = fresh(slot + column_at);
         f32x16 s[BK / 32];
 #pragma unroll
         for (int b = 0; b < BK / 32; ++b) {
             s[b] = 0.f;
 #pragma unroll
-            for (int e = 0; e < HD / 16; ++e) s[b] = mfma32(T::by_row(kt, 32 * b + (lane & 31), e, half), qf[e], s[b]);
+            for (int e = 0; e < HD / 16; ++e) s[b] = mfma32(T::by_row(rows, e, 32 * b * T::kRowBytes), qf[e], s[b]);
         }
-        const int64_t j0 = static_cast<int64_t>(t) * BK;
+        if (t >= clear) {       // some row of the wavefront does not see all of the tile
+            stay_branch();
+            const int limit = w.sees - t * BK - 4 * half;
+#pragma unroll
+            for (int b = 0; b < BK / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) < limit ? s[b][r] : -INFINITY;
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < BK / 32; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t j = j0 + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3);
-                s[b][r] = j < sees ? s[b][r] * c : -INFINITY;
-                top = fmaxf(top, s[b][r]);
-            }
-        top = half_max(top);
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+        top = half_max(top) * c;
         // the sums are moved to a new maximum only where it has grown by 2^8: exp2 then stays below 256 and nothing is lost
         if (__any(top > m + 8.f)) {
             const float to = fmaxf(m, top);
@@ -128,32 +149,39 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
         for (int b = 0; b < BK / 32; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - base);
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -base));
                 l += s[b][r];
             }
 #pragma unroll
         for (int b = 0; b < BK / 32; ++b)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const bf16x8 p = as_fragment(s[b], e);      // weights in bf16: at most 2^-9 off each, their sum l is of the unrounded ones
+                const bf16x8 p = as_fragment(s[b], e);      // weights in bf16: at most 2^-8 off each, their sum l is of the unrounded ones
 #pragma unroll
-                for (int d = 0; d < HD / 32; ++d) o[d] = mfma32(T::by_column(vt, 2 * b + e, d, lane), p, o[d]);
+                for (int d = 0; d < HD / 32; ++d) o[d] = mfma32(T::by_column(columns, 2 * b + e, d, kTileBytes), p, o[d]);
             }
-        if (t + 1 < n_tiles) {
-            ks.store(lds[cur ^ 1][0]);
-            vs.store(lds[cur ^ 1][1]);
-        }
-        __syncthreads();
+    };
+    if (n_tiles > 0) {
+        point(BK);
+        fetch(0);
+    }
+    tiles_ready();
+    for (int t = 0; t < n_tiles; ++t) {
+        if (t + 1 < n_tiles) fetch(t + 1);
+        if (t < needed) step(t);
+        tiles_ready();
     }
     l = half_sum(l);
-    store_own<HD>(o, l == 0.f ? 0.f : 1.f / l, out + (row0 * a.heads + head) * a.hd, static_cast<int64_t>(a.heads) * a.hd, own_valid, a.hd, lane);
-    if (lse_out && lane < own_valid && lane < 32)
-        lse_out[static_cast<int64_t>(head) * a.pq.T + row0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    store_own<HD>(o, l == 0.f ? 0.f : 1.f / l, out + (w.row0 * a.heads + head) * a.hd, static_cast<int64_t>(a.heads) * a.hd, w.own_valid, a.hd, lane);
+    if (lse_out && lane < w.own_valid && lane < 32)
+        lse_out[static_cast<int64_t>(head) * a.pq.T + w.row0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-// D_i = <do_i, o_i> in fp32: a group of 16 lanes takes a row of a head, 8 elements a lane.
-__global__ __launch_bounds__(256) void attention_row_dot_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ go, int64_t rows, int64_t T, int heads,
-                                                               int hd, float* __restrict__ dot) {
+// What the gradient needs of a row: -lse / scale, and behind all of those -D, D_i = <do_i, o_i>, in fp32.  They are what the products z and dp start from:
+// z / scale - lse / scale and dp - D come out of the matrix cores.  A row that sees nothing has lse = -inf, and is masked everywhere.
+// A group of 16 lanes takes a row of a head, 8 elements a lane.
+__global__ __launch_bounds__(256) void attention_row_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ go, const float* __restrict__ lse, int64_t rows,
+                                                            int64_t T, int heads, int hd, float scale, float* __restrict__ stats) {
     const int e = (threadIdx.x & 15) * 8;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * 16; base < rows; base += static_cast<int64_t>(gridDim.x) * 16) {
         const int64_t row = base + (threadIdx.x >> 4);       // token * heads + head
@@ -165,20 +193,24 @@ __global__ __launch_bounds__(256) void attention_row_dot_kernel(const uint16_t* 
         }
         const auto add = [](float u, float w) { return u + w; };
         sum = wave_step<1>(wave_step<2>(wave_step<4>(wave_step<8>(sum, add), add), add), add);
-        if (row < rows && (threadIdx.x & 15) == 0) dot[(row % heads) * T + row / heads] = sum;
+        if (row < rows && (threadIdx.x & 15) == 0) {
+            const int64_t at = (row % heads) * T + row / heads;
+            stats[at] = -lse[at] / scale;
+            stats[rows + at] = -sum;
+        }
     }
 }
 
 // dK and dV: a workgroup takes 128 keys of a kv head, a wavefront 32 of them (K and V as fragments in registers), and walks over the
-// queries of every head that reads them, 32 at a time: the sum over the shared heads is made in registers, in a fixed order.
+// queries of every head that reads them in tiles of 64: the sum over the shared heads is made in registers, in a fixed order.
 // S = Q K^T and dP = dO V^T have the own key as column; dV^T += dO^T P and dK^T += Q^T dS.
 template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ lse,
-                                                                        const float* __restrict__ dot, uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
-    constexpr int BQ = 32;
+__global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
+                                                                        uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
+    constexpr int BQ = 64;
     using T = Tile<HD>;
-    __shared__ __align__(16) unsigned char lds[2][2][BQ * T::kRowBytes];
-    __shared__ __align__(16) float stats[2][2][BQ];
+    constexpr int kTileBytes = BQ * T::kRowBytes, kSlot = 2 * kTileBytes + 2 * BQ * 4;
+    __shared__ __align__(1024) unsigned char lds[2][kSlot];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads;
     int kvh;
@@ -187,25 +219,24 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
     int segment;
     int64_t first, end;
     if (!find_tile<kOwn>(a.pk, tile, lane, segment, first, end)) return;
-    const int64_t k_begin = a.pk.bound(segment), nk = end - k_begin;
-    int64_t q_begin = 0, nq = 0;
+    const int64_t k_begin = a.pk.bound(segment), row0 = first + 32 * wave;
+    const int nk = uniform(static_cast<int>(end - k_begin)), own_valid = clamp32(end - row0), j0 = uniform(static_cast<int>(row0 - k_begin));
+    int64_t q_begin = 0;
+    int nq = 0;
     if (segment >= 1 && segment <= a.pk.n) {
         q_begin = a.pq.bound(segment);
-        nq = a.pq.bound(segment + 1) - q_begin;
-        if (nq < 0) nq = 0;
+        const int64_t n = a.pq.bound(segment + 1) - q_begin;
+        nq = uniform(static_cast<int>(n < 0 ? 0 : n));
     }
-    const int64_t row0 = first + 32 * wave;
-    const int own_valid = static_cast<int>(end - row0 < 32 ? (end - row0 < 0 ? 0 : end - row0) : 32);
-    const int64_t my_j = row0 - k_begin + (lane & 31);
     // key j is seen by queries i >= j + nq - nk (causal)
-    int64_t from = a.causal ? my_j + nq - nk : 0;
-    from = from < 0 ? 0 : from;
-    int64_t i_first = a.causal ? first - k_begin + nq - nk : 0;
-    i_first = i_first < 0 ? 0 : i_first;
-    const int64_t t_first = i_first / BQ;
-    int64_t n_t = (nq + BQ - 1) / BQ - t_first;
-    n_t = n_t < 0 ? 0 : n_t;
-    const int total = static_cast<int>(n_t) * per;
+    const auto seen_from = [&](int j) {
+        const int i = a.causal ? nq + (j - nk) : 0;
+        return i < 0 ? 0 : i;
+    };
+    const int from = seen_from(j0 + (lane & 31)), from_least = seen_from(j0), from_most = seen_from(j0 + 31);
+    const int t_first = seen_from(j0 - 32 * wave) / BQ;
+    const int n_t = (nq + BQ - 1) / BQ > t_first ? (nq + BQ - 1) / BQ - t_first : 0;
+    const int total = n_t * per;
 
     bf16x8 kf[HD / 16], vf[HD / 16];
     load_own<HD>(kf, a.k + row0 * a.k_stride + static_cast<int64_t>(kvh) * a.hd, a.k_stride, own_valid, a.hd, lane);
@@ -216,176 +247,184 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
     const float c = a.scale * kLog2e;
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
 
-    Staged<HD, BQ, kThreads> qs, gs;
-    float stat = 0.f;
-    int h = 0;
-    int64_t ti = t_first;                             // what is fetched next
-    const auto fetch = [&]() {
-        const int64_t i0 = ti * BQ;
-        const int head = kvh * per + h;
-        const int valid = static_cast<int>(nq - i0 < BQ ? nq - i0 : BQ);
-        qs.load(a.q + (q_begin + i0) * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, valid, a.hd);
-        gs.load(go + (q_begin + i0) * go_stride + static_cast<int64_t>(head) * a.hd, go_stride, valid, a.hd);
-        if (threadIdx.x < 2 * BQ) {
-            const int r = threadIdx.x & (BQ - 1);
-            const float* from_array = threadIdx.x < BQ ? lse : dot;
-            stat = r < valid ? from_array[static_cast<int64_t>(head) * a.pq.T + q_begin + i0 + r] : 0.f;
-            if (threadIdx.x < BQ) stat *= kLog2e;
+    Stream<HD, BQ, kWaves> qs, gs;
+    const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
+    int h = 0, ti = 0, pointed = 0;                   // head and tile that are fetched next
+    const auto fetch = [&](int slot) {
+        const int i0 = (t_first + ti) * BQ, valid = nq - i0 < BQ ? nq - i0 : BQ;
+        if (valid != pointed) {
+            qs.point(static_cast<unsigned>(a.q_stride) * 2, valid, a.hd, wave, lane);
+            gs.point(static_cast<unsigned>(go_stride) * 2, valid, a.hd, wave, lane);
+            pointed = valid;
         }
+        const int head = kvh * per + h;
+        const unsigned to = lds0 + slot * kSlot;
+        qs.issue(uniform(a.q + (q_begin + i0) * a.q_stride + static_cast<int64_t>(head) * a.hd), to, wave);
+        gs.issue(uniform(go + (q_begin + i0) * go_stride + static_cast<int64_t>(head) * a.hd), to + kTileBytes, wave);
+        if (wave < 2) {       // 64 rows' statistics, 4 bytes a lane, one kind a wavefront
+            const float* from_row = stats + (wave * a.heads + head) * a.pq.T + q_begin + i0 + (lane < valid ? lane : valid - 1);
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from_row), "s"(to + 2 * kTileBytes + wave * 256) : "memory");
+        }
+        if (++ti == n_t) ti = 0, ++h;
     };
-    const auto put = [&](int b) {
-        qs.store(lds[b][0]);
-        gs.store(lds[b][1]);
-        if (threadIdx.x < 2 * BQ) stats[b][threadIdx.x / BQ][threadIdx.x & (BQ - 1)] = stat;
-    };
-    const auto next = [&]() {
-        if (++ti == t_first + n_t) ti = t_first, ++h;
-    };
-    if (total > 0) {
-        fetch();
-        put(0);
-    }
-    __syncthreads();
-    for (int t = 0; t < total; ++t) {
-        const int cur = t & 1;
-        const int64_t i0 = ti * BQ;
-        next();
-        if (t + 1 < total) fetch();
-        const unsigned char *qt = lds[cur][0], *gt = lds[cur][1];
+    // 32 queries of a tile
+    const auto step = [&](int slot_index, int b, int i0) {
+        const unsigned slot = lds0 + slot_index * kSlot, block = slot + b * 32 * T::kRowBytes;
+        const unsigned rows = fresh(block + row_at), columns = fresh(block + column_at), st = slot + 2 * kTileBytes + b * 128 + half * 16;
         f32x16 s, dp;
-        s = 0.f;
-        dp = 0.f;
 #pragma unroll
-        for (int e = 0; e < HD / 16; ++e) s = mfma32(T::by_row(qt, lane & 31, e, half), kf[e], s);
+        for (int r = 0; r < 4; ++r) {
+            const f32x4 x = *(lds_f32x4_t)static_cast<uintptr_t>(st + 32 * r), y = *(lds_f32x4_t)static_cast<uintptr_t>(st + 32 * r + BQ * 4);
 #pragma unroll
-        for (int e = 0; e < HD / 16; ++e) dp = mfma32(T::by_row(gt, lane & 31, e, half), vf[e], dp);
+            for (int i = 0; i < 4; ++i) s[4 * r + i] = x[i], dp[4 * r + i] = y[i];
+        }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const f32x4 ls = *reinterpret_cast<const f32x4*>(&stats[cur][0][8 * b + 4 * half]);
-            const f32x4 ds = *reinterpret_cast<const f32x4*>(&stats[cur][1][8 * b + 4 * half]);
+        for (int e = 0; e < HD / 16; ++e) s = mfma32(T::by_row(rows, e, 0), kf[e], s);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t i = i0 + 8 * b + 4 * half + r;
-                const bool seen = i >= from && i < nq;
-                const float p = seen ? __builtin_amdgcn_exp2f(s[4 * b + r] * c - ls[r]) : 0.f;
-                dp[4 * b + r] = seen ? p * (dp[4 * b + r] - ds[r]) : 0.f;
-                s[4 * b + r] = p;
+        for (int e = 0; e < HD / 16; ++e) dp = mfma32(T::by_row(rows, e, kTileBytes), vf[e], dp);
+        if (i0 < from_most || i0 + 32 > nq) {       // some pair is not visible: its weight, exp2 of -inf, is 0
+            stay_branch();
+            const int lo = from - i0 - 4 * half, hi = nq - i0 - 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = 8 * (r >> 2) + (r & 3);
+                const bool seen = i >= lo && i < hi;
+                s[r] = seen ? s[r] : -INFINITY;
+                dp[r] = seen ? dp[r] : 0.f;
             }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+            dp[r] *= s[r];
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const bf16x8 p = as_fragment(s, e), ds = as_fragment(dp, e);    // both at most 2^-9 off, as in the forward pass
+            const bf16x8 p = as_fragment(s, e), ds = as_fragment(dp, e);    // both at most 2^-8 off, as in the forward pass
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) {
-                gv[d] = mfma32(T::by_column(gt, e, d, lane), p, gv[d]);
-                gk[d] = mfma32(T::by_column(qt, e, d, lane), ds, gk[d]);
+                gv[d] = mfma32(T::by_column(columns, e, d, kTileBytes), p, gv[d]);
+                gk[d] = mfma32(T::by_column(columns, e, d, 0), ds, gk[d]);
             }
         }
-        if (t + 1 < total) put(cur ^ 1);
-        __syncthreads();
+    };
+    if (total > 0) fetch(0);
+    tiles_ready();
+    int at = 0;
+    for (int t = 0; t < total; ++t) {
+        if (t + 1 < total) fetch((t + 1) & 1);
+        const int i0 = (t_first + at) * BQ;
+        if (++at == n_t) at = 0;
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+            const int i = i0 + 32 * b;
+            if (own_valid == 0 || i >= nq || i + 31 < from_least) continue;
+            step(t & 1, b, i);
+        }
+        tiles_ready();
     }
-    const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.hd, at = row0 * out_stride + static_cast<int64_t>(kvh) * a.hd;
-    store_own<HD>(gk, a.scale, dk + at, out_stride, own_valid, a.hd, lane);
-    store_own<HD>(gv, 1.f, dv + at, out_stride, own_valid, a.hd, lane);
+    const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.hd, to = row0 * out_stride + static_cast<int64_t>(kvh) * a.hd;
+    store_own<HD>(gk, a.scale, dk + to, out_stride, own_valid, a.hd, lane);
+    store_own<HD>(gv, 1.f, dv + to, out_stride, own_valid, a.hd, lane);
 }
 
-// dQ: a workgroup takes 128 queries of a head (Q and dO as fragments in registers) and walks over the keys, 32 at a time.
+// dQ: a workgroup takes 128 queries of a head (Q and dO as fragments in registers) and walks over the keys in tiles of 64.
 // S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
 template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ go, const float* __restrict__ lse,
-                                                                       const float* __restrict__ dot, uint16_t* __restrict__ dq) {
-    constexpr int BK = 32;
+__global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ go, const float* __restrict__ stats,
+                                                                       uint16_t* __restrict__ dq) {
+    constexpr int BK = 64;
     using T = Tile<HD>;
-    __shared__ __align__(16) unsigned char lds[2][2][BK * T::kRowBytes];
+    constexpr int kTileBytes = BK * T::kRowBytes;
+    __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads;
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
     const int head = kvh * per + static_cast<int>(rest % per);
-    const int64_t tile = tiles - 1 - rest / per;
-    int segment;
-    int64_t first, end;
-    if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, end)) return;
-    const int64_t q_begin = a.pq.bound(segment), nq = end - q_begin;
-    int64_t k_begin = 0, nk = 0;
-    if (segment >= 1 && segment <= a.pq.n) {
-        k_begin = a.pk.bound(segment);
-        nk = a.pk.bound(segment + 1) - k_begin;
-        if (nk < 0) nk = 0;
-    }
-    const int64_t row0 = first + 32 * wave;
-    const int own_valid = static_cast<int>(end - row0 < 32 ? (end - row0 < 0 ? 0 : end - row0) : 32);
-    int64_t sees = a.causal ? row0 - q_begin + (lane & 31) + 1 + nk - nq : nk;
-    sees = sees < 0 ? 0 : sees < nk ? sees : nk;
-    const int64_t last_i = (end - first < kOwn ? end - first : kOwn) - 1 + first - q_begin;
-    int64_t reach = a.causal ? last_i + 1 + nk - nq : nk;
-    reach = reach < 0 ? 0 : reach < nk ? reach : nk;
-    const int n_tiles = static_cast<int>((reach + BK - 1) / BK);
+    QueryBlock w;
+    if (!w.find(a, tiles - 1 - rest / per, wave, lane)) return;
+    const int n_tiles = (w.reach + BK - 1) / BK;
 
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
     bf16x8 qf[HD / 16], gf[HD / 16];
-    load_own<HD>(qf, a.q + row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, own_valid, a.hd, lane);
-    load_own<HD>(gf, go + row0 * go_stride + static_cast<int64_t>(head) * a.hd, go_stride, own_valid, a.hd, lane);
-    float my_lse = 0.f, my_dot = 0.f;
-    if ((lane & 31) < own_valid) {
-        const int64_t at = static_cast<int64_t>(head) * a.pq.T + row0 + (lane & 31);
-        my_lse = lse[at] * kLog2e;
-        my_dot = dot[at];
+    load_own<HD>(qf, a.q + w.row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, w.own_valid, a.hd, lane);
+    load_own<HD>(gf, go + w.row0 * go_stride + static_cast<int64_t>(head) * a.hd, go_stride, w.own_valid, a.hd, lane);
+    float mine[2] = {0.f, 0.f};
+    if ((lane & 31) < w.own_valid) {
+        const float* at = stats + static_cast<int64_t>(head) * a.pq.T + w.row0 + (lane & 31);
+        mine[0] = at[0], mine[1] = at[static_cast<int64_t>(a.heads) * a.pq.T];
     }
-    const uint16_t* kp = a.k + k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd;
-    const uint16_t* vp = a.v + k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd;
+    const uint16_t* kp = uniform(a.k + w.k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* vp = uniform(a.v + w.k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
     f32x16 gq[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) gq[d] = 0.f;
     const float c = a.scale * kLog2e;
-    Staged<HD, BK, kThreads> ks, vs;
-    const auto fetch = [&](int t) {
-        const int64_t j0 = static_cast<int64_t>(t) * BK;
-        const int valid = static_cast<int>(nk - j0 < BK ? nk - j0 : BK);
-        ks.load(kp + j0 * a.k_stride, a.k_stride, valid, a.hd);
-        vs.load(vp + j0 * a.v_stride, a.v_stride, valid, a.hd);
+
+    Stream<HD, BK, kWaves> ks, vs;
+    const int whole = w.nk / BK;
+    const auto point = [&](int valid) {
+        ks.point(static_cast<unsigned>(a.k_stride) * 2, valid, a.hd, wave, lane);
+        vs.point(static_cast<unsigned>(a.v_stride) * 2, valid, a.hd, wave, lane);
     };
-    if (n_tiles > 0) {
-        fetch(0);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
-    }
-    __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        const int cur = t & 1;
-        if (t + 1 < n_tiles) fetch(t + 1);
-        const unsigned char *kt = lds[cur][0], *vt = lds[cur][1];
+    const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
+    const auto fetch = [&](int t) {
+        if (t == whole) point(w.nk - t * BK);
+        const unsigned to = lds0 + (t & 1) * 2 * kTileBytes;
+        ks.issue(kp, to, wave);
+        vs.issue(vp, to + kTileBytes, wave);
+        kp += BK * a.k_stride;
+        vp += BK * a.v_stride;
+    };
+    const auto step = [&](int t, int b, int j0) {
+        const unsigned block = lds0 + (t & 1) * 2 * kTileBytes + b * 32 * T::kRowBytes, rows = fresh(block + row_at), columns = fresh(block + column_at);
         f32x16 s, dp;
-        s = 0.f;
-        dp = 0.f;
+        s = mine[0];
+        dp = mine[1];
 #pragma unroll
-        for (int e = 0; e < HD / 16; ++e) s = mfma32(T::by_row(kt, lane & 31, e, half), qf[e], s);
+        for (int e = 0; e < HD / 16; ++e) s = mfma32(T::by_row(rows, e, 0), qf[e], s);
 #pragma unroll
-        for (int e = 0; e < HD / 16; ++e) dp = mfma32(T::by_row(vt, lane & 31, e, half), gf[e], dp);
-        const int64_t j0 = static_cast<int64_t>(t) * BK;
+        for (int e = 0; e < HD / 16; ++e) dp = mfma32(T::by_row(rows, e, kTileBytes), gf[e], dp);
+        if (j0 + 32 > w.sees_least) {       // some row does not see all of the keys
+            stay_branch();
+            const int limit = w.sees - j0 - 4 * half;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t j = j0 + 8 * (r >> 2) + 4 * half + (r & 3);
-            dp[r] = j < sees ? __builtin_amdgcn_exp2f(s[r] * c - my_lse) * (dp[r] - my_dot) : 0.f;
+            for (int r = 0; r < 16; ++r) {
+                const bool seen = 8 * (r >> 2) + (r & 3) < limit;
+                s[r] = seen ? s[r] : -INFINITY;
+                dp[r] = seen ? dp[r] : 0.f;
+            }
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= __builtin_amdgcn_exp2f(s[r] * c);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const bf16x8 ds = as_fragment(dp, e);
 #pragma unroll
-            for (int d = 0; d < HD / 32; ++d) gq[d] = mfma32(T::by_column(kt, e, d, lane), ds, gq[d]);
+            for (int d = 0; d < HD / 32; ++d) gq[d] = mfma32(T::by_column(columns, e, d, 0), ds, gq[d]);
         }
-        if (t + 1 < n_tiles) {
-            ks.store(lds[cur ^ 1][0]);
-            vs.store(lds[cur ^ 1][1]);
-        }
-        __syncthreads();
+    };
+    if (n_tiles > 0) {
+        point(BK);
+        fetch(0);
     }
-    store_own<HD>(gq, a.scale, dq + (row0 * a.heads + head) * a.hd, go_stride, own_valid, a.hd, lane);
+    tiles_ready();
+    for (int t = 0; t < n_tiles; ++t) {
+        if (t + 1 < n_tiles) fetch(t + 1);
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {
+            const int j = t * BK + 32 * b;
+            if (j < w.sees_most) step(t, b, j);
+        }
+        tiles_ready();
+    }
+    store_own<HD>(gq, a.scale, dq + (w.row0 * a.heads + head) * a.hd, go_stride, w.own_valid, a.hd, lane);
 }
 
 bool row_stride_ok(int64_t stride, int64_t rows, int heads, int hd) {
-    return stride % 8 == 0 && stride >= static_cast<int64_t>(heads) * hd && stride <= (int64_t{1} << 31) && rows <= (int64_t{1} << 31);
+    return stride % 8 == 0 && stride >= static_cast<int64_t>(heads) * hd && stride <= (int64_t{1} << 24) && rows <= (int64_t{1} << 30);
 }
 
 // ARROL_OK, or what is wrong with the arguments that both calls share
@@ -410,7 +449,7 @@ Problem problem(const void* q, int64_t q_stride, const void* k, int64_t k_stride
     return a;
 }
 
-size_t dot_bytes(int64_t T, int heads) { return (static_cast<size_t>(T) * heads * sizeof(float) + 255) / 256 * 256; }
+size_t stat_bytes(int64_t T, int heads) { return static_cast<size_t>(T) * heads * 2 * sizeof(float); }
 
 }  // namespace
 
@@ -431,7 +470,7 @@ extern "C" int arrol_attention(const void* q, int64_t q_stride, const void* k, i
 }
 
 extern "C" size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int32_t n_heads) {
-    return T_q <= 0 || n_heads <= 0 ? 0 : dot_bytes(T_q, n_heads);
+    return T_q <= 0 || n_heads <= 0 ? 0 : stat_bytes(T_q, n_heads);
 }
 
 extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -443,26 +482,26 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
     if (const int rc = check(a, T_q, T_k)) return rc;
     if (T_q > 0 && (!out || !lse || !grad_out || !grad_q || !arrol_aligned16(out) || !arrol_aligned16(grad_out) || !arrol_aligned16(grad_q))) return ARROL_EINVAL;
     if (T_k > 0 && (!grad_k || !grad_v || !arrol_aligned16(grad_k) || !arrol_aligned16(grad_v))) return ARROL_EINVAL;
-    if (T_q > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < dot_bytes(T_q, n_heads))) return ARROL_EWORKSPACE;
+    if (T_q > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < stat_bytes(T_q, n_heads))) return ARROL_EWORKSPACE;
     const auto st = static_cast<hipStream_t>(stream);
     const auto *go = static_cast<const uint16_t*>(grad_out);
-    float* dot = static_cast<float*>(workspace);
+    auto* stats = static_cast<float*>(workspace);
     if (T_q > 0) {
-        const int64_t rows = T_q * n_heads;
-        arrol_launch(attention_row_dot_kernel, dim3(static_cast<unsigned>((rows + 15) / 16 < kDotBlocks ? (rows + 15) / 16 : kDotBlocks)), dim3(256), 0, st, static_cast<const uint16_t*>(out), go, rows, T_q,
-                     n_heads, head_dim, dot);
+        const int64_t rows = T_q * n_heads, blocks = (rows + 15) / 16;
+        arrol_launch(attention_row_kernel, dim3(static_cast<unsigned>(blocks < kRowBlocks ? blocks : kRowBlocks)), dim3(256), 0, st, static_cast<const uint16_t*>(out), go,
+                     lse, rows, T_q, n_heads, head_dim, scale, stats);
     }
     if (T_k > 0) {
         const dim3 grid(static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads));
         auto *dk = static_cast<uint16_t*>(grad_k), *dv = static_cast<uint16_t*>(grad_v);
-        if (head_dim <= 64) arrol_launch(attention_grad_kv_kernel<64>, grid, dim3(kThreads), 0, st, a, go, lse, dot, dk, dv);
-        else arrol_launch(attention_grad_kv_kernel<128>, grid, dim3(kThreads), 0, st, a, go, lse, dot, dk, dv);
+        if (head_dim <= 64) arrol_launch(attention_grad_kv_kernel<64>, grid, dim3(kThreads), 0, st, a, go, stats, dk, dv);
+        else arrol_launch(attention_grad_kv_kernel<128>, grid, dim3(kThreads), 0, st, a, go, stats, dk, dv);
     }
     if (T_q > 0) {
         const int64_t tiles = tile_bound(T_q, n_seq, kOwn);
         const dim3 grid(static_cast<unsigned>(tiles * n_heads));
-        if (head_dim <= 64) arrol_launch(attention_grad_q_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, go, lse, dot, static_cast<uint16_t*>(grad_q));
-        else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, go, lse, dot, static_cast<uint16_t*>(grad_q));
+        if (head_dim <= 64) arrol_launch(attention_grad_q_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, go, stats, static_cast<uint16_t*>(grad_q));
+        else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, go, stats, static_cast<uint16_t*>(grad_q));
     }
     return arrol_launch_status();
 }

@@ -19,6 +19,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
+typedef const __attribute__((address_space(3))) bf16x8* lds_bf16x8_t;
+typedef const __attribute__((address_space(3))) f32x4* lds_f32x4_t;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -35,48 +37,79 @@ struct Tile {
         if constexpr (HD == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
         else return ((r & 2) << 1) | ((r >> 2) & 3);     // odd rows lie 128 bytes on by themselves
     }
-    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ swizzle(r)) << 4); }
-    // A fragment for a product over the head: row `row`, K16 step s
-    __device__ static __forceinline__ bf16x8 by_row(const unsigned char* tile, int row, int s, int half) {
-        return *reinterpret_cast<const bf16x8*>(tile + at(row, 2 * s + half));
+    // Fragments are read at `base` (an LDS address; what a lane adds to a tile's, plus the tile's, a multiple of 256) with the K16 step or the block of
+    // 32 head elements exclusive-ored in and everything else as the instruction's own offset: one address register each for the two ways.
+    // By row: A fragment for a product over the head, lane = row, K16 step s.
+    __device__ static __forceinline__ unsigned row_base(int lane) {
+        const int row = lane & 31;
+        return row * kRowBytes + (((lane >> 5) ^ swizzle(row)) << 4);
     }
-    // A fragment for a product over the tile's rows 16 s .. 16 s + 15, head elements 32 d .. 32 d + 31: the transposing read gives lane j
-    // of a block of 16 the four rows' values of head element j, lane 4 e + q holding the address of row e, elements 4 q .. 4 q + 3
-    __device__ static __forceinline__ bf16x8 by_column(const unsigned char* tile, int s, int d, int lane) {
-        const int row = 16 * s + 4 * (lane >> 5) + ((lane >> 2) & 3);
-        const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), within = (lane & 1) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(tile + at(row, chunk) + within));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(tile + at(row + 8, chunk) + within));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_bit_cast(bf16x8, v);
+    __device__ static __forceinline__ bf16x8 by_row(unsigned base, int s, int offset) {
+        return *(lds_bf16x8_t)static_cast<uintptr_t>((base ^ (s << 5)) + offset);
+    }
+    // By column: A fragment for a product over the tile's rows 16 s .. 16 s + 15, head elements 32 d .. 32 d + 31.  The transposing read gives lane j
+    // of a block of 16 the four rows' values of head element j, lane 4 e + q holding the address of row e, elements 4 q .. 4 q + 3.  (Eight rows on,
+    // bit 1 of the swizzle changes; sixteen on, none.)
+    __device__ static __forceinline__ unsigned column_base(int lane) {
+        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), chunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        return row * kRowBytes + ((chunk ^ swizzle(row)) << 4) + (lane & 1) * 8;
+    }
+    __device__ static __forceinline__ bf16x8 by_column(unsigned base, int s, int d, int offset) {
+        const unsigned at = base ^ (d << 6);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)static_cast<uintptr_t>(at + (16 * s * kRowBytes + offset)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)static_cast<uintptr_t>((at ^ 32) + ((16 * s + 8) * kRowBytes + offset)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };
 
-// ROWS rows on their way from memory to the LDS through registers: rows past `valid` and head elements past hd become zeros,
-// whatever lies there (another sequence's rows, or nothing that may be read).
-template <int HD, int ROWS, int THREADS>
-struct Staged {
-    static constexpr int kPer = ROWS * Tile<HD>::kChunks / THREADS;
-    static_assert(kPer * THREADS == ROWS * Tile<HD>::kChunks, "whole rounds");
-    u32x4 x[kPer];
-    __device__ __forceinline__ void load(const uint16_t* base, int64_t stride, int valid, int hd) {
+// The same value, of which the compiler knows nothing: what is computed from it in a loop is not kept in registers over the loop.
+__device__ __forceinline__ unsigned fresh(unsigned v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// In a branch that is seldom taken: keeps it one (the compiler would do its selects always, 64 instructions a tile).
+__device__ __forceinline__ void stay_branch() { asm volatile(""); }
+
+// ROWS rows on their way from memory straight into the LDS (16 bytes a lane, no registers): an instruction fills 1,024 bytes of the tile in order, so
+// the lane that fills a position fetches the chunk that belongs there.  Rows past `valid` (>= 1) are the last valid row once more and
+// chunks past the head the head's last: what is made of them is masked, or multiplied by zeros of the other operand, or not
+// stored, and it is never more than that row's own NaN that goes along.  Addresses are a scalar base and 32-bit offsets in the lanes.
+template <int HD, int ROWS, int WAVES>
+struct Stream {
+    static constexpr int kPer = ROWS * Tile<HD>::kRowBytes / 1024 / WAVES;      // instructions of a wavefront
+    static_assert(kPer * 1024 * WAVES == ROWS * Tile<HD>::kRowBytes, "whole instructions");
+    unsigned offset[kPer];
+    __device__ __forceinline__ void point(unsigned stride_bytes, int valid, int hd, int wave, int lane) {
+        const int last = hd / 8 - 1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int id = threadIdx.x + i * THREADS, row = id / Tile<HD>::kChunks, c = id % Tile<HD>::kChunks;
-            u32x4 v = {0, 0, 0, 0};
-            if (row < valid && c * 8 < hd) v = *reinterpret_cast<const u32x4*>(base + row * stride + c * 8);
-            x[i] = v;
+            const int r = (wave * kPer + i) * (64 / Tile<HD>::kChunks) + lane / Tile<HD>::kChunks;
+            const int c = (lane % Tile<HD>::kChunks) ^ Tile<HD>::swizzle(r);
+            offset[i] = static_cast<unsigned>(r < valid ? r : valid - 1) * stride_bytes + static_cast<unsigned>(c < last ? c : last) * 16;
         }
     }
-    __device__ __forceinline__ void store(unsigned char* tile) const {
+    __device__ __forceinline__ void issue(const uint16_t* base, unsigned lds, int wave) const {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int id = threadIdx.x + i * THREADS;
-            *reinterpret_cast<u32x4*>(tile + Tile<HD>::at(id / Tile<HD>::kChunks, id % Tile<HD>::kChunks)) = x[i];
+            const unsigned to = lds + (wave * kPer + i) * 1024;
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset[i]), "s"(base), "s"(to) : "memory");
         }
     }
 };
+
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+    return static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p));
+}
+template <class T>
+__device__ __forceinline__ T* uniform(T* p) {       // the same pointer in every lane, in scalar registers
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(u >> 32));
+    return reinterpret_cast<T*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// Waits for this wavefront's loads into the LDS and its reads of it, then for the workgroup.
+__device__ __forceinline__ void tiles_ready() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // B fragments of the wavefront's own 32 rows (lane = row), zeros past `valid` and hd.
 template <int HD>
