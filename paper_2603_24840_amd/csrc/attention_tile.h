@@ -201,6 +201,6 @@ template <unsigned ROWS>
 __device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
     return find_tile<ROWS>([&](int s) { return p.bound(s); }, p.n + 2, tile, lane, segment, first, end);
 }
-inline int64_t tile_bound(int64_t T, int n, int rows) { return T / rows + n + 2; }
+__host__ __device__ inline int64_t tile_bound(int64_t T, int n, int rows) { return T / rows + n + 2; }
 
 }  // namespace attention

@@ -69,8 +69,8 @@ def test_decode_refuses(L):
     import paper_2603_24840_amd as A
     lay = lambda **kw: A.KVLayout(*[kw.get(x, y) for x, y in (("layers", 2), ("page", 16), ("KV", 2), ("hd", 64), ("pages", 128))])
     for bad in (dict(q=None), dict(q=ODD), dict(kv=None), dict(kv=ODD), dict(table=None), dict(lens=None), dict(out=None), dict(out=ODD), dict(n=-1), dict(H=7), dict(H=0), dict(layer=2),
-                dict(layer=-1), dict(width=0), dict(width=2 ** 31 - 1), dict(pt=None), dict(pl=None), dict(off=None), dict(pw=0), dict(groups=-1), dict(groups=65536), dict(scale=0.0),
-                dict(scale=float("nan")), dict(win=FAKE), dict(pwin=FAKE), dict(groups=0, pwout=FAKE), dict(n=70000, wout=FAKE), dict(lay=lay(layers=0)), dict(lay=lay(page=0)), dict(lay=lay(KV=0)),
+                dict(layer=-1), dict(width=0), dict(width=2 ** 31 - 1), dict(pt=None), dict(pl=None), dict(off=None), dict(pw=0), dict(groups=-1), dict(groups=2 ** 20 + 1), dict(scale=0.0),
+                dict(scale=float("nan")), dict(win=FAKE), dict(pwin=FAKE), dict(groups=0, pwout=FAKE), dict(n=2 ** 24, wout=FAKE), dict(lay=lay(layers=0)), dict(lay=lay(page=0)), dict(lay=lay(KV=0)),
                 dict(lay=lay(KV=3)), dict(lay=lay(hd=12)), dict(lay=lay(hd=256)), dict(lay=lay(pages=-1)), dict(lay=lay(pages=2 ** 31))):
         assert decode(L, **bad) == -1, bad
     assert decode(L, n=0, groups=0, ws=None, nbytes=0, q=None, kv=None) == 0
