@@ -138,7 +138,7 @@ class _NoMarshal:
         return None
 
 
-MARSHAL_INTERFACE = 2    # of setup() and the argument lists of marshal.cpp; 1 was without a number
+MARSHAL_INTERFACE = 3    # of setup() and the calls and argument lists of marshal.cpp; 1 was without a number
 
 
 def built_for():
@@ -758,11 +758,20 @@ def _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale):
     return (q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2]), ends
 
 
-@_on_stream
-def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, stream=None):
+def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, *, stream=None):
     """Attention over packed sequences: q bf16 [T_q, n_heads, head_dim], k and v bf16 [T_k, n_kv_heads, head_dim] (rows may be strided),
     cu_seqlens int64 [n_seq+1] of the queries and, where they differ, cu_seqlens_k of the keys; scale None: head_dim ** -0.5.
     -> (out bf16 [T_q, n_heads, head_dim], lse fp32 [n_heads, T_q])."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out)
+        if result is not None:
+            return result
+        return _py_attention.__wrapped__(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out)
+    return _py_attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, stream=stream)
+
+
+@_on_stream
+def _py_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, stream=None):
     head, ends = _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale)
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
@@ -774,10 +783,19 @@ def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=N
     return out, lse
 
 
-@_on_stream
-def arrol_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, workspace=None, stream=None):
+def arrol_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, workspace=None, *, stream=None):
     """Gradient of arrol_attention, given its out and lse and grad_out = dL/dout: -> dict(grad_q, grad_k, grad_v), bf16 in the shapes of
     q, k and v."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k, causal, scale, workspace)
+        if result is not None:
+            return result
+        return _py_attention_grad.__wrapped__(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k, causal, scale, workspace)
+    return _py_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k, causal, scale, workspace, stream=stream)
+
+
+@_on_stream
+def _py_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, workspace=None, stream=None):
     head, ends = _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale)
     if out.shape != q.shape or grad_out.shape != q.shape or lse.shape != (q.shape[1], q.shape[0]):
         raise ValueError("out and grad_out must have the shape of q, lse [n_heads, T_q]")
@@ -793,15 +811,29 @@ def arrol_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=N
     return grads
 
 
-@_on_stream
 def arrol_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None, prefix_len=None, group_offsets=None, scale=None,
                            want_weight=False, weight=None, prefix_weight=None, out_weight=None, out_prefix_weight=None, workspace=None,
-                           stream=None):
+                           *, stream=None):
     """Attention of one new token per rollout over one layer of the paged pool: q bf16 [n, n_heads, head_dim], kv the pool, block_table
     int32 [n, pages] and seq_len int32 [n] of the rollouts' own tokens; with prefix_table int32 [groups, pages], prefix_len int32 [groups]
     and group_offsets int64 [groups+1] the rollouts of a group share its prefix.  want_weight: the attention weight of every token is added to
     weight fp32 [n, pages * page_tokens] and prefix_weight (None: zeros) into out_weight and out_prefix_weight (None: new; may be the inputs).
     -> dict(out bf16 [n, n_heads, head_dim], lse fp32 [n, n_heads], weight, prefix_weight (None where not wanted or without prefixes))."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).decode_attention(q, kv, layer, block_table, seq_len, prefix_table, prefix_len, group_offsets, scale, want_weight, weight, prefix_weight,
+                      out_weight, out_prefix_weight, workspace)
+        if result is not None:
+            return result
+        return _py_decode_attention.__wrapped__(q, kv, layer, block_table, seq_len, prefix_table, prefix_len, group_offsets, scale, want_weight, weight, prefix_weight,
+                      out_weight, out_prefix_weight, workspace)
+    return _py_decode_attention(q, kv, layer, block_table, seq_len, prefix_table, prefix_len, group_offsets, scale, want_weight, weight, prefix_weight,
+                      out_weight, out_prefix_weight, workspace, stream=stream)
+
+
+@_on_stream
+def _py_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None, prefix_len=None, group_offsets=None, scale=None,
+                         want_weight=False, weight=None, prefix_weight=None, out_weight=None, out_prefix_weight=None, workspace=None,
+                         stream=None):
     if q.dim() != 3 or block_table.dim() != 2 or block_table.shape[0] != q.shape[0] or seq_len.numel() != q.shape[0]:
         raise ValueError("q must be [n, n_heads, head_dim], block_table [n, pages], seq_len [n]")
     n, H, hd = q.shape
@@ -843,11 +875,20 @@ def arrol_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None
     return dict(out=out, lse=lse, weight=out_weight, prefix_weight=out_prefix_weight)
 
 
-@_on_stream
-def arrol_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, position=None, out=None, workspace=None, stream=None):
+def arrol_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, position=None, out=None, workspace=None, *, stream=None):
     """Cuts every row's cache to `budget` tokens by their gathered attention weight (kv is modified in place): block_table int32 [rows, pages],
     seq_len int32 [rows], weight fp32 and position (None: the slots themselves) int32 [rows, pages * page_tokens].
     -> dict(block_table, seq_len, weight, position); `out`: such a dict to write into, whose tensors may be the inputs."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).evict(kv, block_table, seq_len, weight, budget, n_first, n_recent, position, out, workspace)
+        if result is not None:
+            return result
+        return _py_evict.__wrapped__(kv, block_table, seq_len, weight, budget, n_first, n_recent, position, out, workspace)
+    return _py_evict(kv, block_table, seq_len, weight, budget, n_first, n_recent, position, out, workspace, stream=stream)
+
+
+@_on_stream
+def _py_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, position=None, out=None, workspace=None, stream=None):
     if block_table.dim() != 2 or seq_len.numel() != block_table.shape[0]:
         raise ValueError("block_table must be [rows, pages], seq_len [rows]")
     rows, width = block_table.shape

@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstring>
 
 #include "arrol.h"
@@ -461,6 +462,199 @@ PyObject* grpo_objective(Args& a) {
     return tuple(wrap(std::move(J)), want ? wrap(std::move(grad)) : keep(Py_None), wrap(std::move(clip)));
 }
 
+// [rows, heads, head_dim] bf16, rows strided, the heads of a row contiguous
+struct Heads {
+    const at::Tensor& t;
+    int64_t n = 0, stride = 0;
+    int32_t heads = 0, hd = 0;
+    Heads(Args& a, int i) : t(a.tensor(i)) {
+        if (a.odd || a.refuse(t.dim() != 3 || t.scalar_type() != at::kBFloat16)) return;
+        const int64_t h = t.size(1), d = t.size(2);
+        if (a.refuse((d > 1 && t.stride(2) != 1) || (h > 1 && t.stride(1) != d) || h > INT32_MAX || d > INT32_MAX)) return;
+        n = t.size(0), heads = static_cast<int32_t>(h), hd = static_cast<int32_t>(d);
+        stride = n > 1 ? t.stride(0) : (h * d > t.stride(0) / 8 * 8 ? h * d : t.stride(0) / 8 * 8);
+    }
+};
+
+// q, k, v, at `from`; cu_seqlens, cu_seqlens_k, causal, scale at `behind`
+struct Packed {
+    Heads q, k, v;
+    const int64_t *cu = nullptr, *cu_k = nullptr;
+    int32_t n = 0, causal = 0;
+    float scale = 0.f;
+    Packed(Args& a, int from, int behind) : q(a, from), k(a, from + 1), v(a, from + 2) {
+        if (a.odd || a.refuse(k.n != v.n || k.heads != v.heads || k.hd != v.hd || k.hd != q.hd)) return;
+        const at::Tensor& c = a.tensor(behind, at::kLong);
+        if (a.odd || a.refuse(c.numel() < 1 || c.numel() > INT32_MAX || (!a.given(behind + 1) && k.n != q.n))) return;
+        n = static_cast<int32_t>(c.numel() - 1);
+        cu = static_cast<const int64_t*>(data(c));
+        cu_k = a.ptr<int64_t>(behind + 1, at::kLong, c.numel());
+        causal = a.truth(behind + 2);
+        scale = static_cast<float>(a.given(behind + 3) ? a.number(behind + 3) : std::pow(static_cast<double>(q.hd), -0.5));
+    }
+};
+
+// q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out
+PyObject* attention(Args& a) {
+    const Packed p(a, 0, 3);
+    if (a.odd) return nullptr;
+    void* po = a.ptr(7, at::kBFloat16);
+    if (a.given(7) && a.refuse(a.odd || a.tensor(7).sizes() != p.q.t.sizes())) return nullptr;
+    void* st = stream(a, p.q.t);
+    if (a.odd) return nullptr;
+    at::Tensor out, lse;
+    const bool own = !a.given(7);
+    if (failed("arrol_attention", launch([&] {
+            if (own) po = made(out, p.q.t.sizes(), at::kBFloat16, p.q.t);
+            float* pl = made<float>(lse, {p.q.heads, p.q.n}, at::kFloat, p.q.t);
+            return arrol_attention(data(p.q.t), p.q.stride, data(p.k.t), p.k.stride, data(p.v.t), p.v.stride, p.cu, p.cu_k, p.q.n, p.k.n, p.n, p.q.heads,
+                                   p.k.heads, p.q.hd, p.causal, p.scale, po, pl, st);
+        })))
+        return nullptr;
+    return tuple(own ? wrap(std::move(out)) : keep(a[7]), wrap(std::move(lse)));
+}
+
+// q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k, causal, scale, workspace
+PyObject* attention_grad(Args& a) {
+    const Packed p(a, 0, 6);
+    if (a.odd) return nullptr;
+    const at::Tensor &o = a.tensor(3, at::kBFloat16), &go = a.tensor(5, at::kBFloat16), &lse = a.tensor(4, at::kFloat);
+    if (a.odd || a.refuse(o.sizes() != p.q.t.sizes() || go.sizes() != p.q.t.sizes() || lse.dim() != 2 || lse.size(0) != p.q.heads || lse.size(1) != p.q.n)) return nullptr;
+    void* st = stream(a, p.q.t);
+    if (a.odd) return nullptr;
+    const size_t need = arrol_attention_grad_workspace_bytes(p.q.n, p.q.heads);
+    Scratch ws(a, 10, need > 16 ? need : 16);
+    if (a.odd) return nullptr;
+    at::Tensor gq, gk, gv;
+    if (failed("arrol_attention_grad", launch([&] {
+            ws.get(p.q.t);
+            void *pq = made(gq, p.q.t.sizes(), at::kBFloat16, p.q.t), *pk = made(gk, p.k.t.sizes(), at::kBFloat16, p.q.t), *pv = made(gv, p.k.t.sizes(), at::kBFloat16, p.q.t);
+            return arrol_attention_grad(data(p.q.t), p.q.stride, data(p.k.t), p.k.stride, data(p.v.t), p.v.stride, data(o), static_cast<const float*>(data(lse)),
+                                        data(go), p.cu, p.cu_k, p.q.n, p.k.n, p.n, p.q.heads, p.k.heads, p.q.hd, p.causal, p.scale, pq, pk, pv, ws.p, ws.bytes, st);
+        })))
+        return nullptr;
+    PyObject* out = PyDict_New();
+    if (!out) return nullptr;
+    if (!put(out, "grad_q", wrap(std::move(gq))) || !put(out, "grad_k", wrap(std::move(gk))) || !put(out, "grad_v", wrap(std::move(gv)))) {
+        Py_DECREF(out);
+        return nullptr;
+    }
+    return out;
+}
+
+// the KV pool and its geometry
+struct Pool {
+    const at::Tensor& t;
+    arrol_kv_layout layout{};
+    Pool(Args& a, int i) : t(a.tensor(i, at::kBFloat16)) {
+        if (a.odd || a.refuse(t.dim() != 6 || t.size(1) != 2)) return;
+        for (int d : {0, 3, 4, 5}) a.refuse(t.size(d) > INT32_MAX);
+        layout = {static_cast<int32_t>(t.size(0)), static_cast<int32_t>(t.size(3)), static_cast<int32_t>(t.size(4)), static_cast<int32_t>(t.size(5)), t.size(2)};
+    }
+};
+
+// a block table [rows, pages] and its lengths
+struct Table {
+    const int32_t *ids = nullptr, *len = nullptr;
+    int32_t rows = 0, width = 0;
+    Table(Args& a, int table, int length) {
+        const at::Tensor& t = a.tensor(table, at::kInt);
+        if (a.odd || a.refuse(t.dim() != 2 || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)) return;
+        rows = static_cast<int32_t>(t.size(0)), width = static_cast<int32_t>(t.size(1));
+        ids = static_cast<const int32_t*>(data(t));
+        len = a.ptr<int32_t>(length, at::kInt, rows);
+        a.refuse(!a.given(length));
+    }
+    Table() = default;
+};
+
+// a given [rows, tokens] array of a table
+template <class T>
+T* per_token(Args& a, int i, at::ScalarType type, int64_t rows, int64_t tokens) {
+    if (!a.given(i)) return nullptr;
+    const at::Tensor& t = a.tensor(i, type);
+    return a.odd || a.refuse(t.dim() != 2 || t.size(0) != rows || t.size(1) != tokens) ? nullptr : static_cast<T*>(data(t));
+}
+
+// q, kv, layer, block_table, seq_len, prefix_table, prefix_len, group_offsets, scale, want_weight, weight, prefix_weight, out_weight, out_prefix_weight, workspace
+PyObject* decode_attention(Args& a) {
+    const at::Tensor& q = a.tensor(0, at::kBFloat16);
+    const Pool kv(a, 1);
+    const int32_t layer = a.integer(2);
+    const Table own(a, 3, 4);
+    if (a.odd || a.refuse(q.dim() != 3 || q.size(0) != own.rows || q.size(1) > INT32_MAX || q.size(2) != kv.layout.head_dim)) return nullptr;
+    const bool grouped = a.given(5), want = a.truth(9);
+    if (a.refuse(a.given(6) != grouped || a.given(7) != grouped)) return nullptr;
+    const Table pre = grouped ? Table(a, 5, 6) : Table();
+    if (a.odd || a.refuse(grouped && pre.rows == 0)) return nullptr;
+    const int64_t* offsets = a.ptr<int64_t>(7, at::kLong, pre.rows + int64_t{1});
+    const float scale = static_cast<float>(a.given(8) ? a.number(8) : std::pow(static_cast<double>(kv.layout.head_dim), -0.5));
+    const int64_t tokens = static_cast<int64_t>(own.width) * kv.layout.page_tokens, pre_tokens = static_cast<int64_t>(pre.width) * kv.layout.page_tokens;
+    if (a.refuse((!want && (a.given(10) || a.given(12))) || ((!want || !grouped) && (a.given(11) || a.given(13))))) return nullptr;
+    const float *in = per_token<float>(a, 10, at::kFloat, own.rows, tokens), *pre_in = per_token<float>(a, 11, at::kFloat, pre.rows, pre_tokens);
+    float *pw = per_token<float>(a, 12, at::kFloat, own.rows, tokens), *pp = per_token<float>(a, 13, at::kFloat, pre.rows, pre_tokens);
+    if (a.odd) return nullptr;
+    void* st = stream(a, q);
+    if (a.odd) return nullptr;
+    const int32_t H = static_cast<int32_t>(q.size(1));
+    const size_t need = arrol_decode_attention_workspace_bytes(own.rows, H, kv.layout.n_kv_heads, kv.layout.head_dim, kv.layout.page_tokens, own.width, pre.width, pre.rows, want);
+    Scratch ws(a, 14, need > 16 ? need : 16);
+    if (a.odd) return nullptr;
+    at::Tensor out, lse, w, p;
+    if (failed("arrol_decode_attention", launch([&] {
+            ws.get(q);
+            void* po = made(out, q.sizes(), at::kBFloat16, q);
+            float* pl = made<float>(lse, {own.rows, H}, at::kFloat, q);
+            if (want && !pw) pw = made<float>(w, {own.rows, tokens}, at::kFloat, q);
+            if (want && grouped && !pp) pp = made<float>(p, {pre.rows, pre_tokens}, at::kFloat, q);
+            return arrol_decode_attention(data(q), own.rows, H, data(kv.t), kv.layout, layer, own.ids, own.len, own.width, pre.ids, pre.len, pre.width, offsets, pre.rows, scale,
+                                          po, pl, in, pre_in, pw, pp, ws.p, ws.bytes, st);
+        })))
+        return nullptr;
+    PyObject* d = PyDict_New();
+    if (!d) return nullptr;
+    if (!put(d, "out", wrap(std::move(out))) || !put(d, "lse", wrap(std::move(lse))) || !put(d, "weight", w.defined() ? wrap(std::move(w)) : keep(a[12])) ||
+        !put(d, "prefix_weight", p.defined() ? wrap(std::move(p)) : keep(a[13]))) {
+        Py_DECREF(d);
+        return nullptr;
+    }
+    return d;
+}
+
+// kv, block_table, seq_len, weight, budget, n_first, n_recent, position, out, workspace
+PyObject* evict(Args& a) {
+    const Pool kv(a, 0);
+    const Table t(a, 1, 2);
+    if (a.odd || a.refuse(a.given(8) || !a.given(3))) return nullptr;
+    const int64_t tokens = static_cast<int64_t>(t.width) * kv.layout.page_tokens;
+    const float* w = per_token<float>(a, 3, at::kFloat, t.rows, tokens);
+    const int32_t budget = a.integer(4), first = a.integer(5), recent = a.integer(6);
+    const int32_t* position = per_token<int32_t>(a, 7, at::kInt, t.rows, tokens);
+    if (a.odd) return nullptr;
+    void* st = stream(a, kv.t);
+    if (a.odd) return nullptr;
+    const size_t need = arrol_evict_workspace_bytes(t.rows, t.width, kv.layout.page_tokens, budget);
+    Scratch ws(a, 9, need > 16 ? need : 16);
+    if (a.odd) return nullptr;
+    at::Tensor table, len, weight, place;
+    if (failed("arrol_evict", launch([&] {
+            ws.get(kv.t);
+            int32_t *pt = made<int32_t>(table, {t.rows, t.width}, at::kInt, kv.t), *pl = made<int32_t>(len, {t.rows}, at::kInt, kv.t);
+            float* pw = made<float>(weight, {t.rows, tokens}, at::kFloat, kv.t);
+            int32_t* pp = made<int32_t>(place, {t.rows, tokens}, at::kInt, kv.t);
+            return arrol_evict(data(kv.t), kv.layout, t.ids, t.len, t.rows, t.width, w, position, budget, first, recent, pt, pl, pw, pp, ws.p, ws.bytes, st);
+        })))
+        return nullptr;
+    PyObject* d = PyDict_New();
+    if (!d) return nullptr;
+    if (!put(d, "block_table", wrap(std::move(table))) || !put(d, "seq_len", wrap(std::move(len))) || !put(d, "weight", wrap(std::move(weight))) ||
+        !put(d, "position", wrap(std::move(place)))) {
+        Py_DECREF(d);
+        return nullptr;
+    }
+    return d;
+}
+
 template <PyObject* (*F)(Args&), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -506,7 +700,7 @@ PyMethodDef methods[] = {
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&setup)), METH_FASTCALL, nullptr},
     ENTRY(score, 7), ENTRY(score_mlp, 7), ENTRY(score_grad, 6), ENTRY(score_mlp_grad, 9), ENTRY(adamw_step, 11), ENTRY(select, 7),
     ENTRY(weighted_vote, 5), ENTRY(histogram, 3), ENTRY(calibrate, 3), ENTRY(prune_bernoulli, 4), ENTRY(grpo_advantage, 4),
-    ENTRY(grpo_objective, 10),
+    ENTRY(grpo_objective, 10), ENTRY(attention, 8), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
