@@ -13,7 +13,6 @@ namespace {
 using namespace attention;
 
 constexpr int kThreads = 256, kWaves = kThreads / ARROL_WAVE, kOwn = 32 * kWaves;   // 32 own rows a wavefront
-constexpr int64_t kRowBlocks = 1 << 20;
 
 struct Problem {
     const uint16_t *q, *k, *v;
@@ -177,41 +176,23 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
         lse_out[static_cast<int64_t>(head) * a.pq.T + w.row0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-// What the gradient needs of a row: -lse / scale, and behind all of those -D, D_i = <do_i, o_i>, in fp32.  They are what the products z and dp start from:
-// z / scale - lse / scale and dp - D come out of the matrix cores.  A row that sees nothing has lse = -inf, and is masked everywhere.
-// A group of 16 lanes takes a row of a head, 8 elements a lane.
-__global__ __launch_bounds__(256) void attention_row_kernel(const uint16_t* __restrict__ o, const uint16_t* __restrict__ go, const float* __restrict__ lse, int64_t rows,
-                                                            int64_t T, int heads, int hd, float scale, float* __restrict__ stats) {
-    const int e = (threadIdx.x & 15) * 8;
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * 16; base < rows; base += static_cast<int64_t>(gridDim.x) * 16) {
-        const int64_t row = base + (threadIdx.x >> 4);       // token * heads + head
-        float sum = 0.f;
-        if (row < rows && e < hd) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(o + row * hd + e), y = *reinterpret_cast<const u32x4*>(go + row * hd + e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += bf16_lo(x[i]) * bf16_lo(y[i]) + bf16_hi(x[i]) * bf16_hi(y[i]);
-        }
-        const auto add = [](float u, float w) { return u + w; };
-        sum = wave_step<1>(wave_step<2>(wave_step<4>(wave_step<8>(sum, add), add), add), add);
-        if (row < rows && (threadIdx.x & 15) == 0) {
-            const int64_t at = (row % heads) * T + row / heads;
-            stats[at] = -lse[at] / scale;
-            stats[rows + at] = -sum;
-        }
-    }
-}
-
-// dK and dV: a workgroup takes 128 keys of a kv head, a wavefront 32 of them (K and V as fragments in registers), and walks over the
-// queries of every head that reads them in tiles of 64: the sum over the shared heads is made in registers, in a fixed order.
-// S = Q K^T and dP = dO V^T have the own key as column; dV^T += dO^T P and dK^T += Q^T dS.
+// dK and dV: a workgroup takes 128 keys of a kv head and walks over the queries of every head that reads them in tiles of 64.  Two groups of four
+// wavefronts take every other tile (with its own part of the LDS each), a wavefront 32 of the keys (K and V as fragments in
+// registers); the sum over the shared heads is made in registers and the groups' sums are added at the end, all in a fixed order.  The longest walk - the
+// first keys of a long sequence, all heads - bounds the launch where there are few sequences: with one group 859 us on 4 survivors of up to 4,096 tokens,
+// 32 heads of 128 over 8.
+// S = Q K^T and dP = dO V^T have the own key as column and start from -lse / scale and -D of their rows, so that z / scale - lse / scale and
+// dp - D come out of the matrix cores (a row that sees nothing has lse = -inf, and is masked everywhere); dV^T += dO^T P, dK^T += Q^T dS.
+constexpr int kKvThreads = 2 * kThreads;
 template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
-                                                                        uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
+__global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
+                                                                          uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
     constexpr int BQ = 64;
     using T = Tile<HD>;
     constexpr int kTileBytes = BQ * T::kRowBytes, kSlot = 2 * kTileBytes + 2 * BQ * 4;
-    __shared__ __align__(1024) unsigned char lds[2][kSlot];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    extern __shared__ __align__(1024) unsigned char lds[];       // [group][slot][kSlot]
+    const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int wave = wave8 & (kWaves - 1), group = wave8 / kWaves;
     const int per = a.heads / a.kv_heads;
     int kvh;
     int64_t tile;
@@ -236,7 +217,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
     const int from = seen_from(j0 + (lane & 31)), from_least = seen_from(j0), from_most = seen_from(j0 + 31);
     const int t_first = seen_from(j0 - 32 * wave) / BQ;
     const int n_t = (nq + BQ - 1) / BQ > t_first ? (nq + BQ - 1) / BQ - t_first : 0;
-    const int total = n_t * per;
+    const int total = n_t * per;                      // tiles, head by head
 
     bf16x8 kf[HD / 16], vf[HD / 16];
     load_own<HD>(kf, a.k + row0 * a.k_stride + static_cast<int64_t>(kvh) * a.hd, a.k_stride, own_valid, a.hd, lane);
@@ -248,9 +229,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
 
     Stream<HD, BQ, kWaves> qs, gs;
-    const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
-    int h = 0, ti = 0, pointed = 0;                   // head and tile that are fetched next
+    const unsigned lds0 = lds_address(lds) + group * 2 * kSlot, row_at = T::row_base(lane), column_at = T::column_base(lane);
+    int h = 0, ti = group, pointed = 0;               // head and tile that are fetched next
+    const auto wrap = [&](int& tile_of, int* head_of) {
+        while (tile_of >= n_t) {
+            tile_of -= n_t;
+            if (head_of) ++*head_of;
+        }
+    };
     const auto fetch = [&](int slot) {
+        wrap(ti, &h);
         const int i0 = (t_first + ti) * BQ, valid = nq - i0 < BQ ? nq - i0 : BQ;
         if (valid != pointed) {
             qs.point(static_cast<unsigned>(a.q_stride) * 2, valid, a.hd, wave, lane);
@@ -265,7 +253,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
             const float* from_row = stats + (wave * a.heads + head) * a.pq.T + q_begin + i0 + (lane < valid ? lane : valid - 1);
             asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from_row), "s"(to + 2 * kTileBytes + wave * 256) : "memory");
         }
-        if (++ti == n_t) ti = 0, ++h;
+        ti += 2;
     };
     // 32 queries of a tile
     const auto step = [&](int slot_index, int b, int i0) {
@@ -308,31 +296,50 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_kv_kernel(Problem 
             }
         }
     };
-    if (total > 0) fetch(0);
+    const int mine = total > group ? (total - group + 1) / 2 : 0;      // this group's tiles: group, group + 2, ...
+    if (mine > 0) fetch(0);
     tiles_ready();
-    int at = 0;
-    for (int t = 0; t < total; ++t) {
-        if (t + 1 < total) fetch((t + 1) & 1);
-        const int i0 = (t_first + at) * BQ;
-        if (++at == n_t) at = 0;
+    int at = group;
+    for (int t = 0; t < (total + 1) / 2; ++t) {
+        if (t + 1 < mine) fetch((t + 1) & 1);
+        if (t < mine) {
+            wrap(at, nullptr);
+            const int i0 = (t_first + at) * BQ;
+            at += 2;
 #pragma unroll 1
-        for (int b = 0; b < 2; ++b) {
-            const int i = i0 + 32 * b;
-            if (own_valid == 0 || i >= nq || i + 31 < from_least) continue;
-            step(t & 1, b, i);
+            for (int b = 0; b < 2; ++b) {
+                const int i = i0 + 32 * b;
+                if (own_valid == 0 || i >= nq || i + 31 < from_least) continue;
+                step(t & 1, b, i);
+            }
         }
         tiles_ready();
     }
+    // group 1's sums by way of the LDS, a quarter of HD 128's at a time
+    f32x16* parts = reinterpret_cast<f32x16*>(lds);
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) {
+            f32x16& sum = which ? gv[d] : gk[d];
+            if (group == 1) parts[wave * 64 + lane] = sum;
+            __syncthreads();
+            if (group == 0) sum += parts[wave * 64 + lane];
+            __syncthreads();
+        }
+    if (group == 1) return;
     const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.hd, to = row0 * out_stride + static_cast<int64_t>(kvh) * a.hd;
     store_own<HD>(gk, a.scale, dk + to, out_stride, own_valid, a.hd, lane);
     store_own<HD>(gv, 1.f, dv + to, out_stride, own_valid, a.hd, lane);
 }
+template <int HD>
+constexpr int kKvLds = 4 * (2 * 64 * Tile<HD>::kRowBytes + 512);
 
 // dQ: a workgroup takes 128 queries of a head (Q and dO as fragments in registers) and walks over the keys in tiles of 64.
-// S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.
+// S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  It goes first, and leaves what the other kernel needs of a row: -lse / scale, and behind all
+// of those -D, D_i = <do_i, o_i>, in fp32.
 template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ go, const float* __restrict__ stats,
-                                                                       uint16_t* __restrict__ dq) {
+__global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ out, const uint16_t* __restrict__ go,
+                                                                       const float* __restrict__ lse, float* __restrict__ stats, uint16_t* __restrict__ dq) {
     constexpr int BK = 64;
     using T = Tile<HD>;
     constexpr int kTileBytes = BK * T::kRowBytes;
@@ -352,9 +359,20 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
     load_own<HD>(qf, a.q + w.row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, w.own_valid, a.hd, lane);
     load_own<HD>(gf, go + w.row0 * go_stride + static_cast<int64_t>(head) * a.hd, go_stride, w.own_valid, a.hd, lane);
     float mine[2] = {0.f, 0.f};
-    if ((lane & 31) < w.own_valid) {
-        const float* at = stats + static_cast<int64_t>(head) * a.pq.T + w.row0 + (lane & 31);
-        mine[0] = at[0], mine[1] = at[static_cast<int64_t>(a.heads) * a.pq.T];
+    {
+        bf16x8 of[HD / 16];
+        load_own<HD>(of, out + w.row0 * go_stride + static_cast<int64_t>(head) * a.hd, go_stride, w.own_valid, a.hd, lane);
+        float dot = 0.f;
+#pragma unroll
+        for (int s = 0; s < HD / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot = fmaf(static_cast<float>(of[s][e]), static_cast<float>(gf[s][e]), dot);
+        mine[1] = -half_sum(dot);
+        if ((lane & 31) < w.own_valid) {
+            const int64_t at = static_cast<int64_t>(head) * a.pq.T + w.row0 + (lane & 31);
+            mine[0] = -lse[at] / a.scale;
+            stats[half ? static_cast<int64_t>(a.heads) * a.pq.T + at : at] = mine[half];
+        }
     }
     const uint16_t* kp = uniform(a.k + w.k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
     const uint16_t* vp = uniform(a.v + w.k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
@@ -487,21 +505,24 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
     const auto *go = static_cast<const uint16_t*>(grad_out);
     auto* stats = static_cast<float*>(workspace);
     if (T_q > 0) {
-        const int64_t rows = T_q * n_heads, blocks = (rows + 15) / 16;
-        arrol_launch(attention_row_kernel, dim3(static_cast<unsigned>(blocks < kRowBlocks ? blocks : kRowBlocks)), dim3(256), 0, st, static_cast<const uint16_t*>(out), go,
-                     lse, rows, T_q, n_heads, head_dim, scale, stats);
+        const int64_t tiles = tile_bound(T_q, n_seq, kOwn);
+        const dim3 grid(static_cast<unsigned>(tiles * n_heads));
+        const auto* o = static_cast<const uint16_t*>(out);
+        auto* dq = static_cast<uint16_t*>(grad_q);
+        if (head_dim <= 64) arrol_launch(attention_grad_q_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, o, go, lse, stats, dq);
+        else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, o, go, lse, stats, dq);
     }
     if (T_k > 0) {
         const dim3 grid(static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads));
         auto *dk = static_cast<uint16_t*>(grad_k), *dv = static_cast<uint16_t*>(grad_v);
-        if (head_dim <= 64) arrol_launch(attention_grad_kv_kernel<64>, grid, dim3(kThreads), 0, st, a, go, stats, dk, dv);
-        else arrol_launch(attention_grad_kv_kernel<128>, grid, dim3(kThreads), 0, st, a, go, stats, dk, dv);
-    }
-    if (T_q > 0) {
-        const int64_t tiles = tile_bound(T_q, n_seq, kOwn);
-        const dim3 grid(static_cast<unsigned>(tiles * n_heads));
-        if (head_dim <= 64) arrol_launch(attention_grad_q_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, go, stats, static_cast<uint16_t*>(grad_q));
-        else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, go, stats, static_cast<uint16_t*>(grad_q));
+        static arrol_device_flags allowed[2];
+        if (head_dim <= 64) {
+            if (!arrol_allow_lds(attention_grad_kv_kernel<64>, kKvLds<64>, allowed[0])) return arrol_launch_status(), ARROL_EHIP;
+            arrol_launch(attention_grad_kv_kernel<64>, grid, dim3(kKvThreads), kKvLds<64>, st, a, go, stats, dk, dv);
+        } else {
+            if (!arrol_allow_lds(attention_grad_kv_kernel<128>, kKvLds<128>, allowed[1])) return arrol_launch_status(), ARROL_EHIP;
+            arrol_launch(attention_grad_kv_kernel<128>, grid, dim3(kKvThreads), kKvLds<128>, st, a, go, stats, dk, dv);
+        }
     }
     return arrol_launch_status();
 }
