@@ -464,18 +464,23 @@ int arrol_probe_mfma_rate(const void* a_bf16, int64_t n_a, const void* b_bf16, i
  * ascending; clamped into [0, T]).  With nq queries and nk keys in a sequence, query head h reads kv head h / (n_heads / n_kv_heads):
  *   z_ij = scale <q_i, k_j>,  j visible to i: all, or with causal != 0 those with j + nq <= i + nk (the ends aligned, so that the
  *   queries may be the last rows of a longer context);  lse_i = log sum_j exp z_ij,  o_i = sum_j exp(z_ij - lse_i) v_j.
- * A query that sees no key, and a row of no sequence, has o = 0 and lse = -inf.  Whatever lies in other sequences' rows (NaN, too) takes no part.
+ * A query that sees no key, and a row of no sequence, has o = 0 and lse = -inf.  Whatever lies in keys and values that a query does not see, and in other
+ * sequences' rows (NaN and infinities, too), takes no part.
  * q bf16, row t of head h at q + t*q_stride + h*head_dim (elements; k and v in the same way, n_kv_heads of them): slices of a
  *   fused projection need no copy.  Strides multiples of 8, at least heads*head_dim and at most 2^24, bases 16-byte aligned.
- * cu_seqlens_k NULL: the same as the queries'.   n_heads a multiple of n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0.
+ * cu_seqlens_k NULL: the same as the queries' (and T_k == T_q).   n_heads a multiple of n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0.
  * out bf16 [T_q, n_heads, head_dim];  lse_out NULL or fp32 [n_heads, T_q].
  * bf16 products, fp32 accumulation, maximum, sum and lse; the weights are rounded to bf16 for the product with v (2^-9 each).
  * T_q == 0 is a no-op.  (T / 128 + n_seq + 2) * n_heads has to stay below 2^24, else ARROL_EINVAL.
+ * workspace: optional.  Given the queried size (16-byte aligned; the query returns 0 where this does not apply) the keys of a sequence are cut into ranges
+ * where few queries read many keys, and the ranges joined in a fixed order by a second launch; without it one workgroup walks over all of them.
+ * The results differ by fp32 rounding of the joining only.
  */
+size_t arrol_attention_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t head_dim);
 int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                     const int64_t* cu_seqlens_q, const int64_t* cu_seqlens_k, int64_t T_q, int64_t T_k, int32_t n_seq,
                     int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale, void* out,
-                    float* lse_out, void* stream);
+                    float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The gradient of the above, given out, lse (arrol_attention's of the same inputs) and grad_out = dL/dout bf16 [T_q, n_heads, head_dim]:
@@ -483,6 +488,8 @@ int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_st
  *   dv_j = sum_i p_ij do_i,  dk_j = scale sum_i ds_ij q_i (sums over all query heads of the kv head),  dq_i = scale sum_j ds_ij k_j
  * grad_q bf16 [T_q, n_heads, head_dim], grad_k and grad_v bf16 [T_k, n_kv_heads, head_dim], each rounded once from fp32 sums (p and ds are
  * rounded to bf16 for their products).  No atomics: bit-reproducible run to run.  Rows of no sequence get zeros.
+ * Other sequences' rows take no part, whatever they hold; a NaN or infinity of a row, though, may reach the gradients of the 32 rows around it in
+ * its own sequence, whether or not they see it.
  * workspace: arrol_attention_grad_workspace_bytes(T_q, n_heads) bytes, 16-byte aligned.
  */
 size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int32_t n_heads);

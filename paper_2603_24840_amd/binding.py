@@ -93,7 +93,8 @@ _SIGNATURES = {
     "arrol_calibrate_search": (ctypes.c_int, [_vp, _vp, _i32, Policy, _vp, _vp]),
     "arrol_prune_bernoulli": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
     "arrol_attention": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _i32, _i32, _i32, _f32,
-                                       _vp, _vp, _vp]),
+                                       _vp, _vp, _vp, _sz, _vp]),
+    "arrol_attention_workspace_bytes": (_sz, [_i64, _i64, _i32, _i32, _i32]),
     "arrol_attention_grad_workspace_bytes": (_sz, [_i64, _i32]),
     "arrol_attention_grad": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32,
                                             _i32, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
@@ -758,27 +759,32 @@ def _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale):
     return (q.data_ptr(), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2]), ends
 
 
-def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, *, stream=None):
+def arrol_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, workspace="auto", *, stream=None):
     """Attention over packed sequences: q bf16 [T_q, n_heads, head_dim], k and v bf16 [T_k, n_kv_heads, head_dim] (rows may be strided),
     cu_seqlens int64 [n_seq+1] of the queries and, where they differ, cu_seqlens_k of the keys; scale None: head_dim ** -0.5.
+    workspace: "auto" allocates what the library asks for (keys in ranges where few queries read many), None passes none, or a uint8 tensor.
     -> (out bf16 [T_q, n_heads, head_dim], lse fp32 [n_heads, T_q])."""
     if stream is None:
-        result = (_marshal or _load_marshal()).attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out)
+        result = (_marshal or _load_marshal()).attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, workspace)
         if result is not None:
             return result
-        return _py_attention.__wrapped__(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out)
-    return _py_attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, stream=stream)
+        return _py_attention.__wrapped__(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, workspace)
+    return _py_attention(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, workspace, stream=stream)
 
 
 @_on_stream
-def _py_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, stream=None):
+def _py_attention(q, k, v, cu_seqlens, cu_seqlens_k=None, causal=True, scale=None, out=None, workspace="auto", stream=None):
     head, ends = _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale)
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     elif out.shape != q.shape:
         raise ValueError("out must have the shape of q")
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-    rc = lib().arrol_attention(*head, *ends, _ptr(out, torch.bfloat16, "out"), lse.data_ptr(), _stream(stream))
+    if isinstance(workspace, str):
+        need = lib().arrol_attention_workspace_bytes(q.shape[0], k.shape[0], cu_seqlens.numel() - 1, q.shape[1], q.shape[2])
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    rc = lib().arrol_attention(*head, *ends, _ptr(out, torch.bfloat16, "out"), lse.data_ptr(), _ptr(workspace, torch.uint8, "workspace"),
+                               workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("arrol_attention", rc)
     return out, lse
 

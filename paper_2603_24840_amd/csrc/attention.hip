@@ -40,14 +40,14 @@ struct QueryBlock {
     int reach;                      // most over the workgroup's rows
     __device__ __forceinline__ bool find(const Problem& a, int64_t tile, int wave, int lane) {
         int segment;
-        int64_t first, end;
-        if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, end)) return false;
-        const int64_t q_begin = a.pq.bound(segment);
+        int64_t first, q_begin, end;
+        if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, q_begin, end)) return false;
         const int nq = uniform(static_cast<int>(end - q_begin));
         k_begin = 0, nk = 0;
         if (segment >= 1 && segment <= a.pq.n) {       // rows of no sequence see no keys: zeros
-            k_begin = a.pk.bound(segment);
-            const int64_t n = a.pk.bound(segment + 1) - k_begin;
+            const bool same = a.pk.cu == a.pq.cu && a.pk.T == a.pq.T;
+            k_begin = same ? q_begin : a.pk.bound(segment);
+            const int64_t n = (same ? end : a.pk.bound(segment + 1)) - k_begin;
             nk = uniform(static_cast<int>(n < 0 ? 0 : n));
         }
         row0 = first + 32 * wave;
@@ -66,29 +66,80 @@ struct QueryBlock {
     }
 };
 
-// Forward pass: a workgroup takes 128 queries of a head, a wavefront 32 of them, and walks over the keys in tiles of 64.
-// S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.  While a tile is worked on the next one is on its way into the
-// other half of the LDS.
+// What a wavefront of the forward pass leaves: the output, or, where the keys of a sequence are cut into several ranges, its part of it.
+struct Output {
+    uint16_t* out;
+    float* lse;
+    int splits;                     // ranges of the keys
+    float *part_o, *part_ml;        // [split][row][head][hd], [split][row][head][2] where there are several
+};
+
+// O of a wavefront's rows over the keys [from, to), once more and by themselves: key by key, so that a key takes no part in a row that does not see it.  Where
+// all rows see all keys, or V is finite, the matrix instructions give the same; but the product of a hidden key's weight, 0, and an
+// infinity or NaN of its value is NaN.  Only rows that hold such values come here.
 template <int HD>
-__global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem a, int64_t tiles, uint16_t* __restrict__ out, float* __restrict__ lse_out) {
+__device__ __forceinline__ void repair_rows(const Problem& a, const QueryBlock& w, const bf16x8 (&qf)[HD / 16], int kvh, int from, int to, float base, int lane, f32x16 (&o)[HD / 32]) {
+    const int half = lane >> 5;
+    const float c = a.scale * kLog2e;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
+    for (int j = from; j < to; ++j) {
+        const uint16_t* k = a.k + (w.k_begin + j) * a.k_stride + static_cast<int64_t>(kvh) * a.hd;
+        const uint16_t* v = a.v + (w.k_begin + j) * a.v_stride + static_cast<int64_t>(kvh) * a.hd;
+        float z = 0.f;
+#pragma unroll
+        for (int s = 0; s < HD / 16; ++s) {
+            const int e = 16 * s + 8 * half;
+            if (e >= a.hd) continue;
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(k + e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z = fmaf(static_cast<float>(x[i]), static_cast<float>(qf[s][i]), z);
+        }
+        z = half_sum(z);
+        const bool seen = j < w.sees;
+        const float p = __builtin_amdgcn_exp2f(fmaf(z, c, -base));
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int e = 32 * d + 8 * (r >> 2) + 4 * half + (r & 3);
+                if (e >= a.hd) continue;
+                const float x = bf16_lo(v[e]);
+                o[d][r] = seen ? fmaf(p, x, o[d][r]) : o[d][r];
+            }
+    }
+}
+
+// Forward pass: a workgroup takes 128 queries of a head, a wavefront 32 of them, and walks over the keys in tiles of 64.
+// S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.  The tiles that come next are on their way into the other halves of the
+// LDS.  With heads of 128, whose registers leave two wavefronts to a SIMD, the scores of the next tile are formed while the exponentials of this one
+// are (K runs a tile ahead of V): 4 survivors of up to 4,096 tokens, 32 heads over 8, 298 us against 355.  With heads of 64 four fit, which
+// do that for each other: 64 prompts of up to 512 tokens 83 us, and 108 the other way.
+template <int HD>
+__global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem a, int64_t tiles, Output to) {
     constexpr int BK = 64;
+    constexpr bool kAhead = HD == 128;
     using T = Tile<HD>;
     constexpr int kTileBytes = BK * T::kRowBytes;
-    __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];
+    __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];      // [slot][K, V]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads;
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
     const int head = kvh * per + static_cast<int>(rest % per);
+    rest /= per;
+    const int split = static_cast<int>(rest % to.splits);
     QueryBlock w;
-    if (!w.find(a, tiles - 1 - rest / per, wave, lane)) return;
-    const int n_tiles = (w.reach + BK - 1) / BK;
+    if (!w.find(a, tiles - 1 - rest / to.splits, wave, lane)) return;
+    // this workgroup's tiles of 64 keys: those that some of its rows see, or a range of them
+    const int all = (w.reach + BK - 1) / BK, t_lo = static_cast<int>(static_cast<int64_t>(all) * split / to.splits),
+              n_tiles = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / to.splits) - t_lo;
 
     bf16x8 qf[HD / 16];
     load_own<HD>(qf, a.q + w.row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, w.own_valid, a.hd, lane);
-    const uint16_t* kp = uniform(a.k + w.k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
-    const uint16_t* vp = uniform(a.v + w.k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* kp = uniform(a.k + (w.k_begin + static_cast<int64_t>(t_lo) * BK) * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* vp = uniform(a.v + (w.k_begin + static_cast<int64_t>(t_lo) * BK) * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
     f32x16 o[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) o[d] = 0.f;
@@ -96,38 +147,42 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
     const float c = a.scale * kLog2e;
 
     Stream<HD, BK, kWaves> ks, vs;
-    const int whole = w.nk / BK;      // tiles of 64 keys that exist
-    const auto point = [&](int valid) {
-        ks.point(static_cast<unsigned>(a.k_stride) * 2, valid, a.hd, wave, lane);
-        vs.point(static_cast<unsigned>(a.v_stride) * 2, valid, a.hd, wave, lane);
-    };
+    const int keys = w.nk - t_lo * BK, whole = keys / BK;      // from the first tile on; tiles of 64 keys that exist
     const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
-    const auto fetch = [&](int t) {
-        if (t == whole) point(w.nk - t * BK);
-        const unsigned to = lds0 + (t & 1) * 2 * kTileBytes;
-        ks.issue(kp, to, wave);
-        vs.issue(vp, to + kTileBytes, wave);
+    const auto fetch_k = [&](int t) {
+        if (t == whole) ks.point(static_cast<unsigned>(a.k_stride) * 2, keys - t * BK, a.hd, wave, lane);
+        ks.issue(kp, lds0 + (t & 1) * 2 * kTileBytes, wave);
         kp += BK * a.k_stride;
+    };
+    const auto fetch_v = [&](int t) {
+        if (t == whole) vs.point(static_cast<unsigned>(a.v_stride) * 2, keys - t * BK, a.hd, wave, lane);
+        vs.issue(vp, lds0 + ((t & 1) * 2 + 1) * kTileBytes, wave);
         vp += BK * a.v_stride;
     };
-    const int clear = w.sees_least / BK, needed = (w.sees_most + BK - 1) / BK;
-    const auto step = [&](int t) {
-        const unsigned slot = lds0 + (t & 1) * 2 * kTileBytes, rows = fresh(slot + row_at), columns = fresh(slot + column_at);
-        f32x16 s[BK / 32];
+    const auto fetch_for = [&](int t) {           // what iteration t + 1 needs
+        if (t + 2 < n_tiles) fetch_k(t + 2);
+        if (t + 1 < n_tiles) fetch_v(t + 1);
+    };
+    const int clear = w.sees_least / BK - t_lo, most = (w.sees_most + BK - 1) / BK - t_lo, needed = most < 0 ? 0 : most < n_tiles ? most : n_tiles;
+    const auto scores = [&](int t, int b, f32x16 (&s)[BK / 32]) {
+        const unsigned rows = fresh(lds0 + (t & 1) * 2 * kTileBytes + row_at);
+        s[b] = 0.f;
 #pragma unroll
-        for (int b = 0; b < BK / 32; ++b) {
-            s[b] = 0.f;
-#pragma unroll
-            for (int e = 0; e < HD / 16; ++e) s[b] = mfma32(T::by_row(rows, e, 32 * b * T::kRowBytes), qf[e], s[b]);
-        }
+        for (int e = 0; e < HD / 16; ++e) s[b] = mfma32(T::by_row(rows, e, 32 * b * T::kRowBytes), qf[e], s[b]);
+    };
+    // weights and output of tile t from its scores s; NEXT: and the scores of the next one
+    const auto step = [&](auto more, int t, f32x16 (&s)[BK / 32], f32x16 (&next)[BK / 32]) {
+        constexpr bool NEXT = decltype(more)::value;
+        const unsigned columns = fresh(lds0 + (t & 1) * 2 * kTileBytes + column_at);
         if (t >= clear) {       // some row of the wavefront does not see all of the tile
             stay_branch();
-            const int limit = w.sees - t * BK - 4 * half;
+            const int limit = w.sees - (t_lo + t) * BK - 4 * half;
 #pragma unroll
             for (int b = 0; b < BK / 32; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r >> 2) + (r & 3) < limit ? s[b][r] : -INFINITY;
         }
+        if constexpr (NEXT) scores(t + 1, 0, next);
         float top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < BK / 32; ++b)
@@ -136,14 +191,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
         top = half_max(top) * c;
         // the sums are moved to a new maximum only where it has grown by 2^8: exp2 then stays below 256 and nothing is lost
         if (__any(top > m + 8.f)) {
-            const float to = fmaxf(m, top);
-            const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            m = to;
+            const float up = fmaxf(m, top);
+            const float f = up == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - up);
+            m = up;
             l *= f;
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d) o[d] *= f;
         }
         const float base = m == -INFINITY ? 0.f : m;
+        if constexpr (NEXT) scores(t + 1, 1, next);
 #pragma unroll
         for (int b = 0; b < BK / 32; ++b)
 #pragma unroll
@@ -161,31 +217,138 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
             }
     };
     if (n_tiles > 0) {
-        point(BK);
-        fetch(0);
+        ks.point(static_cast<unsigned>(a.k_stride) * 2, BK, a.hd, wave, lane);
+        vs.point(static_cast<unsigned>(a.v_stride) * 2, BK, a.hd, wave, lane);
+        fetch_k(0);
+        fetch_v(0);
+        if (kAhead && n_tiles > 1) fetch_k(1);
     }
     tiles_ready();
-    for (int t = 0; t < n_tiles; ++t) {
-        if (t + 1 < n_tiles) fetch(t + 1);
-        if (t < needed) step(t);
+    int t = 0;
+    f32x16 x[BK / 32];
+    if constexpr (!kAhead) {
+        for (; t < n_tiles; ++t) {
+            if (t + 1 < n_tiles) {
+                fetch_k(t + 1);
+                fetch_v(t + 1);
+            }
+            if (t < needed) {
+#pragma unroll
+                for (int b = 0; b < BK / 32; ++b) scores(t, b, x);
+                step(std::false_type{}, t, x, x);
+            }
+            tiles_ready();
+        }
+    } else if (needed > 0) {
+        f32x16 y[BK / 32];
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b) scores(0, b, x);
+        if (n_tiles > 2) tiles_ready();           // every wavefront has read K's first tile, whose place the third one takes
+        for (; t + 2 < needed; t += 2) {
+            fetch_for(t);
+            step(std::true_type{}, t, x, y);
+            tiles_ready();
+            fetch_for(t + 1);
+            step(std::true_type{}, t + 1, y, x);
+            tiles_ready();
+        }
+        if (t + 1 < needed) {
+            fetch_for(t);
+            step(std::true_type{}, t, x, y);
+            tiles_ready();
+            ++t;
+#pragma unroll
+            for (int b = 0; b < BK / 32; ++b) x[b] = y[b];
+        }
+        fetch_for(t);
+        step(std::false_type{}, t, x, y);
+        tiles_ready();
+        ++t;
+    } else if (n_tiles > 2) {
+        tiles_ready();
+    }
+    for (; t < n_tiles; ++t) {                    // tiles of the other wavefronts
+        fetch_for(t);
         tiles_ready();
     }
     l = half_sum(l);
-    store_own<HD>(o, l == 0.f ? 0.f : 1.f / l, out + (w.row0 * a.heads + head) * a.hd, static_cast<int64_t>(a.heads) * a.hd, w.own_valid, a.hd, lane);
-    if (lse_out && lane < w.own_valid && lane < 32)
-        lse_out[static_cast<int64_t>(head) * a.pq.T + w.row0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    // An output that is no number: is it from a value that some of the rows do not see?
+    const int hidden = w.sees_least > t_lo * BK ? w.sees_least : t_lo * BK, end = (t_lo + needed) * BK < w.nk ? (t_lo + needed) * BK : w.nk;
+    if (hidden < end) {
+        float odd = 0.f;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) odd = fmaf(o[d][r], 0.f, odd);        // NaN if any is NaN or infinite
+        if (__any(odd != 0.f)) {
+            bool found = false;
+            for (int j = hidden + lane; j < end; j += 64) {
+                const uint16_t* v = a.v + (w.k_begin + j) * a.v_stride + static_cast<int64_t>(kvh) * a.hd;
+                for (int e = 0; e < a.hd; ++e) found |= (v[e] & 0x7f80) == 0x7f80;
+            }
+            if (__any(found)) {
+                const int last = w.sees_most < end ? w.sees_most : end;
+                repair_rows<HD>(a, w, qf, kvh, t_lo * BK, last, m == -INFINITY ? 0.f : m, lane, o);
+            }
+        }
+    }
+    const int64_t row_heads = static_cast<int64_t>(a.heads) * a.hd;
+    if (to.splits == 1) {
+        store_own<HD>(o, l == 0.f ? 0.f : 1.f / l, &lds[0][0][0] + wave * 32 * T::kRowBytes, to.out + (w.row0 * a.heads + head) * a.hd, row_heads, w.own_valid, a.hd, lane);
+        if (to.lse && lane < w.own_valid) to.lse[static_cast<int64_t>(head) * a.pq.T + w.row0 + lane] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+        return;
+    }
+    const int64_t at = (split * a.pq.T + w.row0 + (lane & 31)) * a.heads + head;
+    if ((lane & 31) >= w.own_valid) return;
+    if (half == 0) *reinterpret_cast<f32x2*>(to.part_ml + 2 * at) = f32x2{m, l};
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int e = 32 * d + 8 * b + 4 * half;
+            if (e < a.hd) *reinterpret_cast<f32x4*>(to.part_o + at * a.hd + e) = f32x4{o[d][4 * b], o[d][4 * b + 1], o[d][4 * b + 2], o[d][4 * b + 3]};
+        }
 }
 
-// dK and dV: a workgroup takes 128 keys of a kv head and walks over the queries of every head that reads them in tiles of 64.  Two groups of four
-// wavefronts take every other tile (with its own part of the LDS each), a wavefront 32 of the keys (K and V as fragments in
-// registers); the sum over the shared heads is made in registers and the groups' sums are added at the end, all in a fixed order.  The longest walk - the
-// first keys of a long sequence, all heads - bounds the launch where there are few sequences: with one group 859 us on 4 survivors of up to 4,096 tokens,
-// 32 heads of 128 over 8.
+// Joins the ranges: 16 lanes a row of a head, 8 head elements each.
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(Output to, int64_t T, int heads, int hd) {
+    const int64_t rows = T * heads, at = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / 16;
+    const int e = (threadIdx.x & 15) * 8;
+    if (at >= rows) return;
+    float top = -INFINITY;
+    for (int s = 0; s < to.splits; ++s) top = fmaxf(top, to.part_ml[2 * (s * rows + at)]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    for (int s = 0; s < to.splits; ++s) {
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(to.part_ml + 2 * (s * rows + at));
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        if (f == 0.f) continue;
+        sum += f * ml.y;
+        if (e < hd) {
+            const f32x4* p = reinterpret_cast<const f32x4*>(to.part_o + (s * rows + at) * hd + e);
+            x += p[0] * f, y += p[1] * f;
+        }
+    }
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+    if (e < hd) {
+        typedef float f32x8 __attribute__((ext_vector_type(8)));
+        const f32x8 z = {x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse, y[0] * inverse, y[1] * inverse, y[2] * inverse, y[3] * inverse};
+        *reinterpret_cast<bf16x8*>(to.out + at * hd + e) = __builtin_convertvector(z, bf16x8);
+    }
+    if (to.lse && e == 0) to.lse[at % heads * T + at / heads] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+}
+
+// dK and dV: a workgroup takes 128 keys of a kv head and walks over the queries of every head that reads them in tiles of 64, a wavefront with 32
+// of the keys (K and V as fragments in registers); the sum over the shared heads is made in registers, in a fixed order.
+// With heads of 128, whose registers leave two wavefronts to a SIMD, these are two groups of four of one workgroup: each takes every other tile (with its own
+// part of the LDS), and their sums are added at the end.  That halves the longest walk - the first keys of a long sequence, all heads - which
+// bounds the launch where there are few sequences: 4 survivors of up to 4,096 tokens, 32 heads over 8, 1,268 us for the whole gradient with one group and
+// 1,069 with two.  With heads of 64 three workgroups of one group fit: 16 survivors of up to 1,000 tokens 206 us, and 218 with two groups.
 // S = Q K^T and dP = dO V^T have the own key as column and start from -lse / scale and -D of their rows, so that z / scale - lse / scale and
 // dp - D come out of the matrix cores (a row that sees nothing has lse = -inf, and is masked everywhere); dV^T += dO^T P, dK^T += Q^T dS.
-constexpr int kKvThreads = 2 * kThreads;
-template <int HD>
-__global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
+template <int HD, int GROUPS>
+__global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
                                                                           uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
     constexpr int BQ = 64;
     using T = Tile<HD>;
@@ -198,15 +361,16 @@ __global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Proble
     int64_t tile;
     split_block(blockIdx.x, a.kv_heads, kvh, tile);
     int segment;
-    int64_t first, end;
-    if (!find_tile<kOwn>(a.pk, tile, lane, segment, first, end)) return;
-    const int64_t k_begin = a.pk.bound(segment), row0 = first + 32 * wave;
+    int64_t first, k_begin, end;
+    if (!find_tile<kOwn>(a.pk, tile, lane, segment, first, k_begin, end)) return;
+    const int64_t row0 = first + 32 * wave;
     const int nk = uniform(static_cast<int>(end - k_begin)), own_valid = clamp32(end - row0), j0 = uniform(static_cast<int>(row0 - k_begin));
     int64_t q_begin = 0;
     int nq = 0;
     if (segment >= 1 && segment <= a.pk.n) {
-        q_begin = a.pq.bound(segment);
-        const int64_t n = a.pq.bound(segment + 1) - q_begin;
+        const bool same = a.pk.cu == a.pq.cu && a.pk.T == a.pq.T;
+        q_begin = same ? k_begin : a.pq.bound(segment);
+        const int64_t n = (same ? end : a.pq.bound(segment + 1)) - q_begin;
         nq = uniform(static_cast<int>(n < 0 ? 0 : n));
     }
     // key j is seen by queries i >= j + nq - nk (causal)
@@ -253,7 +417,7 @@ __global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Proble
             const float* from_row = stats + (wave * a.heads + head) * a.pq.T + q_begin + i0 + (lane < valid ? lane : valid - 1);
             asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from_row), "s"(to + 2 * kTileBytes + wave * 256) : "memory");
         }
-        ti += 2;
+        ti += GROUPS;
     };
     // 32 queries of a tile
     const auto step = [&](int slot_index, int b, int i0) {
@@ -296,16 +460,16 @@ __global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Proble
             }
         }
     };
-    const int mine = total > group ? (total - group + 1) / 2 : 0;      // this group's tiles: group, group + 2, ...
+    const int mine = (total - group + GROUPS - 1) / GROUPS;      // this group's tiles: group, group + GROUPS, ...
     if (mine > 0) fetch(0);
     tiles_ready();
     int at = group;
-    for (int t = 0; t < (total + 1) / 2; ++t) {
+    for (int t = 0; t < (total + GROUPS - 1) / GROUPS; ++t) {
         if (t + 1 < mine) fetch((t + 1) & 1);
         if (t < mine) {
             wrap(at, nullptr);
             const int i0 = (t_first + at) * BQ;
-            at += 2;
+            at += GROUPS;
 #pragma unroll 1
             for (int b = 0; b < 2; ++b) {
                 const int i = i0 + 32 * b;
@@ -316,23 +480,32 @@ __global__ __launch_bounds__(kKvThreads, 1) void attention_grad_kv_kernel(Proble
         tiles_ready();
     }
     // group 1's sums by way of the LDS, a quarter of HD 128's at a time
-    f32x16* parts = reinterpret_cast<f32x16*>(lds);
-    for (int which = 0; which < 2; ++which)
+    if constexpr (GROUPS == 2) {
+        f32x16* parts = reinterpret_cast<f32x16*>(lds);
+        for (int which = 0; which < 2; ++which)
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-            f32x16& sum = which ? gv[d] : gk[d];
-            if (group == 1) parts[wave * 64 + lane] = sum;
-            __syncthreads();
-            if (group == 0) sum += parts[wave * 64 + lane];
-            __syncthreads();
-        }
-    if (group == 1) return;
+            for (int d = 0; d < HD / 32; ++d) {
+                f32x16& sum = which ? gv[d] : gk[d];
+                if (group == 1) parts[wave * 64 + lane] = sum;
+                __syncthreads();
+                if (group == 0) sum += parts[wave * 64 + lane];
+                __syncthreads();
+            }
+        if (group == 1) return;
+    }
     const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.hd, to = row0 * out_stride + static_cast<int64_t>(kvh) * a.hd;
-    store_own<HD>(gk, a.scale, dk + to, out_stride, own_valid, a.hd, lane);
-    store_own<HD>(gv, 1.f, dv + to, out_stride, own_valid, a.hd, lane);
+    unsigned char* own = lds + wave * 32 * T::kRowBytes;
+    store_own<HD>(gk, a.scale, own, dk + to, out_stride, own_valid, a.hd, lane);
+    store_own<HD>(gv, 1.f, own, dv + to, out_stride, own_valid, a.hd, lane);
 }
-template <int HD>
-constexpr int kKvLds = 4 * (2 * 64 * Tile<HD>::kRowBytes + 512);
+template <int HD, int GROUPS>
+bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const float* stats, void* dk, void* dv, hipStream_t st) {
+    constexpr int kLds = GROUPS * 2 * (2 * 64 * Tile<HD>::kRowBytes + 512);
+    static arrol_device_flags allowed;
+    if (!arrol_allow_lds(attention_grad_kv_kernel<HD, GROUPS>, kLds, allowed)) return false;
+    arrol_launch(attention_grad_kv_kernel<HD, GROUPS>, dim3(blocks), dim3(GROUPS * kThreads), kLds, st, a, go, stats, static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv));
+    return true;
+}
 
 // dQ: a workgroup takes 128 queries of a head (Q and dO as fragments in registers) and walks over the keys in tiles of 64.
 // S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  It goes first, and leaves what the other kernel needs of a row: -lse / scale, and behind all
@@ -438,7 +611,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
         }
         tiles_ready();
     }
-    store_own<HD>(gq, a.scale, dq + (w.row0 * a.heads + head) * a.hd, go_stride, w.own_valid, a.hd, lane);
+    store_own<HD>(gq, a.scale, &lds[0][0][0] + wave * 32 * T::kRowBytes, dq + (w.row0 * a.heads + head) * a.hd, go_stride, w.own_valid, a.hd, lane);
 }
 
 bool row_stride_ok(int64_t stride, int64_t rows, int heads, int hd) {
@@ -449,6 +622,7 @@ bool row_stride_ok(int64_t stride, int64_t rows, int heads, int hd) {
 int check(const Problem& a, int64_t T_q, int64_t T_k) {
     if (T_q < 0 || T_k < 0 || a.pq.n < 0 || a.heads < 1 || a.kv_heads < 1 || a.heads % a.kv_heads || a.heads > 65536 || a.hd < 8 || a.hd > 128 || a.hd % 8) return ARROL_EINVAL;
     if (!(a.scale > 0.f) || a.scale > 3e38f) return ARROL_EINVAL;
+    if (a.pk.cu == a.pq.cu && T_q != T_k) return ARROL_EINVAL;      // the keys' offsets are the queries'
     if (!row_stride_ok(a.q_stride, T_q, a.heads, a.hd) || !row_stride_ok(a.k_stride, T_k, a.kv_heads, a.hd) || !row_stride_ok(a.v_stride, T_k, a.kv_heads, a.hd)) return ARROL_EINVAL;
     if (T_q > 0 && (!a.q || !arrol_aligned16(a.q) || !a.pq.cu || !a.pk.cu)) return ARROL_EINVAL;
     if (T_k > 0 && (!a.k || !a.v || !arrol_aligned16(a.k) || !arrol_aligned16(a.v) || !a.pq.cu || !a.pk.cu)) return ARROL_EINVAL;
@@ -471,19 +645,39 @@ size_t stat_bytes(int64_t T, int heads) { return static_cast<size_t>(T) * heads 
 
 }  // namespace
 
+namespace {
+// Ranges that the keys of a sequence are cut into: enough for 1,024 workgroups, as long as a range keeps 256 keys of an average sequence.
+int key_splits(int64_t T_q, int64_t T_k, int n_seq, int heads) {
+    const int64_t blocks = (T_q / kOwn + n_seq) * heads, by_work = (1024 + blocks - 1) / (blocks > 0 ? blocks : 1), by_keys = n_seq > 0 ? T_k / n_seq / 256 : 1;
+    const int64_t s = by_work < by_keys ? by_work : by_keys;
+    return static_cast<int>(s < 1 ? 1 : s < 16 ? s : 16);
+}
+size_t part_bytes(int64_t T, int heads, int hd, int splits) { return splits == 1 ? 0 : static_cast<size_t>(splits) * T * heads * (hd + 2) * sizeof(float); }
+}  // namespace
+
+extern "C" size_t arrol_attention_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t head_dim) {
+    if (T_q <= 0 || T_k < 0 || n_seq < 0 || n_heads < 1 || head_dim < 8 || head_dim > 128) return 0;
+    return part_bytes(T_q, n_heads, head_dim, key_splits(T_q, T_k, n_seq, n_heads));
+}
+
 extern "C" int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const int64_t* cu_seqlens_q, const int64_t* cu_seqlens_k, int64_t T_q, int64_t T_k, int32_t n_seq,
                                int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t causal, float scale, void* out,
-                               float* lse_out, void* stream) {
+                               float* lse_out, void* workspace, size_t workspace_bytes, void* stream) {
     const Problem a = problem(q, q_stride, k, k_stride, v, v_stride, cu_seqlens_q, cu_seqlens_k, T_q, T_k, n_seq, n_heads, n_kv_heads, head_dim, causal, scale);
     if (const int rc = check(a, T_q, T_k)) return rc;
     if (T_q == 0) return ARROL_OK;
-    if (!out || !arrol_aligned16(out)) return ARROL_EINVAL;
-    const int64_t tiles = tile_bound(T_q, n_seq, kOwn);
-    const dim3 grid(static_cast<unsigned>(tiles * n_heads));
+    if (!out || !arrol_aligned16(out) || (workspace && !arrol_aligned16(workspace))) return ARROL_EINVAL;
+    const int64_t tiles = tile_bound(T_q, n_seq, kOwn), rows = T_q * n_heads;
+    int splits = key_splits(T_q, T_k, n_seq, n_heads);
+    if (!workspace || workspace_bytes < part_bytes(T_q, n_heads, head_dim, splits)) splits = 1;
+    auto* ws = static_cast<float*>(workspace);
+    const Output to = {static_cast<uint16_t*>(out), lse_out, splits, ws, splits > 1 ? ws + static_cast<size_t>(splits) * rows * head_dim : nullptr};
+    const dim3 grid(static_cast<unsigned>(tiles * n_heads * splits));
     const auto st = static_cast<hipStream_t>(stream);
-    if (head_dim <= 64) arrol_launch(attention_forward_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, static_cast<uint16_t*>(out), lse_out);
-    else arrol_launch(attention_forward_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, static_cast<uint16_t*>(out), lse_out);
+    if (head_dim <= 64) arrol_launch(attention_forward_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, to);
+    else arrol_launch(attention_forward_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, to);
+    if (splits > 1) arrol_launch(attention_join_kernel, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(kThreads), 0, st, to, T_q, n_heads, head_dim);
     return arrol_launch_status();
 }
 
@@ -513,15 +707,11 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
         else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, o, go, lse, stats, dq);
     }
     if (T_k > 0) {
-        const dim3 grid(static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads));
-        auto *dk = static_cast<uint16_t*>(grad_k), *dv = static_cast<uint16_t*>(grad_v);
-        static arrol_device_flags allowed[2];
-        if (head_dim <= 64) {
-            if (!arrol_allow_lds(attention_grad_kv_kernel<64>, kKvLds<64>, allowed[0])) return arrol_launch_status(), ARROL_EHIP;
-            arrol_launch(attention_grad_kv_kernel<64>, grid, dim3(kKvThreads), kKvLds<64>, st, a, go, stats, dk, dv);
-        } else {
-            if (!arrol_allow_lds(attention_grad_kv_kernel<128>, kKvLds<128>, allowed[1])) return arrol_launch_status(), ARROL_EHIP;
-            arrol_launch(attention_grad_kv_kernel<128>, grid, dim3(kKvThreads), kKvLds<128>, st, a, go, stats, dk, dv);
+        const auto blocks = static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads);
+        const bool ok = head_dim > 64 ? launch_grad_kv<128, 2>(a, blocks, go, stats, grad_k, grad_v, st) : launch_grad_kv<64, 1>(a, blocks, go, stats, grad_k, grad_v, st);
+        if (!ok) {
+            arrol_launch_status();
+            return ARROL_EHIP;
         }
     }
     return arrol_launch_status();

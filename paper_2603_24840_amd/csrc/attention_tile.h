@@ -124,22 +124,30 @@ __device__ __forceinline__ void load_own(bf16x8 (&f)[HD / 16], const uint16_t* b
     }
 }
 
-// Own rows' results: lane l has elements 32 d + 8 b + 4 (l / 32) + r of row l % 32.
+// Own rows' results: lane l has elements 32 d + 8 b + 4 (l / 32) + r of row l % 32.  They go through `tile`, 32 rows of the LDS that are the
+// wavefront's own by now, so that a store instruction writes whole rows: 8 bytes a lane, 32 rows apart, straight from the registers took 14 of 84 us on 64
+// prompts of up to 512 tokens.
 template <int HD>
-__device__ __forceinline__ void store_own(const f32x16 (&acc)[HD / 32], float factor, uint16_t* base, int64_t stride, int valid, int hd, int lane) {
-    const int row = lane & 31;
-    if (row >= valid) return;
+__device__ __forceinline__ void store_own(const f32x16 (&acc)[HD / 32], float factor, unsigned char* tile, uint16_t* base, int64_t stride, int valid, int hd, int lane) {
+    using T = Tile<HD>;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const int mine = lane & 31;
+    wave_lds_exchange();
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int e = 32 * d + 8 * b + 4 * (lane >> 5);
-            if (e < hd) {
-                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                const f32x4 v = {acc[d][4 * b] * factor, acc[d][4 * b + 1] * factor, acc[d][4 * b + 2] * factor, acc[d][4 * b + 3] * factor};
-                *reinterpret_cast<bf16x4*>(base + row * stride + e) = __builtin_convertvector(v, bf16x4);
-            }
+            const f32x4 v = {acc[d][4 * b] * factor, acc[d][4 * b + 1] * factor, acc[d][4 * b + 2] * factor, acc[d][4 * b + 3] * factor};
+            *reinterpret_cast<bf16x4*>(tile + mine * T::kRowBytes + (((4 * d + b) ^ T::swizzle(mine)) << 4) + (lane >> 5) * 8) = __builtin_convertvector(v, bf16x4);
         }
+    wave_lds_exchange();
+    const int c = lane % T::kChunks;
+#pragma unroll
+    for (int i = 0; i < T::kChunks / 2; ++i) {
+        const int row = i * (64 / T::kChunks) + lane / T::kChunks;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(tile + row * T::kRowBytes + ((c ^ T::swizzle(row)) << 4));
+        if (row < valid && c * 8 < hd) *reinterpret_cast<u32x4*>(base + row * stride + c * 8) = x;
+    }
 }
 
 // 16 rows' worth of a 32 x 32 result (registers 8 s .. 8 s + 7) as the B fragment of K16 step s.
@@ -174,32 +182,41 @@ struct Packed {
     }
 };
 
-// Tiles of `rows` rows, none across two segments: segment s has the tiles from bound(s) / rows + s on, which leaves it at least as
-// many as it needs whatever the lengths, and at most one spare.  So the grid is T / rows + n + 2 without a look at the offsets, and a workgroup finds
-// its segment by a search that 64 lanes do together (two rounds for 4,096 sequences).  Offsets out of order give empty or misplaced tiles, all
-// within [0, T).
+// Tiles of ROWS rows, none across two segments: segment s has the tiles from bound(s) / ROWS + s on, which leaves it at least as
+// many as it needs whatever the lengths, and at most one spare.  So the grid is T / ROWS + n + 2 without a look at the offsets, and a workgroup finds
+// its segment by a search that 64 lanes do together, two offsets each: one round for up to 126 sequences, two for 8,000, and the segment's own bounds
+// come out of the last one (a chain of four loads, one for each question, was 2 us of a short workgroup's 8).  Offsets out of order give empty
+// or misplaced tiles, all within [0, T).
+__device__ __forceinline__ int64_t lane_value(int64_t lo64, int64_t hi64, int index) {      // of 128 values, two a lane
+    const int64_t low = wave_bcast(lo64, index & 63), high = wave_bcast(hi64, index & 63);
+    return index < 64 ? low : high;
+}
 template <unsigned ROWS, class Bound>
-__device__ __forceinline__ bool find_tile(const Bound& bound, int segments, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
-    const auto start_of = [&](int s) { return static_cast<int64_t>(static_cast<uint64_t>(bound(s)) / ROWS) + s; };
+__device__ __forceinline__ bool find_tile(const Bound& bound, int segments, int64_t tile, int lane, int& segment, int64_t& first, int64_t& begin, int64_t& end) {
+    const auto start_of = [&](int64_t b, int s) { return static_cast<int64_t>(static_cast<uint64_t>(b) / ROWS) + s; };
     int lo = 0, count = segments;
-    while (count > 1) {
-        const int step = (count + 63) >> 6, at = lane * step;
-        const bool before = at < count && start_of(lo + at) <= tile;
-        const uint64_t votes = __ballot(before);
-        const int k = votes == ~0ull ? 63 : __builtin_ctzll(~votes) - 1;
-        const int skip = (k < 0 ? 0 : k) * step;
-        lo += skip;
-        count = count - skip < step ? count - skip : step;
+    for (;;) {
+        const int step = (count + 127) >> 7, at0 = lane * step, at1 = (lane + 64) * step;
+        const int64_t b0 = bound(lo + at0), b1 = bound(lo + at1);
+        const uint64_t v0 = __ballot(at0 < count && start_of(b0, lo + at0) <= tile), v1 = __ballot(at1 < count && start_of(b1, lo + at1) <= tile);
+        int k = v0 != ~0ull ? __builtin_ctzll(~v0) - 1 : v1 != ~0ull ? 63 + __builtin_ctzll(~v1) : 127;
+        k = uniform(k < 0 ? 0 : k);
+        if (step == 1) {
+            segment = lo + k;
+            begin = lane_value(b0, b1, k);
+            end = k < 127 ? lane_value(b0, b1, k + 1) : bound(segment + 1);
+            break;
+        }
+        lo += k * step;
+        count = count - k * step < step ? count - k * step : step;
     }
-    segment = __builtin_amdgcn_readfirstlane(lo);
-    const int64_t start = start_of(segment);
-    end = bound(segment + 1);
-    first = bound(segment) + (tile - start) * ROWS;
+    const int64_t start = start_of(begin, segment);
+    first = begin + (tile - start) * ROWS;
     return tile >= start && first < end;
 }
 template <unsigned ROWS>
-__device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lane, int& segment, int64_t& first, int64_t& end) {
-    return find_tile<ROWS>([&](int s) { return p.bound(s); }, p.n + 2, tile, lane, segment, first, end);
+__device__ __forceinline__ bool find_tile(const Packed& p, int64_t tile, int lane, int& segment, int64_t& first, int64_t& begin, int64_t& end) {
+    return find_tile<ROWS>([&](int s) { return p.bound(s); }, p.n + 2, tile, lane, segment, first, begin, end);
 }
 __host__ __device__ inline int64_t tile_bound(int64_t T, int n, int rows) { return T / rows + n + 2; }
 

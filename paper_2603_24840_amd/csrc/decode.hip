@@ -276,12 +276,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a, int64_t p
     const int64_t rest = block / a.kv_heads;
     const int kvh = static_cast<int>((block + rest) % a.kv_heads);
     int row, split;
-    int64_t first, end;
+    int64_t first, begin, end;
     if (prefix) {
         const int64_t tiles = tile_bound(static_cast<int64_t>(a.n) * per, a.groups.n, 16 * NQ);       // tiles of the same range lie next to each other
         split = static_cast<int>(rest / tiles);
         int segment;
-        if (!find_tile<16 * NQ>([&](int s) { return a.groups.bound(s) * per; }, a.groups.n + 2, rest % tiles, lane, segment, first, end)) return;
+        if (!find_tile<16 * NQ>([&](int s) { return a.groups.bound(s) * per; }, a.groups.n + 2, rest % tiles, lane, segment, first, begin, end)) return;
         if (segment < 1 || segment > a.groups.n) return;
         row = segment - 1;
     } else {

@@ -494,7 +494,7 @@ struct Packed {
     }
 };
 
-// q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out
+// q, k, v, cu_seqlens, cu_seqlens_k, causal, scale, out, workspace (as score_mlp's)
 PyObject* attention(Args& a) {
     const Packed p(a, 0, 3);
     if (a.odd) return nullptr;
@@ -502,13 +502,16 @@ PyObject* attention(Args& a) {
     if (a.given(7) && a.refuse(a.odd || a.tensor(7).sizes() != p.q.t.sizes())) return nullptr;
     void* st = stream(a, p.q.t);
     if (a.odd) return nullptr;
+    Scratch ws(a, 8, arrol_attention_workspace_bytes(p.q.n, p.k.n, p.n, p.q.heads, p.q.hd), true);
+    if (a.odd) return nullptr;
     at::Tensor out, lse;
     const bool own = !a.given(7);
     if (failed("arrol_attention", launch([&] {
+            ws.get(p.q.t);
             if (own) po = made(out, p.q.t.sizes(), at::kBFloat16, p.q.t);
             float* pl = made<float>(lse, {p.q.heads, p.q.n}, at::kFloat, p.q.t);
             return arrol_attention(data(p.q.t), p.q.stride, data(p.k.t), p.k.stride, data(p.v.t), p.v.stride, p.cu, p.cu_k, p.q.n, p.k.n, p.n, p.q.heads,
-                                   p.k.heads, p.q.hd, p.causal, p.scale, po, pl, st);
+                                   p.k.heads, p.q.hd, p.causal, p.scale, po, pl, ws.p, ws.bytes, st);
         })))
         return nullptr;
     return tuple(own ? wrap(std::move(out)) : keep(a[7]), wrap(std::move(lse)));
@@ -700,7 +703,7 @@ PyMethodDef methods[] = {
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&setup)), METH_FASTCALL, nullptr},
     ENTRY(score, 7), ENTRY(score_mlp, 7), ENTRY(score_grad, 6), ENTRY(score_mlp_grad, 9), ENTRY(adamw_step, 11), ENTRY(select, 7),
     ENTRY(weighted_vote, 5), ENTRY(histogram, 3), ENTRY(calibrate, 3), ENTRY(prune_bernoulli, 4), ENTRY(grpo_advantage, 4),
-    ENTRY(grpo_objective, 10), ENTRY(attention, 8), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10),
+    ENTRY(grpo_objective, 10), ENTRY(attention, 9), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -27,16 +27,20 @@ def packed(**kw):
 
 BAD_PACKED = [dict(q=None), dict(k=None), dict(v=None), dict(cu=None), dict(out=None), dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(out=ODD), dict(qs=248), dict(qs=260),
               dict(ks=120), dict(vs=132), dict(Tq=-1), dict(Tk=-1), dict(n=-1), dict(H=3), dict(H=0), dict(KV=0), dict(hd=0), dict(hd=12), dict(hd=136),
-              dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(Tq=2 ** 30, H=4096, KV=4096), dict(n=2 ** 24, H=2)]
+              dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(Tq=2 ** 30, H=4096, KV=4096), dict(n=2 ** 24, H=2), dict(Tk=11), dict(Tk=9)]
 
 
 @pytest.mark.parametrize("bad", BAD_PACKED)
 def test_attention_refuses(L, bad):
-    assert L.arrol_attention(*packed(**bad), None) == -1
+    assert L.arrol_attention(*packed(**bad), FAKE, 1 << 30, None) == -1
 
 
 def test_attention_without_rows_is_a_no_op(L):
-    assert L.arrol_attention(*packed(Tq=0, Tk=0, q=None, k=None, v=None, out=None, cu=None, n=0), None) == 0
+    assert L.arrol_attention(*packed(Tq=0, Tk=0, q=None, k=None, v=None, out=None, cu=None, n=0), None, 0, None) == 0
+    assert L.arrol_attention(*packed(), ODD, 1 << 30, None) == -1
+    size = L.arrol_attention_workspace_bytes
+    assert size(10, 10, 2, 4, 64) == 0 and size(0, 10, 2, 4, 64) == 0               # nothing to cut
+    assert size(1200, 20000, 8, 16, 128) >= 2 * 1200 * 16 * 130 * 4 and size(200000, 200000, 8, 16, 128) == 0
 
 
 @pytest.mark.parametrize("bad", [b for b in BAD_PACKED if "out" not in b] + [dict(o=None), dict(o=ODD), dict(stat=None), dict(go=None), dict(go=ODD), dict(dq=None), dict(dk=None),

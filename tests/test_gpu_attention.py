@@ -229,6 +229,48 @@ def test_gradient_agrees_with_differences(A):
             assert abs(got - want) <= float(np.sum(tol[short] * np.abs(step.numpy()))) + 1e-4 * abs(want) + 1e-3, (name, got, want)
 
 
+@pytest.mark.parametrize("nq,nk,H,KV,hd", [([1, 200, 33], [5000, 3000, 4097], 4, 2, 64), ([150], [9000], 2, 1, 128), ([64, 0, 7], [2600, 2000, 7], 1, 1, 72), ([2000], None, 2, 2, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_queries_over_many_keys_in_ranges(A, nq, nk, H, KV, hd, causal):
+    """Given its workspace the call cuts the keys; without it one workgroup walks over all of them.  Both are held to the reference."""
+    print("[case] attention in ranges nq=%s nk=%s causal=%d" % (nq, nk, causal), flush=True)
+    q, k, v, go, cu_q, cu_k = make(nq, nk, H, KV, hd, 77, before=3, behind=2)
+    assert A.lib().arrol_attention_workspace_bytes(q.shape[0], k.shape[0], len(nq), H, hd) > 0
+    val, tol = reference(q, k, v, cu_q, cu_q if cu_k is None else cu_k, causal, hd ** -0.5)
+    for workspace in ("auto", None):
+        out, lse = A.arrol_attention(q, k, v, cu_q, cu_k, causal=causal, workspace=workspace)
+        torch.cuda.synchronize()
+        agree("out", out, val["out"], tol["out"])
+        agree("lse", lse, val["lse"], tol["lse"])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("lengths,ranges", [([70, 200, 33], None), ([100], [6000])])
+def test_keys_that_a_query_does_not_see_take_no_part(A, lengths, ranges, bad):
+    """NaN and infinities in some keys and values: rows that do not see them are what they are without, and the others no numbers."""
+    print("[case] attention, %g in hidden keys" % bad, flush=True)
+    q, k, v, _, cu_q, cu_k = make(lengths, ranges, 4, 2, 128 if ranges else 64, 5)
+    clean = A.arrol_attention(q, k, v, cu_q, cu_k)
+    ends, starts = npy(cu_q if cu_k is None else cu_k)[1:], npy(cu_q)[:-1]
+    for where in ("k", "v", "both"):
+        x, y = k.clone(), v.clone()
+        spoiled = [(s, end - back) for s, end in enumerate(ends) for back in (1, 9)]
+        for s, at in spoiled:
+            if where != "v":
+                x[at] = bad
+            if where != "k":
+                y[at, :, 3::7] = bad
+        out, lse = A.arrol_attention(q, x, y, cu_q, cu_k)
+        torch.cuda.synchronize()
+        for s, n in enumerate(lengths):
+            good = torch.arange(starts[s], starts[s] + n - 9, device=DEV)          # the row 9 from the end sees the first spoiled key
+            assert torch.equal(lse[:, good], clean[1][:, good]), where
+            off = (out[good].float() - clean[0][good].float()).abs()
+            assert bool((off <= 2 * U * clean[0][good].float().abs() + U * 4.0).all()) and bool(torch.isfinite(out[good].float()).all()), where
+            last = out[starts[s] + n - 1].float()
+            assert not bool(torch.isfinite(last if where == "k" and bad != -float("inf") else last[:, 3::7] if where != "k" else torch.full((1,), float("nan"))).any()), where
+
+
 def test_calls_repeat_bit_for_bit_on_a_side_stream_and_in_a_graph(A):
     print("[case] attention repeated, on a side stream, captured", flush=True)
     q, k, v, go, cu_q, _ = make([200, 90, 333], None, 4, 2, 128, 21)

@@ -26,7 +26,8 @@ def calls(dev):
     scratch = lambda: torch.zeros(1 << 20, dtype=torch.uint8, device=dev)
     return {
         "attention": [((q, k, v, cu), {}), ((q, k2, k2, cu, cu_k), dict(causal=False, scale=0.25)), ((q, k, v, cu), dict(out=torch.zeros(70, 4, 64, dtype=torch.bfloat16, device=dev))),
-                      ((q[:1], k[:1], v[:1], cu), {})],
+                      ((q[:1], k[:1], v[:1], cu), {}), ((q, f(9000, 2, 64).bfloat16(), f(9000, 2, 64).bfloat16(), cu, i64(0, 4000, 9000)), {}),
+                      ((q, k2, k2, cu, cu_k), dict(workspace=None)), ((q, k2, k2, cu, cu_k), dict(workspace=scratch()))],
         "attention_grad": [((q, k, v, out, lse, go, cu), {}), ((q, k2, k2, out, lse, go, cu, cu_k), dict(causal=False, scale=1)), ((q, k, v, out, lse, go, cu), dict(workspace=scratch()))],
         "decode_attention": [((dq, kv, 1, table, lens), {}), ((dq, kv, 0, table, lens, pt, pl, off), {}), ((dq, kv, 1, table, lens, pt, pl, off), dict(want_weight=True, scale=0.2)),
                              ((dq, kv, 1, table, lens), dict(want_weight=True, weight=w)),
