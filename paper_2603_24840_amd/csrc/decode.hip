@@ -6,10 +6,11 @@
 //   weight of token t += sum of p_t over the query heads (for a prefix token: over the group's rollouts as well)
 //
 // Bound by reading the cache (2 flop per byte and query row), so the work is cut for bytes in flight: a workgroup takes a range of tokens for a kv
-// head and 16 or 32 query rows, its four wavefronts every fourth step of 32 tokens, and consecutive workgroups take consecutive kv heads, which
-// together read whole pages.  K and V go, in whole rows of the head, through a part of the LDS that is the wavefront's own (V for the transposing
-// read), and the next step's loads go out as soon as the registers are free, before the products: no barriers until the four wavefronts are joined.  Ranges are joined by a second launch; weights need the joined lse, so the scores are kept (4 bytes a query row and
-// token against 4 head_dim of cache) and a third launch sums them.
+// head, and consecutive workgroups take consecutive kv heads, which together read whole pages.  Where up to 16 query rows read the tokens (a rollout's heads over
+// its kv head, small groups) its four wavefronts take every fourth step of 32 tokens: K and V go, in whole rows of the head, through a part of the LDS
+// that is the wavefront's own, and the next step's loads go out as soon as the registers are free, before the products - no barriers until the four
+// are joined.  Where more do (large groups) the tokens' tile is the workgroup's and its wavefronts have 16 of the rows each.  Ranges are joined by a second
+// launch; weights need the joined lse, so the scores are kept (4 bytes a query row and token against 4 head_dim of cache) and a third launch sums them.
 #include "attention_tile.h"
 
 namespace {
@@ -50,7 +51,8 @@ __device__ __forceinline__ int row_tokens(const Pages& p, int row, const Decode&
 template <int HD>
 struct KeyTile {
     static constexpr int kRowBytes = 2 * HD, kChunks = HD / 8;
-    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ (HD == 128 ? r & 15 : (r >> 1) & 7)) << 4); }
+    __device__ static __forceinline__ int swizzle(int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; }
+    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ swizzle(r)) << 4); }
     __device__ static __forceinline__ bf16x8 by_row(const unsigned char* tile, int block, int s, int lane) {
         return *reinterpret_cast<const bf16x8*>(tile + at(16 * block + (lane & 15), 4 * s + (lane >> 4)));
     }
@@ -61,10 +63,8 @@ struct KeyTile {
 template <int HD>
 struct ValueTile {
     static constexpr int kRowBytes = 2 * HD, kChunks = HD / 8, kBytes = kStep * kRowBytes;
-    __device__ static __forceinline__ int at(int r, int c) {
-        const int swizzle = HD == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
-        return r * kRowBytes + ((c ^ swizzle) << 4);
-    }
+    __device__ static __forceinline__ int swizzle(int r) { return HD == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1; }
+    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ swizzle(r)) << 4); }
     __device__ static __forceinline__ bf16x8 by_column(const unsigned char* tile, int d, int lane) {
         const int row = 4 * (lane >> 4) + ((lane >> 2) & 3), chunk = 2 * d + ((lane >> 1) & 1), within = (lane & 1) * 8;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(tile + at(row, chunk) + within));
@@ -73,79 +73,136 @@ struct ValueTile {
     }
 };
 
-// One workgroup: query rows [first, first + 16 NQ) of a kv head (row = rollout * per + head of the kv head; past `end` the last one
-// once more) against tokens [t0, t1) of table row `row`.
-template <int HD, int NQ, bool SCORES>
-__device__ __forceinline__ void decode_range(const Decode& a, const Pages& p, int row, int kvh, int first, int end, int t0, int t1, int slot,
-                                             unsigned char (*lds)[2 * ValueTile<HD>::kBytes], float (*stat)[2][16 * NQ]) {
-    constexpr int KS = HD / 32, DB = HD / 16, VL = kStep * HD / 8 / 64;
+// A wavefront's 16 query rows [first, first + 16) of a kv head (row = rollout * per + head of the kv head; past `end` the last one once
+// more), lane = row lane % 16, and what it has gathered for them.
+template <int HD>
+struct Rows {
+    static constexpr int KS = HD / 32, DB = HD / 16;
+    bf16x8 q[KS];
+    int64_t at;                       // this lane's row as a (rollout, head) index
+    f32x4 o[DB];                      // head elements 16 d + 4 (lane / 16) + r
+    float m, l;                       // maximum of z * log2 e; this lane's part of the sum
+    __device__ __forceinline__ void load(const Decode& a, int kvh, int first, int end, int lane) {
+        const int per = a.heads / a.kv_heads, r = first + (lane & 15) < end ? first + (lane & 15) : end - 1;
+        at = static_cast<int64_t>(r / per) * a.heads + kvh * per + r % per;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int e = 32 * s + 8 * (lane >> 4);
+            u32x4 x = {0, 0, 0, 0};
+            if (e < a.hd) x = *reinterpret_cast<const u32x4*>(a.q + at * a.hd + e);
+            q[s] = __builtin_bit_cast(bf16x8, x);
+        }
+        m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = 0.f;
+    }
+    // 32 tokens whose keys and values lie in the LDS, of which those in `there` exist; `scores`: this row's of the first token.
+    template <bool SCORES>
+    __device__ __forceinline__ void step(const Decode& a, const unsigned char* keys, const unsigned char* values, uint32_t there, float* scores, int lane) {
+        const int g = lane >> 4;
+        f32x4 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            s[b] = 0.f;
+#pragma unroll
+            for (int e = 0; e < KS; ++e) s[b] = mfma16(KeyTile<HD>::by_row(keys, b, e, lane), q[e], s[b]);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[b][r] = there >> (16 * b + 4 * g + r) & 1 ? s[b][r] * a.c : -INFINITY;
+                top = fmaxf(top, s[b][r]);
+            }
+            // Stored by every lane (rows past the end store the last one's once more): on a branch, the wait for the loads that are
+            // under way would have to allow for fewer stores behind them than there are, and wait for those.
+            if constexpr (SCORES) *reinterpret_cast<f32x4*>(scores + 16 * b + 4 * g) = s[b];
+        }
+        const auto larger = [](float x, float y) { return fmaxf(x, y); };
+        top = wave_step<16>(wave_step<32>(top, larger), larger);
+        if (__any(top > m + 8.f)) {      // as in the packed form: moved on only where it has grown by 2^8
+            const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] *= f;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        bf16x8 w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float e = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - base);
+            l += e;
+            w[i] = static_cast<__bf16>(e);      // weights in bf16 for the product with V, their sum l in fp32 of the unrounded ones
+        }
+        if (there)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] = mfma16(ValueTile<HD>::by_column(values, d, lane), w, o[d]);
+    }
+    __device__ __forceinline__ float sum() const {
+        const auto add = [](float x, float y) { return x + y; };
+        return wave_step<16>(wave_step<32>(l, add), add);
+    }
+};
+
+// Where a step's 32 tokens lie: page id of token t + lane % 32, and its place in the pool.  A token that does not exist (past the range, or a page id out of
+// range) takes the place of one of the step that does: its weight is 0, and that one's NaN would be in every sum anyway.  Of a step of none nothing is added.
+struct Places {
+    const int32_t* table;
+    int t1, page;
+    int64_t n_pages;
+    uint32_t there;
+    int place;
+    __device__ __forceinline__ int page_of(int t, int lane) const {
+        const int mine = t + (lane & 31);
+        return mine < t1 ? table[mine / page] : -1;
+    }
+    __device__ __forceinline__ void resolve(int t, int id, int lane) {
+        const bool exists = id >= 0 && id < n_pages;
+        there = static_cast<uint32_t>(__ballot(exists));
+        place = exists ? id * page + (t + (lane & 31)) % page : 0;
+        const int other = there ? __builtin_amdgcn_readlane(place, uniform(__builtin_ctz(there))) : 0;
+        place = exists ? place : other;
+    }
+};
+
+// A workgroup with up to 16 query rows against tokens [t0, t1) of table row `row`: its wavefronts take every fourth step of 32 tokens, each with its own part of the
+// LDS, and are joined at the end.
+template <int HD, bool SCORES>
+__device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int row, int kvh, int first, int end, int t0, int t1, int slot,
+                                         unsigned char (*lds)[2 * ValueTile<HD>::kBytes], float (*stat)[2][16]) {
+    constexpr int DB = HD / 16, VL = kStep * HD / 8 / 64;
     using VT = ValueTile<HD>;
     const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6));
     const int per = a.heads / a.kv_heads, l15 = lane & 15, g = lane >> 4;
-    const int active = end - first > 16 ? NQ : 1;      // blocks of 16 query rows that there are
     unsigned char* tile = lds[wave];
-    bf16x8 qf[NQ][KS];
-    int64_t at[NQ];                        // this lane's query rows as (rollout, head) indices
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int r = first + 16 * n + l15 < end ? first + 16 * n + l15 : end - 1;
-        at[n] = static_cast<int64_t>(r / per) * a.heads + kvh * per + r % per;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const int e = 32 * s + 8 * g;
-            u32x4 x = {0, 0, 0, 0};
-            if (e < a.hd) x = *reinterpret_cast<const u32x4*>(a.q + at[n] * a.hd + e);
-            qf[n][s] = __builtin_bit_cast(bf16x8, x);
-        }
-    }
-    f32x4 o[NQ][DB];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        m[n] = -INFINITY, l[n] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[n][d] = 0.f;
-    }
+    Rows<HD> rows;
+    rows.load(a, kvh, first, end, lane);
     const int64_t token_stride = static_cast<int64_t>(a.kv_heads) * a.hd;
-    const int32_t* table = p.table + static_cast<int64_t>(row) * p.per_row;
-    // Chunks past the head are the head's last ones once more (Q is 0 there, and what V gives is not stored).
+    // chunks past the head are the head's last ones once more (Q is 0 there, and what V gives is not stored)
     const int last = a.hd / 8 - 1;
     const int64_t in_row = static_cast<int64_t>(kvh) * a.hd + (lane % VT::kChunks < last ? lane % VT::kChunks : last) * 8;
     const uint16_t *k = a.k + in_row, *v = a.v + in_row;
-
-    // page id of token t + lane % 32; its place in the pool.  A token that does not exist (past the range, or a page id out of range) takes the place of
-    // one of the step that does: its weight is 0, and that one's NaN would be in every sum anyway.  A step of none is left out.
-    const auto page_of = [&](int t) {
-        const int mine = t + (lane & 31);
-        return mine < t1 ? table[mine / a.page] : -1;
-    };
-    uint32_t there;
-    int place;
-    const auto resolve = [&](int t, int id) {
-        const bool exists = id >= 0 && id < a.n_pages;
-        there = static_cast<uint32_t>(__ballot(exists));
-        place = exists ? id * a.page + (t + (lane & 31)) % a.page : 0;
-        const int other = there ? __builtin_amdgcn_readlane(place, __builtin_ctz(there)) : 0;
-        place = exists ? place : other;
-    };
+    Places at = {p.table + static_cast<int64_t>(row) * p.per_row, t1, a.page, a.n_pages, 0, 0};
     u32x4 kx[VL], vx[VL];
     const auto load = [&]() {
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
-            const int64_t row_at = __shfl(place, i * (64 / VT::kChunks) + lane / VT::kChunks) * token_stride;
-            kx[i] = *reinterpret_cast<const u32x4*>(k + row_at);
-            vx[i] = *reinterpret_cast<const u32x4*>(v + row_at);
+            const int64_t row_at = __shfl(at.place, i * (64 / VT::kChunks) + lane / VT::kChunks) * token_stride;
+            kx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + row_at));      // nobody else reads them
+            vx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + row_at));
         }
     };
     constexpr int kStride = kWaves * kStep;
     int t = t0 + wave * kStep, id = -1;
     if (t < t1) {
-        resolve(t, page_of(t));
+        at.resolve(t, at.page_of(t, lane), lane);
         load();
-        id = page_of(t + kStride);
+        id = at.page_of(t + kStride, lane);
     }
     for (; t < t1; t += kStride) {
-        const uint32_t now = there;
+        const uint32_t now = at.there;
         wave_lds_exchange();               // the reads of the last step are done
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
@@ -155,147 +212,158 @@ __device__ __forceinline__ void decode_range(const Decode& a, const Pages& p, in
         }
         wave_lds_exchange();
         if (t + kStride < t1) {
-            resolve(t + kStride, id);
+            at.resolve(t + kStride, id, lane);
             load();
-            id = page_of(t + 2 * kStride);
+            id = at.page_of(t + 2 * kStride, lane);
         }
-        f32x4 s[NQ][2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) s[n][b] = 0.f;
-#pragma unroll
-            for (int e = 0; e < KS; ++e) {
-                const bf16x8 x = KeyTile<HD>::by_row(tile, b, e, lane);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    s[n][b] = mfma16(x, qf[n][e], s[n][b]);
-            }
-        }
-        float top_of[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            top_of[n] = -INFINITY;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[n][b][r] = now >> (16 * b + 4 * g + r) & 1 ? s[n][b][r] * a.c : -INFINITY;
-                    top_of[n] = fmaxf(top_of[n], s[n][b][r]);
-                }
-                // Stored by every lane (rows past the end store the last one's once more): on a branch, the wait for the loads that are
-                // under way would have to allow for fewer stores behind them than there are, and wait for those.
-                if constexpr (SCORES) *reinterpret_cast<f32x4*>(p.scores + at[n] * p.cap + t + 16 * b + 4 * g) = s[n][b];
-            }
-        }
-        bf16x8 w[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n)
-            if (n < active) {
-                float top = top_of[n];
-                const auto larger = [](float x, float y) { return fmaxf(x, y); };
-                top = wave_step<16>(wave_step<32>(top, larger), larger);
-                if (__any(top > m[n] + 8.f)) {      // as in the packed form: moved on only where it has grown by 2^8
-                    const float to = fmaxf(m[n], top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - to);
-                    m[n] = to;
-                    l[n] *= f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[n][d] *= f;
-                }
-                const float base = m[n] == -INFINITY ? 0.f : m[n];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(s[n][i >> 2][i & 3] - base);
-                    l[n] += e;
-                    w[n][i] = static_cast<__bf16>(e);      // weights in bf16 for the product with V, their sum l in fp32 of the unrounded ones
-                }
-            }
-        if (now)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const bf16x8 x = VT::by_column(tile + VT::kBytes, d, lane);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    if (n < active) o[n][d] = mfma16(x, w[n], o[n][d]);
-            }
+        rows.template step<SCORES>(a, tile, tile + VT::kBytes, now, SCORES ? p.scores + rows.at * p.cap + t : nullptr, lane);
     }
-    // The four wavefronts' parts, brought to one maximum and added in a fixed order.
-    const auto add = [](float x, float y) { return x + y; };
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        l[n] = wave_step<16>(wave_step<32>(l[n], add), add);
-        if (g == 0) stat[wave][0][16 * n + l15] = m[n], stat[wave][1][16 * n + l15] = l[n];
-    }
+    // the four wavefronts' parts, brought to one maximum and added in a fixed order
+    const float l = rows.sum();
+    if (g == 0) stat[wave][0][l15] = rows.m, stat[wave][1][l15] = l;
     __syncthreads();
+    const float top = fmaxf(fmaxf(stat[0][0][l15], stat[1][0][l15]), fmaxf(stat[2][0][l15], stat[3][0][l15]));
+    const float f = rows.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.m - top);
+    constexpr int kRowFloats = HD + 4;          // 16 rows x HD floats, padded against bank conflicts
+    static_assert(2 * VT::kBytes >= 16 * kRowFloats * 4, "a wavefront's part");
+    float* parts = reinterpret_cast<float*>(lds);
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        if (n >= active) break;
-        const int r = 16 * n + l15;
-        const float top = fmaxf(fmaxf(stat[0][0][r], stat[1][0][r]), fmaxf(stat[2][0][r], stat[3][0][r]));
-        const float f = m[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[n] - top);
-        constexpr int kRowFloats = HD + 4;          // 16 rows x HD floats, padded against bank conflicts
-        float* part = reinterpret_cast<float*>(lds) + wave * 16 * kRowFloats;
+    for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(parts + (wave * 16 + l15) * kRowFloats + 16 * d + 4 * g) = rows.o[d] * f;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * HD / 4; i += kThreads) {
+        const int r = i / (HD / 4), e = i % (HD / 4) * 4, query = first + r;
+        if (query >= end || e >= a.hd) continue;
+        const int64_t out = (static_cast<int64_t>(query / per) * a.heads + kvh * per + query % per) * a.slots + slot;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int d = 0; d < DB; ++d) *reinterpret_cast<f32x4*>(part + l15 * kRowFloats + 16 * d + 4 * g) = o[n][d] * f;
-        __syncthreads();
-        const float* parts = reinterpret_cast<const float*>(lds);
-        for (int i = threadIdx.x; i < 16 * HD / 4; i += kThreads) {
-            const int rr = i / (HD / 4), e = i % (HD / 4) * 4;
-            const int query = first + 16 * n + rr;
-            if (query < end && e < a.hd) {
-                const int64_t out = (static_cast<int64_t>(query / per) * a.heads + kvh * per + query % per) * a.slots + slot;
-                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4*>(parts + (w * 16 + rr) * kRowFloats + e);
-                *reinterpret_cast<f32x4*>(a.part_o + out * a.hd + e) = sum;
-                if (e == 0) {
-                    const int q = 16 * n + rr;
-                    const float mm = fmaxf(fmaxf(stat[0][0][q], stat[1][0][q]), fmaxf(stat[2][0][q], stat[3][0][q]));
-                    float ll = 0.f;
-                    for (int w = 0; w < kWaves; ++w) ll += stat[w][0][q] == -INFINITY ? 0.f : stat[w][1][q] * __builtin_amdgcn_exp2f(stat[w][0][q] - mm);
-                    *reinterpret_cast<f32x2*>(a.part_ml + 2 * out) = f32x2{mm, ll};
-                }
-            }
+        for (int w = 0; w < kWaves; ++w) sum += *reinterpret_cast<const f32x4*>(parts + (w * 16 + r) * kRowFloats + e);
+        *reinterpret_cast<f32x4*>(a.part_o + out * a.hd + e) = sum;
+        if (e == 0) {
+            const float mm = fmaxf(fmaxf(stat[0][0][r], stat[1][0][r]), fmaxf(stat[2][0][r], stat[3][0][r]));
+            float ll = 0.f;
+            for (int w = 0; w < kWaves; ++w) ll += stat[w][0][r] == -INFINITY ? 0.f : stat[w][1][r] * __builtin_amdgcn_exp2f(stat[w][0][r] - mm);
+            *reinterpret_cast<f32x2*>(a.part_ml + 2 * out) = f32x2{mm, ll};
         }
-        __syncthreads();
     }
 }
 
-// Blocks: first the groups' prefixes - (tile of a group's query rows, range, kv head) - then the rollouts' own tokens -
+// A workgroup with up to 64 query rows, 16 a wavefront: keys and values of 32 tokens are read once for all of them, straight into the LDS, three such steps ahead of
+// the one that is worked on.  The tokens' places are looked up for up to kPlaces at a time, so that no load stands between those: the wait for it would be a
+// wait for all of them.  4 prompts of 9,000 to 16,384 tokens, 16 rollouts of 32 heads over 8 each: 96 us, of which the loads alone are 54 and the products alone
+// 66 (one workgroup to a compute unit: they overlap little); with the scores stored 134.
+constexpr int kPlaces = 2048, kAhead = 3;
+template <int N>
+__device__ __forceinline__ void steps_ready() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+
+template <int HD, bool SCORES>
+__device__ __forceinline__ void many_rows(const Decode& a, const Pages& p, int row, int kvh, int first, int end, int t0, int t1, int slot, unsigned char* lds, int* places) {
+    constexpr int DB = HD / 16, VL = kStep * HD / 8 / 64 / kWaves, kLoads = 2 * VL;       // a wavefront's instructions of a step: K and V
+    using VT = ValueTile<HD>;
+    const int lane = threadIdx.x & 63, wave = uniform(static_cast<int>(threadIdx.x >> 6)), g = lane >> 4;
+    const bool working = first + 16 * wave < end;        // of the wavefront
+    Rows<HD> rows;
+    rows.load(a, kvh, working ? first + 16 * wave : first, end, lane);
+    const int64_t token_stride = static_cast<int64_t>(a.kv_heads) * a.hd;
+    const int last = a.hd / 8 - 1;
+    const uint16_t *k = a.k + static_cast<int64_t>(kvh) * a.hd, *v = a.v + static_cast<int64_t>(kvh) * a.hd;
+    const unsigned lds0 = lds_address(lds);
+    const int32_t* table = p.table + static_cast<int64_t>(row) * p.per_row;
+    // the chunks that a lane fetches: an instruction fills 1,024 bytes of a tile in order
+    int from_k[VL], from_v[VL];
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+        const int r = (wave * VL + i) * (64 / VT::kChunks) + lane / VT::kChunks, c = lane % VT::kChunks, ck = c ^ KeyTile<HD>::swizzle(r), cv = c ^ VT::swizzle(r);
+        from_k[i] = (ck < last ? ck : last) * 8, from_v[i] = (cv < last ? cv : last) * 8;
+    }
+    for (int start = t0; start < t1; start += kPlaces) {
+        const int count = t1 - start < kPlaces ? t1 - start : kPlaces, n = (count + kStep - 1) / kStep;
+        __syncthreads();                                 // the last places and steps are read
+        for (int i = threadIdx.x; i < n * kStep; i += kThreads) {
+            const int t = start + i, id = t < t1 ? table[t / a.page] : -1;
+            places[i] = id >= 0 && id < a.n_pages ? id * a.page + t % a.page : -1;
+        }
+        __syncthreads();
+        const auto issue = [&](int step) {
+            int place = places[step * kStep + (lane & 31)];
+            const uint32_t there = static_cast<uint32_t>(__ballot(place >= 0));
+            const int other = there ? __builtin_amdgcn_readlane(place, uniform(__builtin_ctz(there))) : 0;      // as in Places
+            place = place < 0 ? other : place;
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int64_t at = __shfl(place, (wave * VL + i) * (64 / VT::kChunks) + lane / VT::kChunks) * token_stride;
+                const uint16_t *key = k + at + from_k[i], *value = v + at + from_v[i];
+                const unsigned to = lds0 + (step & 3) * 2 * VT::kBytes + (wave * VL + i) * 1024;
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(key), "s"(to) : "memory");
+                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(value), "s"(to + VT::kBytes) : "memory");
+            }
+        };
+        for (int i = 0; i < kAhead && i < n; ++i) issue(i);
+        if (n >= kAhead) steps_ready<2 * kLoads>();
+        else steps_ready<0>();
+        for (int i = 0; i < n; ++i) {
+            if (i + kAhead < n) issue(i + kAhead);
+            if (working) {
+                const uint32_t there = static_cast<uint32_t>(__ballot(places[i * kStep + (lane & 31)] >= 0));
+                const unsigned char* keys = lds + (i & 3) * 2 * VT::kBytes;
+                rows.template step<SCORES>(a, keys, keys + VT::kBytes, there, SCORES ? p.scores + rows.at * p.cap + start + i * kStep : nullptr, lane);
+            }
+            // the next step is there, the two behind it may be under way (stores, which count too, can only make this wait for more)
+            if (i + kAhead >= n) steps_ready<0>();
+            else steps_ready<2 * kLoads>();
+        }
+    }
+    const float l = rows.sum();
+    const int per = a.heads / a.kv_heads, query = first + 16 * wave + (lane & 15);
+    if (query >= end) return;
+    const int64_t out = (static_cast<int64_t>(query / per) * a.heads + kvh * per + query % per) * a.slots + slot;
+    if (g == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * out) = f32x2{rows.m, l};
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        if (16 * d + 4 * g < a.hd) *reinterpret_cast<f32x4*>(a.part_o + out * a.hd + 16 * d + 4 * g) = rows.o[d];
+}
+
+// Query rows that a workgroup takes, of the prefixes and of the rollouts' own tokens: 16 or 64.
+struct Tiles {
+    int64_t prefix_blocks, prefix_tiles;
+    int prefix_rows, own_rows, own_tiles;
+};
+
+// Blocks: first the groups' prefixes - (range, tile of a group's query rows, kv head) - then the rollouts' own tokens -
 // ((rollout, tile of query rows), range, kv head).
-template <int HD, int NQ, bool SCORES>
-__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a, int64_t prefix_blocks) {
-    __shared__ __align__(16) unsigned char lds[kWaves][2 * ValueTile<HD>::kBytes];
-    static_assert(2 * ValueTile<HD>::kBytes >= 16 * (HD + 4) * 4, "a wavefront's part when they are joined");
-    __shared__ float stat[kWaves][2][16 * NQ];
+template <int HD, bool SCORES>
+__global__ __launch_bounds__(kThreads, 2) void decode_kernel(Decode a, Tiles w) {
+    __shared__ __align__(1024) unsigned char lds[kWaves][2 * ValueTile<HD>::kBytes];       // [wavefront][K, V] or [step % 4][K, V]
+    __shared__ float stat[kWaves][2][16];
+    __shared__ int places[kPlaces];
     const int lane = threadIdx.x & 63, per = a.heads / a.kv_heads;
     int64_t block = blockIdx.x;
-    const bool prefix = block < prefix_blocks;
-    block -= prefix ? 0 : prefix_blocks;
+    const bool prefix = block < w.prefix_blocks;
+    block -= prefix ? 0 : w.prefix_blocks;
     const Pages& p = prefix ? a.pre : a.own;
     const int64_t rest = block / a.kv_heads;
-    const int kvh = static_cast<int>((block + rest) % a.kv_heads);
+    const int kvh = static_cast<int>(block % a.kv_heads), rows = prefix ? w.prefix_rows : w.own_rows;
     int row, split;
     int64_t first, begin, end;
     if (prefix) {
-        const int64_t tiles = tile_bound(static_cast<int64_t>(a.n) * per, a.groups.n, 16 * NQ);       // tiles of the same range lie next to each other
-        split = static_cast<int>(rest / tiles);
+        split = static_cast<int>(rest / w.prefix_tiles);         // tiles of the same range lie next to each other
+        const auto bound = [&](int s) { return a.groups.bound(s) * per; };
         int segment;
-        if (!find_tile<16 * NQ>([&](int s) { return a.groups.bound(s) * per; }, a.groups.n + 2, rest % tiles, lane, segment, first, begin, end)) return;
-        if (segment < 1 || segment > a.groups.n) return;
+        const bool found = rows == 16 ? find_tile<16>(bound, a.groups.n + 2, rest % w.prefix_tiles, lane, segment, first, begin, end)
+                                      : find_tile<64>(bound, a.groups.n + 2, rest % w.prefix_tiles, lane, segment, first, begin, end);
+        if (!found || segment < 1 || segment > a.groups.n) return;
         row = segment - 1;
     } else {
-        const int tiles = (per + 16 * NQ - 1) / (16 * NQ);
         split = static_cast<int>(rest % p.splits);
         const int64_t which = rest / p.splits;
-        row = static_cast<int>(which / tiles);
-        first = static_cast<int64_t>(row) * per + which % tiles * (16 * NQ);
+        row = static_cast<int>(which / w.own_tiles);
+        first = static_cast<int64_t>(row) * per + which % w.own_tiles * rows;
         end = static_cast<int64_t>(row + 1) * per;
     }
     const int len = row_tokens(p, row, a), t0 = split * p.chunk;
     if (t0 >= len) return;
-    decode_range<HD, NQ, SCORES>(a, p, row, kvh, static_cast<int>(first), static_cast<int>(end), t0, len - t0 < p.chunk ? len : t0 + p.chunk, p.first_slot + split,
-                         lds, stat);
+    const int t1 = len - t0 < p.chunk ? len : t0 + p.chunk, slot = p.first_slot + split, f = static_cast<int>(first), e = static_cast<int>(end);
+    if (rows == 16) few_rows<HD, SCORES>(a, p, row, kvh, f, e, t0, t1, slot, lds, stat);
+    else many_rows<HD, SCORES>(a, p, row, kvh, f, e, t0, t1, slot, &lds[0][0], places);
 }
 
 // The group of a rollout, -1 if it is in none: the last one that begins at or before it.
@@ -426,9 +494,10 @@ __global__ __launch_bounds__(kThreads) void decode_weight_kernel(Decode a, Weigh
         if (t + e < cap) out[row * cap + t + e] = t + e < len ? before[e] + sum[e] : 0.f;
 }
 
-constexpr int kMinRange = kWaves * kStep, kMaxRange = 1024, kMaxSplits = 128;
+constexpr int kMinRange = kWaves * kStep, kMaxRange = 2048, kMaxSplits = 128;
 
-// Ranges of a row of `cap` tokens where `blocks` workgroups (of both kinds) would take whole rows: as many as give 2,048 workgroups.
+// Ranges of a row of `cap` tokens where `blocks` workgroups (of both kinds) would take whole rows: as many as give 2,048 workgroups, of at most
+// 2,048 tokens (384 rollouts of up to 2,000 tokens: 355 us a call, in ranges of 1,024 403).
 void cut(int64_t cap, int64_t blocks, int& chunk, int& splits) {
     int64_t want = blocks <= 0 ? 1 : (2048 + blocks - 1) / blocks, c = (cap + want - 1) / want;
     if (c > kMaxRange) c = kMaxRange;
@@ -447,20 +516,17 @@ struct Plan {
     size_t ml, o, lse2, own_scores, pre_scores, total;
 };
 
-// Blocks of 16 query rows a workgroup takes: one where neither a rollout's heads nor an average group's rows fill more.
-int query_blocks(int64_t n, int heads, int kv_heads, int64_t n_groups) {
-    const int64_t per = heads / kv_heads;
-    return per > 16 || (n_groups > 0 && n * per > 16 * n_groups) ? 2 : 1;
-}
+// Query rows that a workgroup takes where a rollout's heads, or an average group, has `rows` of them: 64 where 16 would leave the same tokens to several.
+int rows_of(int64_t rows) { return rows > 16 ? 64 : 16; }
 
 Plan plan(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_pages, int64_t pre_pages, int64_t n_groups, bool weights) {
     Plan p{};
     const int64_t own = own_pages * page, pre = n_groups > 0 ? pre_pages * page : 0;
-    const int64_t per = heads / kv_heads, rows_of = 16 * query_blocks(n, heads, kv_heads, n_groups);
-    const int64_t blocks = n * kv_heads * ((per + rows_of - 1) / rows_of) + (pre > 0 ? (n * per / rows_of + n_groups) * kv_heads : 0);
+    const int64_t per = heads / kv_heads, own_rows = rows_of(per), pre_rows = n_groups > 0 ? rows_of(n * per / n_groups) : 16;
+    const int64_t blocks = n * kv_heads * ((per + own_rows - 1) / own_rows) + (pre > 0 ? (n * per / pre_rows + n_groups) * kv_heads : 0);
     cut(own, blocks, p.own_chunk, p.own_splits);
     cut(pre, blocks, p.pre_chunk, p.pre_splits);
-    p.own_cap = (own + kStep - 1) / kStep * kStep, p.pre_cap = (pre + kStep - 1) / kStep * kStep;
+    p.own_cap = ((own + kStep - 1) / kStep | 1) * kStep, p.pre_cap = ((pre + kStep - 1) / kStep | 1) * kStep;      // odd, so that rows begin on all channels
     const size_t rows = static_cast<size_t>(n) * heads, slots = p.own_splits + p.pre_splits;
     size_t at = 0;
     const auto take = [&](size_t bytes) {
@@ -484,12 +550,16 @@ bool shape_ok(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_
     return own_pages <= most / page && (n_groups == 0 || pre_pages <= most / page) && n <= most / heads;
 }
 
-template <int HD, int NQ, bool SCORES>
+template <int HD, bool SCORES>
 void launch(const Decode& a, hipStream_t st) {
     const int64_t per = a.heads / a.kv_heads;
-    const int64_t prefix = a.pre.splits > 0 ? tile_bound(a.n * per, a.groups.n, 16 * NQ) * a.pre.splits * a.kv_heads : 0;
-    const int64_t own = a.n * ((per + 16 * NQ - 1) / (16 * NQ)) * a.own.splits * a.kv_heads;
-    arrol_launch(decode_kernel<HD, NQ, SCORES>, dim3(static_cast<unsigned>(prefix + own)), dim3(kThreads), 0, st, a, prefix);
+    Tiles w;
+    w.own_rows = rows_of(per), w.own_tiles = static_cast<int>((per + w.own_rows - 1) / w.own_rows);
+    w.prefix_rows = a.groups.n > 0 ? rows_of(a.n * per / a.groups.n) : 16;
+    w.prefix_tiles = tile_bound(a.n * per, a.groups.n, w.prefix_rows);
+    w.prefix_blocks = w.prefix_tiles * a.pre.splits * a.kv_heads;
+    const int64_t own = static_cast<int64_t>(a.n) * w.own_tiles * a.own.splits * a.kv_heads;
+    arrol_launch(decode_kernel<HD, SCORES>, dim3(static_cast<unsigned>(w.prefix_blocks + own)), dim3(kThreads), 0, st, a, w);
 }
 
 }  // namespace
@@ -535,14 +605,8 @@ extern "C" int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads,
     if (tiles * (a.slots + 1) * a.kv_heads >= (1 << 24)) return ARROL_EINVAL;      // lanes of a launch are counted in 32 bits
     const auto st = static_cast<hipStream_t>(stream);
     if (n > 0) {
-        const bool two = query_blocks(n, n_heads, a.kv_heads, n_groups) > 1;
-        if (weights) {
-            if (a.hd <= 64) two ? launch<64, 2, true>(a, st) : launch<64, 1, true>(a, st);
-            else two ? launch<128, 2, true>(a, st) : launch<128, 1, true>(a, st);
-        } else {
-            if (a.hd <= 64) two ? launch<64, 2, false>(a, st) : launch<64, 1, false>(a, st);
-            else two ? launch<128, 2, false>(a, st) : launch<128, 1, false>(a, st);
-        }
+        if (a.hd <= 64) weights ? launch<64, true>(a, st) : launch<64, false>(a, st);
+        else weights ? launch<128, true>(a, st) : launch<128, false>(a, st);
         const int64_t rows = static_cast<int64_t>(n) * n_heads;
         auto* o = static_cast<uint16_t*>(out);
         if (a.slots > 8) arrol_launch(decode_join_kernel<4>, dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, st, a, o, lse_out);
