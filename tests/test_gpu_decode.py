@@ -240,6 +240,22 @@ def test_many_ranges(A):
     Batch([1], [30000], [40001], 2, 1, 64, 16, 2).check(A, want_weight=True)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_groups_of_many_query_rows(A, hd):
+    """64 query rows and more of a kv head read a prefix: tiles of 64 rows, some with wavefronts that have none, groups of very different sizes."""
+    print("[case] decode, large groups hd=%d" % hd, flush=True)
+    b = Batch([16, 3, 21], [500, 1, 2100], [1 + 7 * i for i in range(40)], 16, 4, hd, 16, 50)
+    b.check(A, want_weight=True)
+    b.check(A, layer=0)
+
+
+def test_ranges_longer_than_the_table_of_places(A):
+    """More than 128 x 2,048 tokens: a workgroup's range is looked up in parts; 20 query rows for the parts' shared path, and 2 for the other."""
+    for H in (20, 2):
+        print("[case] decode, 270,000 tokens, heads=%d" % H, flush=True)
+        Batch([1], [270000], [300], H, 1, 16, 16, 51, layers=1).check(A, layer=0, want_weight=True)
+
+
 def test_single_tokens_are_the_last_rows_of_the_packed_form(A):
     """The same keys through arrol_attention (nq = 1): both forms are held to the same reference within their tolerances."""
     print("[case] decode against the packed form", flush=True)
