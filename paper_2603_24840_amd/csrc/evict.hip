@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / ARROL_WAVE;
+constexpr int kPlanThreads = 1024;       // of the larger form
 constexpr int kCopyThreads = 256, kCopyMoves = 32, kInFlight = 8;
 
 struct Move { int64_t from, to; };      // places (page * page_tokens + offset) of a token; -1: a page id out of range
@@ -33,6 +33,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 }
 
 // How many of the workgroup's threads before this one have `flag` set, and (in total) how many have it at all.
+template <int WAVES>
 __device__ __forceinline__ int rank_in_block(bool flag, int* totals, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t votes = __ballot(flag);
@@ -41,15 +42,20 @@ __device__ __forceinline__ int rank_in_block(bool flag, int* totals, int& total)
     __syncthreads();
     int before = 0;
     total = 0;
-    for (int w = 0; w < kPlanWaves; ++w) {
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
         before += w < wave ? totals[w] : 0;
         total += totals[w];
     }
     return before + __popcll(votes & ((uint64_t{1} << lane) - 1));
 }
 
-__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(Evict a) {
-    __shared__ int bins[256], totals[kPlanWaves];
+// THREADS: 256 for rows of up to 512 tokens, whose barriers are the time (32 rows of 64: 9.2 us a call, with 1,024 threads 9.9), 1,024 for longer ones
+// (128 rows of 1,024: 224 us, with 256 threads 226).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_plan_kernel(Evict a) {
+    constexpr int kWaves = THREADS / ARROL_WAVE;
+    __shared__ int bins[256], totals[kWaves];
     __shared__ uint32_t digit_found;
     __shared__ int left_over;
     const int row = blockIdx.x, tid = threadIdx.x;
@@ -69,7 +75,7 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(Evict a) {
             for (int shift = 24; shift >= 0; shift -= 8) {
                 if (tid < 256) bins[tid] = 0;
                 __syncthreads();
-                for (int t = lo + tid; t < hi; t += kPlanThreads) {
+                for (int t = lo + tid; t < hi; t += THREADS) {
                     const uint32_t u = order_of(weight[t]);
                     if ((u & mask) == prefix) atomicAdd(&bins[u >> shift & 255], 1);
                 }
@@ -99,19 +105,19 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(Evict a) {
         }
         // what stays: larger than the smallest one that stays, and the first `need` of its equals
         int ties = 0, freed = 0;
-        for (int start = 0; start < len; start += kPlanThreads) {
+        for (int start = 0; start < len; start += THREADS) {
             const int t = start + tid;
             const bool between = t >= lo && t < hi;
             const uint32_t u = between ? order_of(weight[t]) : 0;
             const bool tie = between && u == prefix;
             int total;
-            const int rank = ties + rank_in_block(tie, totals, total);
+            const int rank = ties + rank_in_block<kWaves>(tie, totals, total);
             ties += total;
             const bool stays = t < len && (!between || u > prefix || (tie && rank < need));
             const bool mover = stays && t >= left, hole = !stays && t < left;
-            const int place = rank_in_block(mover, totals, total) + moved;
+            const int place = rank_in_block<kWaves>(mover, totals, total) + moved;
             moved += total;
-            const int slot = rank_in_block(hole, totals, total) + freed;
+            const int slot = rank_in_block<kWaves>(hole, totals, total) + freed;
             freed += total;
             if (mover || hole) {
                 const int id = table[t / a.page];
@@ -128,24 +134,24 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(Evict a) {
     const int32_t* position = a.position ? a.position + base : nullptr;
     int32_t* position_out = a.position_out + base;
     float* weight_out = a.weight_out + base;
-    for (int t = tid; t < left; t += kPlanThreads) {
+    for (int t = tid; t < left; t += THREADS) {
         weight_out[t] = weight[t];
         position_out[t] = position ? position[t] : t;
     }
     __syncthreads();
-    for (int k = tid; k < moved; k += kPlanThreads) {
+    for (int k = tid; k < moved; k += THREADS) {
         const int64_t at = static_cast<int64_t>(row) * a.most + k;
         const int from = a.from[at], to = a.to[at];
         weight_out[to] = weight[from];
         position_out[to] = position ? position[from] : from;
     }
     __syncthreads();
-    for (int t = left + tid; t < cap; t += kPlanThreads) {
+    for (int t = left + tid; t < cap; t += THREADS) {
         weight_out[t] = 0.f;
         position_out[t] = -1;
     }
     const int pages = (left + a.page - 1) / a.page;
-    for (int p = tid; p < a.per_row; p += kPlanThreads) a.table_out[static_cast<int64_t>(row) * a.per_row + p] = p < pages ? table[p] : -1;
+    for (int p = tid; p < a.per_row; p += THREADS) a.table_out[static_cast<int64_t>(row) * a.per_row + p] = p < pages ? table[p] : -1;
     if (tid == 0) a.len_out[row] = left;
 }
 
@@ -226,7 +232,8 @@ extern "C" int arrol_evict(void* kv, arrol_kv_layout layout, const int32_t* bloc
     a.n_pages = layout.n_pages, a.per_row = max_pages_per_seq, a.page = layout.page_tokens;
     a.budget = budget, a.first = n_first, a.recent = n_recent, a.most = static_cast<int>(most);
     const auto st = static_cast<hipStream_t>(stream);
-    arrol_launch(evict_plan_kernel, dim3(n_rows), dim3(kPlanThreads), 0, st, a);
+    if (cap <= 512) arrol_launch(evict_plan_kernel<256>, dim3(n_rows), dim3(256), 0, st, a);
+    else arrol_launch(evict_plan_kernel<kPlanThreads>, dim3(n_rows), dim3(kPlanThreads), 0, st, a);
     if (most > 0) {
         const int64_t groups = (most + kCopyMoves - 1) / kCopyMoves, blocks = groups * n_rows * layout.n_layers * 2;
         const int64_t slab = layout.n_pages * layout.page_tokens * token_bytes;
