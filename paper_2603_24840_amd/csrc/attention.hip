@@ -31,17 +31,22 @@ __device__ __forceinline__ void split_block(unsigned block, int kv_heads, int& k
 
 __device__ __forceinline__ int clamp32(int64_t n) { return uniform(static_cast<int>(n < 0 ? 0 : n < 32 ? n : 32)); }
 
-// Where a workgroup's 128 queries of a head lie, and which keys they see.
+// Where a workgroup's queries lie, and which keys they see.  Its four wavefronts have 32 rows each: 32 rows of HEADS = 4 heads of a kv head, 64 of 2, or
+// 128 of one - as many heads as share it, so that few rows (short or ragged sequences) fill the workgroup, and its wavefronts see the same keys: 64 prompts
+// of up to 512 tokens, 32 heads over 8, 69 us, with one head a workgroup 79.
+template <int HEADS>
 struct QueryBlock {
+    static constexpr int kRows = kOwn / HEADS;
     int64_t row0, k_begin;          // the wavefront's first row; the sequence's first key
-    int nk, own_valid;              // keys; rows of the wavefront that there are
+    int head, nk, own_valid;        // the wavefront's; keys; rows of the wavefront that there are
     int sees;                       // keys that this lane's row sees
     int sees_least, sees_most;      // over the wavefront's rows (causal: its first and its last valid row)
     int reach;                      // most over the workgroup's rows
-    __device__ __forceinline__ bool find(const Problem& a, int64_t tile, int wave, int lane) {
+    __device__ __forceinline__ bool find(const Problem& a, int64_t tile, int first_head, int wave, int lane) {
         int segment;
         int64_t first, q_begin, end;
-        if (!find_tile<kOwn>(a.pq, tile, lane, segment, first, q_begin, end)) return false;
+        if (!find_tile<kRows>(a.pq, tile, lane, segment, first, q_begin, end)) return false;
+        head = first_head + wave % HEADS;
         const int nq = uniform(static_cast<int>(end - q_begin));
         k_begin = 0, nk = 0;
         if (segment >= 1 && segment <= a.pq.n) {       // rows of no sequence see no keys: zeros
@@ -50,18 +55,18 @@ struct QueryBlock {
             const int64_t n = (same ? end : a.pk.bound(segment + 1)) - k_begin;
             nk = uniform(static_cast<int>(n < 0 ? 0 : n));
         }
-        row0 = first + 32 * wave;
+        row0 = first + 32 * (wave / HEADS);
         own_valid = clamp32(end - row0);
         // query i of its sequence sees keys j < min(nk, i + 1 + nk - nq)
         const auto seen_by = [&](int i) {
             const int s = a.causal ? nk + (i + 1 - nq) : nk;
             return s < 0 ? 0 : s < nk ? s : nk;
         };
-        const int at = uniform(static_cast<int>(first - q_begin)), i0 = at + 32 * wave;
+        const int at = uniform(static_cast<int>(first - q_begin)), i0 = at + 32 * (wave / HEADS);
         sees = seen_by(i0 + (lane & 31));
         sees_least = seen_by(i0);
         sees_most = own_valid > 0 ? seen_by(i0 + own_valid - 1) : 0;
-        reach = seen_by((nq - at < kOwn ? nq - at : kOwn) - 1 + at);
+        reach = seen_by((nq - at < kRows ? nq - at : kRows) - 1 + at);
         return true;
     }
 };
@@ -77,8 +82,8 @@ struct Output {
 // O of a wavefront's rows over the keys [from, to), once more and by themselves: key by key, so that a key takes no part in a row that does not see it.  Where
 // all rows see all keys, or V is finite, the matrix instructions give the same; but the product of a hidden key's weight, 0, and an
 // infinity or NaN of its value is NaN.  Only rows that hold such values come here.
-template <int HD>
-__device__ __forceinline__ void repair_rows(const Problem& a, const QueryBlock& w, const bf16x8 (&qf)[HD / 16], int kvh, int from, int to, float base, int lane, f32x16 (&o)[HD / 32]) {
+template <int HD, class Block>
+__device__ __forceinline__ void repair_rows(const Problem& a, const Block& w, const bf16x8 (&qf)[HD / 16], int kvh, int from, int to, float base, int lane, f32x16 (&o)[HD / 32]) {
     const int half = lane >> 5;
     const float c = a.scale * kLog2e;
 #pragma unroll
@@ -110,12 +115,12 @@ __device__ __forceinline__ void repair_rows(const Problem& a, const QueryBlock& 
     }
 }
 
-// Forward pass: a workgroup takes 128 queries of a head, a wavefront 32 of them, and walks over the keys in tiles of 64.
+// Forward pass: a workgroup walks over the keys in tiles of 64, a wavefront with 32 queries of a head.
 // S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.  The tiles that come next are on their way into the other halves of the
 // LDS.  With heads of 128, whose registers leave two wavefronts to a SIMD, the scores of the next tile are formed while the exponentials of this one
 // are (K runs a tile ahead of V): 4 survivors of up to 4,096 tokens, 32 heads over 8, 298 us against 355.  With heads of 64 four fit, which
 // do that for each other: 64 prompts of up to 512 tokens 83 us, and 108 the other way.
-template <int HD>
+template <int HD, int HEADS>
 __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem a, int64_t tiles, Output to) {
     constexpr int BK = 64;
     constexpr bool kAhead = HD == 128;
@@ -123,15 +128,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
     constexpr int kTileBytes = BK * T::kRowBytes;
     __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];      // [slot][K, V]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int per = a.heads / a.kv_heads;
+    const int per = a.heads / a.kv_heads, head_blocks = per / HEADS;
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
-    const int head = kvh * per + static_cast<int>(rest % per);
-    rest /= per;
+    const int first_head = kvh * per + static_cast<int>(rest % head_blocks) * HEADS;
+    rest /= head_blocks;
     const int split = static_cast<int>(rest % to.splits);
-    QueryBlock w;
-    if (!w.find(a, tiles - 1 - rest / to.splits, wave, lane)) return;
+    QueryBlock<HEADS> w;
+    if (!w.find(a, tiles - 1 - rest / to.splits, first_head, wave, lane)) return;
+    const int head = w.head;
     // this workgroup's tiles of 64 keys: those that some of its rows see, or a range of them
     const int all = (w.reach + BK - 1) / BK, t_lo = static_cast<int>(static_cast<int64_t>(all) * split / to.splits),
               n_tiles = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / to.splits) - t_lo;
@@ -507,10 +513,10 @@ bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const
     return true;
 }
 
-// dQ: a workgroup takes 128 queries of a head (Q and dO as fragments in registers) and walks over the keys in tiles of 64.
+// dQ: a workgroup walks over the keys in tiles of 64, a wavefront with 32 queries of a head (Q and dO as fragments in registers).
 // S^T = K Q^T, dP^T = V dO^T, dQ^T += K^T dS^T.  It goes first, and leaves what the other kernel needs of a row: -lse / scale, and behind all
 // of those -D, D_i = <do_i, o_i>, in fp32.
-template <int HD>
+template <int HD, int HEADS>
 __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ out, const uint16_t* __restrict__ go,
                                                                        const float* __restrict__ lse, float* __restrict__ stats, uint16_t* __restrict__ dq) {
     constexpr int BK = 64;
@@ -518,13 +524,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
     constexpr int kTileBytes = BK * T::kRowBytes;
     __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int per = a.heads / a.kv_heads;
+    const int per = a.heads / a.kv_heads, head_blocks = per / HEADS;
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
-    const int head = kvh * per + static_cast<int>(rest % per);
-    QueryBlock w;
-    if (!w.find(a, tiles - 1 - rest / per, wave, lane)) return;
+    QueryBlock<HEADS> w;
+    if (!w.find(a, tiles - 1 - rest / head_blocks, kvh * per + static_cast<int>(rest % head_blocks) * HEADS, wave, lane)) return;
+    const int head = w.head;
     const int n_tiles = (w.reach + BK - 1) / BK;
 
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
@@ -646,6 +652,29 @@ size_t stat_bytes(int64_t T, int heads) { return static_cast<size_t>(T) * heads 
 }  // namespace
 
 namespace {
+// Heads of a kv head that a workgroup takes.
+int heads_together(int per) { return per % 4 == 0 ? 4 : per % 2 == 0 ? 2 : 1; }
+int64_t query_tiles(int64_t T, int n_seq, int per) { return tile_bound(T, n_seq, kOwn / heads_together(per)); }
+
+template <int HD>
+void launch_forward(const Problem& a, const Output& to, hipStream_t st) {
+    const int per = a.heads / a.kv_heads, together = heads_together(per);
+    const int64_t tiles = query_tiles(a.pq.T, a.pq.n, per);
+    const dim3 grid(static_cast<unsigned>(tiles * (a.heads / together) * to.splits));
+    if (together == 4) arrol_launch(attention_forward_kernel<HD, 4>, grid, dim3(kThreads), 0, st, a, tiles, to);
+    else if (together == 2) arrol_launch(attention_forward_kernel<HD, 2>, grid, dim3(kThreads), 0, st, a, tiles, to);
+    else arrol_launch(attention_forward_kernel<HD, 1>, grid, dim3(kThreads), 0, st, a, tiles, to);
+}
+template <int HD>
+void launch_grad_q(const Problem& a, const uint16_t* out, const uint16_t* go, const float* lse, float* stats, uint16_t* dq, hipStream_t st) {
+    const int per = a.heads / a.kv_heads, together = heads_together(per);
+    const int64_t tiles = query_tiles(a.pq.T, a.pq.n, per);
+    const dim3 grid(static_cast<unsigned>(tiles * (a.heads / together)));
+    if (together == 4) arrol_launch(attention_grad_q_kernel<HD, 4>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
+    else if (together == 2) arrol_launch(attention_grad_q_kernel<HD, 2>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
+    else arrol_launch(attention_grad_q_kernel<HD, 1>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
+}
+
 // Ranges that the keys of a sequence are cut into: enough for 1,024 workgroups, as long as a range keeps 256 keys of an average sequence.
 int key_splits(int64_t T_q, int64_t T_k, int n_seq, int heads) {
     const int64_t blocks = (T_q / kOwn + n_seq) * heads, by_work = (1024 + blocks - 1) / (blocks > 0 ? blocks : 1), by_keys = n_seq > 0 ? T_k / n_seq / 256 : 1;
@@ -668,15 +697,14 @@ extern "C" int arrol_attention(const void* q, int64_t q_stride, const void* k, i
     if (const int rc = check(a, T_q, T_k)) return rc;
     if (T_q == 0) return ARROL_OK;
     if (!out || !arrol_aligned16(out) || (workspace && !arrol_aligned16(workspace))) return ARROL_EINVAL;
-    const int64_t tiles = tile_bound(T_q, n_seq, kOwn), rows = T_q * n_heads;
+    const int64_t rows = T_q * n_heads;
     int splits = key_splits(T_q, T_k, n_seq, n_heads);
     if (!workspace || workspace_bytes < part_bytes(T_q, n_heads, head_dim, splits)) splits = 1;
     auto* ws = static_cast<float*>(workspace);
     const Output to = {static_cast<uint16_t*>(out), lse_out, splits, ws, splits > 1 ? ws + static_cast<size_t>(splits) * rows * head_dim : nullptr};
-    const dim3 grid(static_cast<unsigned>(tiles * n_heads * splits));
     const auto st = static_cast<hipStream_t>(stream);
-    if (head_dim <= 64) arrol_launch(attention_forward_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, to);
-    else arrol_launch(attention_forward_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, to);
+    if (head_dim <= 64) launch_forward<64>(a, to, st);
+    else launch_forward<128>(a, to, st);
     if (splits > 1) arrol_launch(attention_join_kernel, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(kThreads), 0, st, to, T_q, n_heads, head_dim);
     return arrol_launch_status();
 }
@@ -699,12 +727,10 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
     const auto *go = static_cast<const uint16_t*>(grad_out);
     auto* stats = static_cast<float*>(workspace);
     if (T_q > 0) {
-        const int64_t tiles = tile_bound(T_q, n_seq, kOwn);
-        const dim3 grid(static_cast<unsigned>(tiles * n_heads));
         const auto* o = static_cast<const uint16_t*>(out);
         auto* dq = static_cast<uint16_t*>(grad_q);
-        if (head_dim <= 64) arrol_launch(attention_grad_q_kernel<64>, grid, dim3(kThreads), 0, st, a, tiles, o, go, lse, stats, dq);
-        else arrol_launch(attention_grad_q_kernel<128>, grid, dim3(kThreads), 0, st, a, tiles, o, go, lse, stats, dq);
+        if (head_dim <= 64) launch_grad_q<64>(a, o, go, lse, stats, dq, st);
+        else launch_grad_q<128>(a, o, go, lse, stats, dq, st);
     }
     if (T_k > 0) {
         const auto blocks = static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads);

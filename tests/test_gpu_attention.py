@@ -137,6 +137,14 @@ def test_head_sizes(A, hd):
     check(A, *make([70, 130], None, 3, 3, hd, hd), True)
 
 
+@pytest.mark.parametrize("H,KV", [(8, 1), (12, 2), (5, 1), (10, 5), (1, 1), (16, 16), (28, 4)])
+def test_heads_over_kv_heads(A, H, KV):
+    """A workgroup takes four, two or one of the heads that share a kv head."""
+    print("[case] attention heads=%d/%d" % (H, KV), flush=True)
+    check(A, *make([33, 1, 129, 64], None, H, KV, 64, H), True)
+    check(A, *make([40, 3], [70, 300], H, KV, 128, H), True)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("nq,nk", [([1, 1], [500, 1]), ([5, 200, 33], [300, 200, 40]), ([130, 64, 10], [100, 0, 3]), ([40], [1]), ([0, 17], [90, 129])])
 def test_keys_of_other_lengths_and_rows_that_see_nothing(A, nq, nk, causal):
