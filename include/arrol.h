@@ -490,9 +490,10 @@ int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_st
  * rounded to bf16 for their products).  No atomics: bit-reproducible run to run.  Rows of no sequence get zeros.
  * Other sequences' rows take no part, whatever they hold; a NaN or infinity of a row, though, may reach the gradients of the 32 rows around it in
  * its own sequence, whether or not they see it.
- * workspace: arrol_attention_grad_workspace_bytes(T_q, n_heads) bytes, 16-byte aligned.
+ * workspace: arrol_attention_grad_workspace_bytes(...) bytes of the same sizes, 16-byte aligned.
  */
-size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int32_t n_heads);
+size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                                            int32_t head_dim);
 int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                          const void* out, const float* lse, const void* grad_out, const int64_t* cu_seqlens_q,
                          const int64_t* cu_seqlens_k, int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads,

@@ -95,7 +95,7 @@ _SIGNATURES = {
     "arrol_attention": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i32, _i32, _i32, _i32, _i32, _f32,
                                        _vp, _vp, _vp, _sz, _vp]),
     "arrol_attention_workspace_bytes": (_sz, [_i64, _i64, _i32, _i32, _i32]),
-    "arrol_attention_grad_workspace_bytes": (_sz, [_i64, _i32]),
+    "arrol_attention_grad_workspace_bytes": (_sz, [_i64, _i64, _i32, _i32, _i32, _i32]),
     "arrol_attention_grad": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32,
                                             _i32, _i32, _f32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "arrol_decode_attention_workspace_bytes": (_sz, [_i32] * 9),
@@ -807,7 +807,8 @@ def _py_attention_grad(q, k, v, out, lse, grad_out, cu_seqlens, cu_seqlens_k=Non
         raise ValueError("out and grad_out must have the shape of q, lse [n_heads, T_q]")
     dev = q.device
     if workspace is None:
-        workspace = torch.empty(max(lib().arrol_attention_grad_workspace_bytes(q.shape[0], q.shape[1]), 16), dtype=torch.uint8, device=dev)
+        need = lib().arrol_attention_grad_workspace_bytes(q.shape[0], k.shape[0], cu_seqlens.numel() - 1, q.shape[1], k.shape[1], q.shape[2])
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
     grads = dict(grad_q=torch.empty(q.shape, dtype=torch.bfloat16, device=dev), grad_k=torch.empty(k.shape, dtype=torch.bfloat16, device=dev),
                  grad_v=torch.empty(k.shape, dtype=torch.bfloat16, device=dev))
     rc = lib().arrol_attention_grad(*head, _ptr(out, torch.bfloat16, "out"), _ptr(lse, torch.float32, "lse"),

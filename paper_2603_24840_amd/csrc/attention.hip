@@ -345,6 +345,45 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(Output to, int
     if (to.lse && e == 0) to.lse[at % heads * T + at / heads] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
+// A gradient on its way out: bf16 rows [T, heads, hd], or, where the walk is cut into ranges because there are few workgroups, every range's fp32 sums
+// [range][T, heads, hd], which attention_grad_join_kernel adds in order.
+struct Sums {
+    uint16_t* out;
+    float* part;
+    int64_t T;
+    int heads;
+};
+template <int HD>
+__device__ __forceinline__ void store_sums(const f32x16 (&acc)[HD / 32], float factor, unsigned char* tile, const Sums& to, int splits, int split, int64_t row0, int head, int valid,
+                                           int hd, int lane) {
+    const int64_t stride = static_cast<int64_t>(to.heads) * hd, at = row0 * stride + static_cast<int64_t>(head) * hd;
+    if (splits == 1) {
+        store_own<HD>(acc, factor, tile, to.out + at, stride, valid, hd, lane);
+        return;
+    }
+    if ((lane & 31) >= valid) return;
+    float* mine = to.part + split * to.T * stride + at + (lane & 31) * stride;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int e = 32 * d + 8 * b + 4 * (lane >> 5);
+            if (e < hd) *reinterpret_cast<f32x4*>(mine + e) = f32x4{acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2], acc[d][4 * b + 3]} * factor;
+        }
+}
+// 8 elements a lane
+__global__ __launch_bounds__(kThreads) void attention_grad_join_kernel(const float* __restrict__ part, int64_t n, int splits, uint16_t* __restrict__ out) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 8;
+    if (i >= n) return;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+    for (int s = 0; s < splits; ++s) {
+        const f32x4* p = reinterpret_cast<const f32x4*>(part + s * n + i);
+        x += p[0], y += p[1];
+    }
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    *reinterpret_cast<bf16x8*>(out + i) = __builtin_convertvector((f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}), bf16x8);
+}
+
 // dK and dV: a workgroup takes 128 keys of a kv head and walks over the queries of every head that reads them in tiles of 64, a wavefront with 32
 // of the keys (K and V as fragments in registers); the sum over the shared heads is made in registers, in a fixed order.
 // With heads of 128, whose registers leave two wavefronts to a SIMD, these are two groups of four of one workgroup: each takes every other tile (with its own
@@ -355,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(Output to, int
 // dp - D come out of the matrix cores (a row that sees nothing has lse = -inf, and is masked everywhere); dV^T += dO^T P, dK^T += Q^T dS.
 template <int HD, int GROUPS>
 __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attention_grad_kv_kernel(Problem a, const uint16_t* __restrict__ go, const float* __restrict__ stats,
-                                                                          uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
+                                                                                           int splits, Sums dk, Sums dv) {
     constexpr int BQ = 64;
     using T = Tile<HD>;
     constexpr int kTileBytes = BQ * T::kRowBytes, kSlot = 2 * kTileBytes + 2 * BQ * 4;
@@ -366,6 +405,8 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     int kvh;
     int64_t tile;
     split_block(blockIdx.x, a.kv_heads, kvh, tile);
+    const int split = static_cast<int>(tile % splits);
+    tile /= splits;
     int segment;
     int64_t first, k_begin, end;
     if (!find_tile<kOwn>(a.pk, tile, lane, segment, first, k_begin, end)) return;
@@ -387,7 +428,8 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     const int from = seen_from(j0 + (lane & 31)), from_least = seen_from(j0), from_most = seen_from(j0 + 31);
     const int t_first = seen_from(j0 - 32 * wave) / BQ;
     const int n_t = (nq + BQ - 1) / BQ > t_first ? (nq + BQ - 1) / BQ - t_first : 0;
-    const int total = n_t * per;                      // tiles, head by head
+    // tiles, head by head; this workgroup's are those from t_lo on
+    const int t_lo = static_cast<int>(static_cast<int64_t>(n_t) * per * split / splits), total = static_cast<int>(static_cast<int64_t>(n_t) * per * (split + 1) / splits) - t_lo;
 
     bf16x8 kf[HD / 16], vf[HD / 16];
     load_own<HD>(kf, a.k + row0 * a.k_stride + static_cast<int64_t>(kvh) * a.hd, a.k_stride, own_valid, a.hd, lane);
@@ -400,7 +442,7 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
 
     Stream<HD, BQ, kWaves> qs, gs;
     const unsigned lds0 = lds_address(lds) + group * 2 * kSlot, row_at = T::row_base(lane), column_at = T::column_base(lane);
-    int h = 0, ti = group, pointed = 0;               // head and tile that are fetched next
+    int h = n_t > 0 ? t_lo / n_t : 0, ti = t_lo - h * n_t + group, at = ti, pointed = 0;      // head and tile that are fetched next, tile that is worked on
     const auto wrap = [&](int& tile_of, int* head_of) {
         while (tile_of >= n_t) {
             tile_of -= n_t;
@@ -469,7 +511,6 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     const int mine = (total - group + GROUPS - 1) / GROUPS;      // this group's tiles: group, group + GROUPS, ...
     if (mine > 0) fetch(0);
     tiles_ready();
-    int at = group;
     for (int t = 0; t < (total + GROUPS - 1) / GROUPS; ++t) {
         if (t + 1 < mine) fetch((t + 1) & 1);
         if (t < mine) {
@@ -499,17 +540,16 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
             }
         if (group == 1) return;
     }
-    const int64_t out_stride = static_cast<int64_t>(a.kv_heads) * a.hd, to = row0 * out_stride + static_cast<int64_t>(kvh) * a.hd;
     unsigned char* own = lds + wave * 32 * T::kRowBytes;
-    store_own<HD>(gk, a.scale, own, dk + to, out_stride, own_valid, a.hd, lane);
-    store_own<HD>(gv, 1.f, own, dv + to, out_stride, own_valid, a.hd, lane);
+    store_sums<HD>(gk, a.scale, own, dk, splits, split, row0, kvh, own_valid, a.hd, lane);
+    store_sums<HD>(gv, 1.f, own, dv, splits, split, row0, kvh, own_valid, a.hd, lane);
 }
 template <int HD, int GROUPS>
-bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const float* stats, void* dk, void* dv, hipStream_t st) {
+bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const float* stats, int splits, const Sums& dk, const Sums& dv, hipStream_t st) {
     constexpr int kLds = GROUPS * 2 * (2 * 64 * Tile<HD>::kRowBytes + 512);
     static arrol_device_flags allowed;
     if (!arrol_allow_lds(attention_grad_kv_kernel<HD, GROUPS>, kLds, allowed)) return false;
-    arrol_launch(attention_grad_kv_kernel<HD, GROUPS>, dim3(blocks), dim3(GROUPS * kThreads), kLds, st, a, go, stats, static_cast<uint16_t*>(dk), static_cast<uint16_t*>(dv));
+    arrol_launch(attention_grad_kv_kernel<HD, GROUPS>, dim3(blocks), dim3(GROUPS * kThreads), kLds, st, a, go, stats, splits, dk, dv);
     return true;
 }
 
@@ -518,7 +558,7 @@ bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const
 // of those -D, D_i = <do_i, o_i>, in fp32.
 template <int HD, int HEADS>
 __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a, int64_t tiles, const uint16_t* __restrict__ out, const uint16_t* __restrict__ go,
-                                                                       const float* __restrict__ lse, float* __restrict__ stats, uint16_t* __restrict__ dq) {
+                                                                       const float* __restrict__ lse, float* __restrict__ stats, int splits, Sums dq) {
     constexpr int BK = 64;
     using T = Tile<HD>;
     constexpr int kTileBytes = BK * T::kRowBytes;
@@ -528,10 +568,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
     int kvh;
     int64_t rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
+    const int first_head = kvh * per + static_cast<int>(rest % head_blocks) * HEADS;
+    rest /= head_blocks;
+    const int split = static_cast<int>(rest % splits);
     QueryBlock<HEADS> w;
-    if (!w.find(a, tiles - 1 - rest / head_blocks, kvh * per + static_cast<int>(rest % head_blocks) * HEADS, wave, lane)) return;
-    const int head = w.head;
-    const int n_tiles = (w.reach + BK - 1) / BK;
+    if (!w.find(a, tiles - 1 - rest / splits, first_head, wave, lane)) return;
+    const int head = w.head, all = (w.reach + BK - 1) / BK, t_lo = static_cast<int>(static_cast<int64_t>(all) * split / splits),
+              n_tiles = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / splits) - t_lo;
 
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
     bf16x8 qf[HD / 16], gf[HD / 16];
@@ -550,25 +593,25 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
         if ((lane & 31) < w.own_valid) {
             const int64_t at = static_cast<int64_t>(head) * a.pq.T + w.row0 + (lane & 31);
             mine[0] = -lse[at] / a.scale;
-            stats[half ? static_cast<int64_t>(a.heads) * a.pq.T + at : at] = mine[half];
+            if (split == 0) stats[half ? static_cast<int64_t>(a.heads) * a.pq.T + at : at] = mine[half];
         }
     }
-    const uint16_t* kp = uniform(a.k + w.k_begin * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
-    const uint16_t* vp = uniform(a.v + w.k_begin * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* kp = uniform(a.k + (w.k_begin + static_cast<int64_t>(t_lo) * BK) * a.k_stride + static_cast<int64_t>(kvh) * a.hd);
+    const uint16_t* vp = uniform(a.v + (w.k_begin + static_cast<int64_t>(t_lo) * BK) * a.v_stride + static_cast<int64_t>(kvh) * a.hd);
     f32x16 gq[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d) gq[d] = 0.f;
     const float c = a.scale * kLog2e;
 
     Stream<HD, BK, kWaves> ks, vs;
-    const int whole = w.nk / BK;
+    const int keys = w.nk - t_lo * BK, whole = keys / BK;
     const auto point = [&](int valid) {
         ks.point(static_cast<unsigned>(a.k_stride) * 2, valid, a.hd, wave, lane);
         vs.point(static_cast<unsigned>(a.v_stride) * 2, valid, a.hd, wave, lane);
     };
     const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
     const auto fetch = [&](int t) {
-        if (t == whole) point(w.nk - t * BK);
+        if (t == whole) point(keys - t * BK);
         const unsigned to = lds0 + (t & 1) * 2 * kTileBytes;
         ks.issue(kp, to, wave);
         vs.issue(vp, to + kTileBytes, wave);
@@ -612,12 +655,12 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
         if (t + 1 < n_tiles) fetch(t + 1);
 #pragma unroll 1
         for (int b = 0; b < 2; ++b) {
-            const int j = t * BK + 32 * b;
+            const int j = (t_lo + t) * BK + 32 * b;
             if (j < w.sees_most) step(t, b, j);
         }
         tiles_ready();
     }
-    store_own<HD>(gq, a.scale, &lds[0][0][0] + wave * 32 * T::kRowBytes, dq + (w.row0 * a.heads + head) * a.hd, go_stride, w.own_valid, a.hd, lane);
+    store_sums<HD>(gq, a.scale, &lds[0][0][0] + wave * 32 * T::kRowBytes, dq, splits, split, w.row0, head, w.own_valid, a.hd, lane);
 }
 
 bool row_stride_ok(int64_t stride, int64_t rows, int heads, int hd) {
@@ -647,7 +690,6 @@ Problem problem(const void* q, int64_t q_stride, const void* k, int64_t k_stride
     return a;
 }
 
-size_t stat_bytes(int64_t T, int heads) { return static_cast<size_t>(T) * heads * 2 * sizeof(float); }
 
 }  // namespace
 
@@ -666,13 +708,13 @@ void launch_forward(const Problem& a, const Output& to, hipStream_t st) {
     else arrol_launch(attention_forward_kernel<HD, 1>, grid, dim3(kThreads), 0, st, a, tiles, to);
 }
 template <int HD>
-void launch_grad_q(const Problem& a, const uint16_t* out, const uint16_t* go, const float* lse, float* stats, uint16_t* dq, hipStream_t st) {
+void launch_grad_q(const Problem& a, const uint16_t* out, const uint16_t* go, const float* lse, float* stats, int splits, const Sums& dq, hipStream_t st) {
     const int per = a.heads / a.kv_heads, together = heads_together(per);
     const int64_t tiles = query_tiles(a.pq.T, a.pq.n, per);
-    const dim3 grid(static_cast<unsigned>(tiles * (a.heads / together)));
-    if (together == 4) arrol_launch(attention_grad_q_kernel<HD, 4>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
-    else if (together == 2) arrol_launch(attention_grad_q_kernel<HD, 2>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
-    else arrol_launch(attention_grad_q_kernel<HD, 1>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, dq);
+    const dim3 grid(static_cast<unsigned>(tiles * (a.heads / together) * splits));
+    if (together == 4) arrol_launch(attention_grad_q_kernel<HD, 4>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, splits, dq);
+    else if (together == 2) arrol_launch(attention_grad_q_kernel<HD, 2>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, splits, dq);
+    else arrol_launch(attention_grad_q_kernel<HD, 1>, grid, dim3(kThreads), 0, st, a, tiles, out, go, lse, stats, splits, dq);
 }
 
 // Ranges that the keys of a sequence are cut into: enough for 1,024 workgroups, as long as a range keeps 256 keys of an average sequence.
@@ -681,6 +723,27 @@ int key_splits(int64_t T_q, int64_t T_k, int n_seq, int heads) {
     const int64_t s = by_work < by_keys ? by_work : by_keys;
     return static_cast<int>(s < 1 ? 1 : s < 16 ? s : 16);
 }
+// Ranges of the gradient's walks, in the same manner: dQ's over the keys, dK/dV's over the queries of all heads that share a kv head.
+struct GradPlan {
+    int q_splits, kv_splits;
+    size_t stats, q, kv;            // floats
+};
+GradPlan grad_plan(int64_t T_q, int64_t T_k, int n_seq, int heads, int kv_heads, int hd) {
+    const auto cut = [](int64_t blocks, int64_t enough, int64_t steps) {       // a range keeps 2 tiles of 64 rows of an average sequence
+        const int64_t by_work = enough / (blocks > 0 ? blocks : 1), s = by_work < steps / 2 ? by_work : steps / 2;
+        return static_cast<int>(s < 1 ? 1 : s < 16 ? s : 16);
+    };
+    const int64_t per = heads / kv_heads, seqs = n_seq > 0 ? n_seq : 1;
+    GradPlan p;
+    p.q_splits = cut((T_q / kOwn + n_seq) * heads, 512, T_k / seqs / 64);
+    p.kv_splits = cut((T_k / kOwn + n_seq) * kv_heads, 512, T_q / seqs / 64 * per);
+    p.stats = static_cast<size_t>(T_q) * heads * 2;
+    p.q = p.q_splits > 1 ? static_cast<size_t>(p.q_splits) * T_q * heads * hd : 0;
+    p.kv = p.kv_splits > 1 ? static_cast<size_t>(p.kv_splits) * T_k * kv_heads * hd : 0;
+    return p;
+}
+// Partial sums begin on 16 bytes behind the statistics.
+size_t up4(size_t floats) { return (floats + 3) / 4 * 4; }
 size_t part_bytes(int64_t T, int heads, int hd, int splits) { return splits == 1 ? 0 : static_cast<size_t>(splits) * T * heads * (hd + 2) * sizeof(float); }
 }  // namespace
 
@@ -709,8 +772,10 @@ extern "C" int arrol_attention(const void* q, int64_t q_stride, const void* k, i
     return arrol_launch_status();
 }
 
-extern "C" size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int32_t n_heads) {
-    return T_q <= 0 || n_heads <= 0 ? 0 : stat_bytes(T_q, n_heads);
+extern "C" size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    if (T_q < 0 || T_k < 0 || n_seq < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || head_dim < 8 || head_dim > 128) return 0;
+    const GradPlan p = grad_plan(T_q, T_k, n_seq, n_heads, n_kv_heads, head_dim);
+    return (up4(p.stats) + p.q + 2 * p.kv) * sizeof(float);
 }
 
 extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -722,23 +787,34 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
     if (const int rc = check(a, T_q, T_k)) return rc;
     if (T_q > 0 && (!out || !lse || !grad_out || !grad_q || !arrol_aligned16(out) || !arrol_aligned16(grad_out) || !arrol_aligned16(grad_q))) return ARROL_EINVAL;
     if (T_k > 0 && (!grad_k || !grad_v || !arrol_aligned16(grad_k) || !arrol_aligned16(grad_v))) return ARROL_EINVAL;
-    if (T_q > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < stat_bytes(T_q, n_heads))) return ARROL_EWORKSPACE;
+    const GradPlan p = grad_plan(T_q, T_k, n_seq, n_heads, n_kv_heads, head_dim);
+    const size_t need = (up4(p.stats) + p.q + 2 * p.kv) * sizeof(float);
+    if (need > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < need)) return ARROL_EWORKSPACE;
     const auto st = static_cast<hipStream_t>(stream);
-    const auto *go = static_cast<const uint16_t*>(grad_out);
+    const auto* go = static_cast<const uint16_t*>(grad_out);
     auto* stats = static_cast<float*>(workspace);
+    const Sums dq = {static_cast<uint16_t*>(grad_q), p.q ? stats + up4(p.stats) : nullptr, T_q, n_heads};
+    const Sums dk = {static_cast<uint16_t*>(grad_k), p.kv ? stats + up4(p.stats) + p.q : nullptr, T_k, n_kv_heads};
+    const Sums dv = {static_cast<uint16_t*>(grad_v), p.kv ? stats + up4(p.stats) + p.q + p.kv : nullptr, T_k, n_kv_heads};
+    const auto join = [&](const Sums& to, int splits) {
+        const int64_t n = to.T * to.heads * head_dim;
+        if (splits > 1) arrol_launch(attention_grad_join_kernel, dim3(static_cast<unsigned>((n / 8 + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, to.part, n, splits, to.out);
+    };
     if (T_q > 0) {
         const auto* o = static_cast<const uint16_t*>(out);
-        auto* dq = static_cast<uint16_t*>(grad_q);
-        if (head_dim <= 64) launch_grad_q<64>(a, o, go, lse, stats, dq, st);
-        else launch_grad_q<128>(a, o, go, lse, stats, dq, st);
+        if (head_dim <= 64) launch_grad_q<64>(a, o, go, lse, stats, p.q_splits, dq, st);
+        else launch_grad_q<128>(a, o, go, lse, stats, p.q_splits, dq, st);
+        join(dq, p.q_splits);
     }
     if (T_k > 0) {
-        const auto blocks = static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads);
-        const bool ok = head_dim > 64 ? launch_grad_kv<128, 2>(a, blocks, go, stats, grad_k, grad_v, st) : launch_grad_kv<64, 1>(a, blocks, go, stats, grad_k, grad_v, st);
+        const auto blocks = static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads * p.kv_splits);
+        const bool ok = head_dim > 64 ? launch_grad_kv<128, 2>(a, blocks, go, stats, p.kv_splits, dk, dv, st) : launch_grad_kv<64, 1>(a, blocks, go, stats, p.kv_splits, dk, dv, st);
         if (!ok) {
             arrol_launch_status();
             return ARROL_EHIP;
         }
+        join(dk, p.kv_splits);
+        join(dv, p.kv_splits);
     }
     return arrol_launch_status();
 }

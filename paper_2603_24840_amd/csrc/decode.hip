@@ -190,7 +190,7 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int64_t row_at = __shfl(at.place, i * (64 / VT::kChunks) + lane / VT::kChunks) * token_stride;
-            kx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + row_at));      // nobody else reads them
+            kx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + row_at));      // read by this workgroup alone, as a rule
             vx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + row_at));
         }
     };

@@ -525,7 +525,7 @@ PyObject* attention_grad(Args& a) {
     if (a.odd || a.refuse(o.sizes() != p.q.t.sizes() || go.sizes() != p.q.t.sizes() || lse.dim() != 2 || lse.size(0) != p.q.heads || lse.size(1) != p.q.n)) return nullptr;
     void* st = stream(a, p.q.t);
     if (a.odd) return nullptr;
-    const size_t need = arrol_attention_grad_workspace_bytes(p.q.n, p.q.heads);
+    const size_t need = p.k.heads < 1 ? 0 : arrol_attention_grad_workspace_bytes(p.q.n, p.k.n, p.n, p.q.heads, p.k.heads, p.q.hd);
     Scratch ws(a, 10, need > 16 ? need : 16);
     if (a.odd) return nullptr;
     at::Tensor gq, gk, gv;

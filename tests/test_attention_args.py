@@ -55,8 +55,10 @@ def grad(L, ws=FAKE, nbytes=1 << 30, o=FAKE, stat=FAKE, go=FAKE, dq=FAKE, dk=FAK
 
 
 def test_attention_gradient_asks_for_its_workspace(L):
-    need = L.arrol_attention_grad_workspace_bytes(10, 4)
-    assert need >= 10 * 4 * 4 and L.arrol_attention_grad_workspace_bytes(0, 4) == 0
+    size = L.arrol_attention_grad_workspace_bytes
+    need = size(10, 10, 2, 4, 2, 64)
+    assert need >= 2 * 10 * 4 * 4 and size(0, 0, 0, 4, 2, 64) == 0 and size(10, 10, 2, 4, 3, 64) == 0
+    assert size(4000, 4000, 1, 4, 1, 64) >= 2 * 4000 * 4 * 4 + 2 * 2 * 4000 * 64 * 4      # one long sequence, few heads: walks in ranges
     assert grad(L, ws=None) == -2 and grad(L, nbytes=need - 1) == -2 and grad(L, ws=ODD) == -2
     assert grad(L, Tq=0, Tk=0, ws=None, nbytes=0) == 0
 

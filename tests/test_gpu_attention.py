@@ -252,6 +252,18 @@ def test_few_queries_over_many_keys_in_ranges(A, nq, nk, H, KV, hd, causal):
         agree("lse", lse, val["lse"], tol["lse"])
 
 
+@pytest.mark.parametrize("nq,nk,H,KV,hd", [([1100], None, 4, 1, 64), ([900, 70], None, 2, 2, 128), ([700, 1, 0], [1500, 900, 300], 3, 1, 72), ([60], [2500], 2, 1, 128), ([2500], [64], 4, 2, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradient_of_few_heads_in_ranges(A, nq, nk, H, KV, hd, causal):
+    """Few workgroups: the walks over keys and queries are cut, and the ranges' sums added."""
+    print("[case] attention gradient in ranges nq=%s nk=%s heads=%d/%d hd=%d causal=%d" % (nq, nk, H, KV, hd, causal), flush=True)
+    args = make(nq, nk, H, KV, hd, 78, before=5, behind=1)
+    T = args[0].shape[0]
+    assert A.lib().arrol_attention_grad_workspace_bytes(T, args[1].shape[0], len(nq), H, KV, hd) > 2 * T * H * 4 + 16
+    check(A, *args, causal)
+    check(A, *args, causal)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("lengths,ranges", [([70, 200, 33], None), ([100], [6000])])
 def test_keys_that_a_query_does_not_see_take_no_part(A, lengths, ranges, bad):
