@@ -24,9 +24,9 @@ struct Problem {
 
 // What a workgroup works on: tiles of the packed rows x heads.  Consecutive workgroups take consecutive kv heads (with 8 of
 // them an XCD's L2 sees one kv head), then the query heads that share it, and tiles from the last one down where late ones are long.
-__device__ __forceinline__ void split_block(unsigned block, int kv_heads, int& kvh, int64_t& rest) {
+__device__ __forceinline__ void split_block(unsigned block, int kv_heads, int& kvh, int& rest) {      // (a grid has fewer than 2^24 workgroups)
     kvh = static_cast<int>(block % static_cast<unsigned>(kv_heads));
-    rest = block / static_cast<unsigned>(kv_heads);
+    rest = static_cast<int>(block / static_cast<unsigned>(kv_heads));
 }
 
 __device__ __forceinline__ int clamp32(int64_t n) { return uniform(static_cast<int>(n < 0 ? 0 : n < 32 ? n : 32)); }
@@ -129,18 +129,16 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
     __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];      // [slot][K, V]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads, head_blocks = per / HEADS;
-    int kvh;
-    int64_t rest;
+    int kvh, rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
-    const int first_head = kvh * per + static_cast<int>(rest % head_blocks) * HEADS;
+    const int first_head = kvh * per + rest % head_blocks * HEADS;
     rest /= head_blocks;
-    const int split = static_cast<int>(rest % to.splits);
+    const int split = rest % to.splits;
     QueryBlock<HEADS> w;
     if (!w.find(a, tiles - 1 - rest / to.splits, first_head, wave, lane)) return;
     const int head = w.head;
     // this workgroup's tiles of 64 keys: those that some of its rows see, or a range of them
-    const int all = (w.reach + BK - 1) / BK, t_lo = static_cast<int>(static_cast<int64_t>(all) * split / to.splits),
-              n_tiles = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / to.splits) - t_lo;
+    const int all = (w.reach + BK - 1) / BK, t_lo = all * split / to.splits, n_tiles = all * (split + 1) / to.splits - t_lo;      // (fewer than 2^25 tiles, at most 16 ranges)
 
     bf16x8 qf[HD / 16];
     load_own<HD>(qf, a.q + w.row0 * a.q_stride + static_cast<int64_t>(head) * a.hd, a.q_stride, w.own_valid, a.hd, lane);
@@ -402,10 +400,9 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     const int lane = threadIdx.x & 63, wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int wave = wave8 & (kWaves - 1), group = wave8 / kWaves;
     const int per = a.heads / a.kv_heads;
-    int kvh;
-    int64_t tile;
+    int kvh, tile;
     split_block(blockIdx.x, a.kv_heads, kvh, tile);
-    const int split = static_cast<int>(tile % splits);
+    const int split = tile % splits;
     tile /= splits;
     int segment;
     int64_t first, k_begin, end;
@@ -429,7 +426,7 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     const int t_first = seen_from(j0 - 32 * wave) / BQ;
     const int n_t = (nq + BQ - 1) / BQ > t_first ? (nq + BQ - 1) / BQ - t_first : 0;
     // tiles, head by head; this workgroup's are those from t_lo on
-    const int t_lo = static_cast<int>(static_cast<int64_t>(n_t) * per * split / splits), total = static_cast<int>(static_cast<int64_t>(n_t) * per * (split + 1) / splits) - t_lo;
+    const int t_lo = n_t * per * split / splits, total = n_t * per * (split + 1) / splits - t_lo;      // (fewer than 2^25 tiles, at most 16 ranges)
 
     bf16x8 kf[HD / 16], vf[HD / 16];
     load_own<HD>(kf, a.k + row0 * a.k_stride + static_cast<int64_t>(kvh) * a.hd, a.k_stride, own_valid, a.hd, lane);
@@ -565,16 +562,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
     __shared__ __align__(1024) unsigned char lds[2][2][kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int per = a.heads / a.kv_heads, head_blocks = per / HEADS;
-    int kvh;
-    int64_t rest;
+    int kvh, rest;
     split_block(blockIdx.x, a.kv_heads, kvh, rest);
-    const int first_head = kvh * per + static_cast<int>(rest % head_blocks) * HEADS;
+    const int first_head = kvh * per + rest % head_blocks * HEADS;
     rest /= head_blocks;
-    const int split = static_cast<int>(rest % splits);
+    const int split = rest % splits;
     QueryBlock<HEADS> w;
     if (!w.find(a, tiles - 1 - rest / splits, first_head, wave, lane)) return;
-    const int head = w.head, all = (w.reach + BK - 1) / BK, t_lo = static_cast<int>(static_cast<int64_t>(all) * split / splits),
-              n_tiles = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / splits) - t_lo;
+    const int head = w.head, all = (w.reach + BK - 1) / BK, t_lo = all * split / splits,
+              n_tiles = all * (split + 1) / splits - t_lo;
 
     const int64_t go_stride = static_cast<int64_t>(a.heads) * a.hd;
     bf16x8 qf[HD / 16], gf[HD / 16];
