@@ -515,7 +515,7 @@ int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t
  *   prefix_weight_out, prefix_weight_in fp32 [n_groups, max_pages_per_prefix * page_tokens] in the same way, summed over the group's rollouts too.
  *   The _out may be the _in.  Called for every layer with the same buffers they gather over the layers.
  * n_heads a multiple of layout.n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0;
- *   n_pages * page_tokens below 2^31; n_groups at most 2^20; with weights, fewer than 2^30 tokens in all rows of both tables together.
+ *   n_pages * page_tokens below 2^31; a table row's tokens (max_pages_per_* * page_tokens) below 2^31 - 4096; n_groups at most 2^20; with weights, fewer than 2^30 tokens in all rows of both tables together.
  * fp32 scores, sums and lse; the weights are rounded to bf16 for the product with v.  No atomics: bit-reproducible run to run.
  * workspace: arrol_decode_attention_workspace_bytes(...) bytes, 16-byte aligned (want_weight: 1 where weight_out or prefix_weight_out is given).
  */

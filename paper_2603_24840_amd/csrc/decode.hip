@@ -495,6 +495,10 @@ __global__ __launch_bounds__(kThreads) void decode_weight_kernel(Decode a, Weigh
 }
 
 constexpr int kMinRange = kWaves * kStep, kMaxRange = 2048, kMaxSplits = 128;
+// Tokens past a row's end that the kernels' 32-bit counters may reach: few_rows looks up pages two strides and a step ahead (2 * 128 + 32), many_rows goes in
+// steps of kPlaces.
+constexpr int kPastTheEnd = 4096;
+static_assert(kPastTheEnd >= kPlaces + kStep && kPastTheEnd >= 3 * kWaves * kStep, "tokens are counted in 32 bits");
 
 // Ranges of a row of `cap` tokens where `blocks` workgroups (of both kinds) would take whole rows: as many as give 2,048 workgroups, of at most
 // 2,048 tokens (384 rollouts of up to 2,000 tokens: 355 us a call, in ranges of 1,024 403).
@@ -548,7 +552,7 @@ Plan plan(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_page
 bool shape_ok(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_pages, int64_t pre_pages, int64_t n_groups) {
     if (n < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || hd < 8 || hd > 128 || hd % 8 || page < 1 || own_pages < 1 || n_groups < 0) return false;
     if (n_groups > 0 && pre_pages < 1) return false;
-    const int64_t most = 0x7fffffff - 64;
+    const int64_t most = 0x7fffffff - kPastTheEnd;
     return own_pages <= most / page && (n_groups == 0 || pre_pages <= most / page) && n <= most / heads;
 }
 

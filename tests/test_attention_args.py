@@ -131,3 +131,15 @@ def test_binding_refuses(L):
         A.arrol_evict(kv, i32(4, 1), i32(4), torch.zeros(4, 15), 8)
     with pytest.raises(ValueError):
         A.arrol_evict(kv, i32(4, 1), i32(4), torch.zeros(4, 16), 8)      # on the CPU
+
+
+def test_decode_counts_a_rows_tokens_in_32_bits(L):
+    """The kernels look some tokens past a row's end: a table row has to end 4,096 tokens before 2^31."""
+    import paper_2603_24840_amd as A
+    size = lambda own, pre: L.arrol_decode_attention_workspace_bytes(1, 1, 1, 8, 1, own, pre, 1 if pre else 0, 0)
+    most = 2 ** 31 - 4097
+    assert size(most, 0) > 0 and size(16, most) > 0
+    lay = A.KVLayout(1, 1, 1, 8, 128)
+    for own, pre in ((most + 1, 0), (2 ** 31 - 65, 0), (16, most + 1)):
+        assert size(own, pre) == 0
+        assert decode(L, lay=lay, layer=0, n=1, H=1, width=own, pw=pre, groups=1 if pre else 0) == -1, (own, pre)
