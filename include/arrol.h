@@ -490,6 +490,7 @@ int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_st
  * rounded to bf16 for their products).  No atomics: bit-reproducible run to run.  Rows of no sequence get zeros.
  * Other sequences' rows take no part, whatever they hold; a NaN or infinity of a row, though, may reach the gradients of the 32 rows around it in
  * its own sequence, whether or not they see it.
+ * Sizes as above; with head_dim > 64 also (T_k / 128 + n_seq + 2) * n_kv_heads below 2^23.
  * workspace: arrol_attention_grad_workspace_bytes(...) bytes of the same sizes, 16-byte aligned.
  */
 size_t arrol_attention_grad_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,

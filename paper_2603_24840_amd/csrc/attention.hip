@@ -541,6 +541,7 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
     store_sums<HD>(gk, a.scale, own, dk, splits, split, row0, kvh, own_valid, a.hd, lane);
     store_sums<HD>(gv, 1.f, own, dv, splits, split, row0, kvh, own_valid, a.hd, lane);
 }
+constexpr int groups_of(int hd) { return hd > 64 ? 2 : 1; }
 template <int HD, int GROUPS>
 bool launch_grad_kv(const Problem& a, unsigned blocks, const uint16_t* go, const float* stats, int splits, const Sums& dk, const Sums& dv, hipStream_t st) {
     constexpr int kLds = GROUPS * 2 * (2 * 64 * Tile<HD>::kRowBytes + 512);
@@ -784,6 +785,8 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
     if (T_q > 0 && (!out || !lse || !grad_out || !grad_q || !arrol_aligned16(out) || !arrol_aligned16(grad_out) || !arrol_aligned16(grad_q))) return ARROL_EINVAL;
     if (T_k > 0 && (!grad_k || !grad_v || !arrol_aligned16(grad_k) || !arrol_aligned16(grad_v))) return ARROL_EINVAL;
     const GradPlan p = grad_plan(T_q, T_k, n_seq, n_heads, n_kv_heads, head_dim);
+    const int64_t kv_blocks = tile_bound(T_k, n_seq, kOwn) * n_kv_heads * p.kv_splits;
+    if (kv_blocks * groups_of(head_dim) >= (1 << 24)) return ARROL_EINVAL;      // as in check(), of a workgroup's 256 or 512 lanes
     const size_t need = (up4(p.stats) + p.q + 2 * p.kv) * sizeof(float);
     if (need > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < need)) return ARROL_EWORKSPACE;
     const auto st = static_cast<hipStream_t>(stream);
@@ -803,8 +806,9 @@ extern "C" int arrol_attention_grad(const void* q, int64_t q_stride, const void*
         join(dq, p.q_splits);
     }
     if (T_k > 0) {
-        const auto blocks = static_cast<unsigned>(tile_bound(T_k, n_seq, kOwn) * n_kv_heads * p.kv_splits);
-        const bool ok = head_dim > 64 ? launch_grad_kv<128, 2>(a, blocks, go, stats, p.kv_splits, dk, dv, st) : launch_grad_kv<64, 1>(a, blocks, go, stats, p.kv_splits, dk, dv, st);
+        const auto blocks = static_cast<unsigned>(kv_blocks);
+        const bool ok = head_dim > 64 ? launch_grad_kv<128, groups_of(128)>(a, blocks, go, stats, p.kv_splits, dk, dv, st)
+                                      : launch_grad_kv<64, groups_of(64)>(a, blocks, go, stats, p.kv_splits, dk, dv, st);
         if (!ok) {
             arrol_launch_status();
             return ARROL_EHIP;
