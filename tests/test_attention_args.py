@@ -148,4 +148,4 @@ def test_decode_counts_a_rows_tokens_in_32_bits(L):
 def test_attention_gradient_counts_a_launchs_lanes(L):
     """Workgroups of 512 lanes with heads of more than 64: 2^23 of them are 2^32 lanes."""
     for hd, n, rc in ((128, 2 ** 22 - 3, -2), (128, 2 ** 22 - 2, -1), (72, 2 ** 23 - 3, -1), (64, 2 ** 22 - 2, -2), (64, 2 ** 23 - 3, -2), (64, 2 ** 23 - 2, -1)):
-        assert grad(L, ws=None, n=n, H=2, KV=2, hd=hd) == rc, (hd, n)
+        assert grad(L, ws=None, n=n, H=2, KV=2, hd=hd, ks=256, vs=256) == rc, (hd, n)
