@@ -218,7 +218,8 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
         }
         rows.template step<SCORES>(a, tile, tile + VT::kBytes, now, SCORES ? p.scores + rows.at * p.cap + t : nullptr, lane);
     }
-    // the four wavefronts' parts, brought to one maximum and added in a fixed order
+    // The four wavefronts' parts, brought to one maximum and added in a fixed order.  A maximum takes no notice of NaN: where all scores are NaN it is -inf, as
+    // where there are none, but the sums are NaN, so every part is multiplied, none left out (here and in the join).
     const float l = rows.sum();
     if (g == 0) stat[wave][0][l15] = rows.m, stat[wave][1][l15] = l;
     __syncthreads();
@@ -241,7 +242,7 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
         if (e == 0) {
             const float mm = fmaxf(fmaxf(stat[0][0][r], stat[1][0][r]), fmaxf(stat[2][0][r], stat[3][0][r]));
             float ll = 0.f;
-            for (int w = 0; w < kWaves; ++w) ll += stat[w][0][r] == -INFINITY ? 0.f : stat[w][1][r] * __builtin_amdgcn_exp2f(stat[w][0][r] - mm);
+            for (int w = 0; w < kWaves; ++w) ll += stat[w][1][r] * (stat[w][0][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[w][0][r] - mm));
             *reinterpret_cast<f32x2*>(a.part_ml + 2 * out) = f32x2{mm, ll};
         }
     }
@@ -414,8 +415,8 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(Decode a, uint16_
             }
 #pragma unroll
             for (int u = 0; u < kInFlight; ++u) {
-                const float f = i + u * WAVES < n ? __builtin_amdgcn_exp2f(s[u].x - base) : 0.f;
-                if (f != 0.f) sum += f * s[u].y, x += f * v[u].x, y += f * v[u].y;
+                const float f = __builtin_amdgcn_exp2f(s[u].x - base);
+                if (i + u * WAVES < n) sum += f * s[u].y, x += f * v[u].x, y += f * v[u].y;
             }
         }
     }

@@ -309,3 +309,43 @@ def test_empty_batches(A):
     assert got["out"].shape == (0, 4, 64) and not got["prefix_weight"].any()
     got = A.arrol_decode_attention(b.q, b.kv, 0, *b.args)
     assert got["prefix_weight"] is None
+
+
+def close(got, clean, rows):
+    """Rows that a spoiled one shares a wavefront with: the maximum they are scaled by may move on at other places."""
+    x, y = got[rows].float(), clean[rows].float()
+    assert bool(torch.isfinite(x).all()) and bool(((x - y).abs() <= 2 * U * y.abs() + U * 4.0).all())
+
+
+@pytest.mark.parametrize("sizes,prefix,H,KV,hd", [([2, 2], [60, 300], 4, 2, 64), ([2, 2], [700, 2600], 20, 1, 128)])
+def test_nan_reaches_the_rollout_that_sees_it(A, sizes, prefix, H, KV, hd):
+    """A query, or a key alone in its range of tokens, whose scores are all NaN: no number comes out, not what a rollout without tokens gets."""
+    print("[case] decode, NaN queries and keys, prefix=%s heads=%d/%d" % (prefix, H, KV), flush=True)
+    nan = float("nan")
+    b = Batch(sizes, prefix, [1, 400, 33, 1], H, KV, hd, 16, 61)
+    clean = b.run(A, want_weight=True)
+    q = b.q.clone()
+    b.q[0, 1], b.q[2] = nan, nan                 # one head of the first rollout, all of the third
+    got = b.run(A, want_weight=True)
+    for name in ("out", "lse"):
+        assert bool(torch.isnan(got[name][0, 1]).all()) and bool(torch.isnan(got[name][2]).all()), name
+    others = torch.ones(4, H, dtype=torch.bool, device=DEV)
+    others[0, 1], others[2] = False, False
+    close(got["out"], clean["out"], others)
+    assert bool(((got["lse"] - clean["lse"])[others].abs() <= 1e-4).all())
+    for name, row, n in (("weight", 0, 1), ("weight", 2, 33), ("prefix_weight", 0, prefix[0]), ("prefix_weight", 1, prefix[1])):
+        assert bool(torch.isnan(got[name][row, :n]).all()) and not got[name][row, n:].any(), (name, row)
+    b.q.copy_(q)
+    kv = b.kv.clone()
+    for row in (0, 3):                           # these rollouts' only tokens
+        ids, at = b.places(b.table, row, 1)
+        b.kv[1, 0, ids[0], at[0]] = nan
+    got = b.run(A, want_weight=True)
+    for name in ("out", "lse"):
+        assert bool(torch.isnan(got[name][[0, 3]]).all()), name
+        assert torch.equal(got[name][[1, 2]], clean[name][[1, 2]]), name
+    b.kv.copy_(kv)
+    ids, at = b.places(b.ptable, 1, prefix[1])   # a whole prefix
+    b.kv[1, 0, torch.from_numpy(ids).to(DEV), torch.from_numpy(at).to(DEV)] = nan
+    got = b.run(A, want_weight=True)
+    assert bool(torch.isnan(got["out"][2:]).all()) and bool(torch.isnan(got["lse"][2:]).all()) and torch.equal(got["out"][:2], clean["out"][:2])
