@@ -326,8 +326,8 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(Output to, int
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
     for (int s = 0; s < to.splits; ++s) {
         const f32x2 ml = *reinterpret_cast<const f32x2*>(to.part_ml + 2 * (s * rows + at));
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;        // nothing seen.  (All scores NaN: the maximum is -inf as well, the sums are NaN.)
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        if (f == 0.f) continue;
         sum += f * ml.y;
         if (e < hd) {
             const f32x4* p = reinterpret_cast<const f32x4*>(to.part_o + (s * rows + at) * hd + e);

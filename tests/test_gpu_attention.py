@@ -357,3 +357,29 @@ def test_empty_batches(A):
     out, lse = A.arrol_attention(q, k, k, torch.zeros(1, dtype=torch.int64, device=DEV))        # no sequences
     torch.cuda.synchronize()
     assert not out.any() and bool(torch.all(lse == -float("inf")))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,nk,H,KV,hd,one", [([60], [2500], 2, 1, 128, (512, 832)), ([20, 3], [5000, 2000], 4, 2, 64, (768, 1152))])      # one: keys of one range
+def test_nan_is_not_lost_between_ranges(A, nq, nk, H, KV, hd, one, causal):
+    """A query, or the keys of a range, whose scores are all NaN: no number comes out, with the keys in ranges as without."""
+    print("[case] attention in ranges, NaN, nq=%s nk=%s causal=%d" % (nq, nk, causal), flush=True)
+    q, k, v, _, cu_q, cu_k = make(nq, nk, H, KV, hd, 64)
+    assert A.lib().arrol_attention_workspace_bytes(q.shape[0], k.shape[0], len(nq), H, hd) > 0
+    val, tol = reference(q, k, v, cu_q, cu_k, causal, hd ** -0.5)
+    x, y = q.clone(), k.clone()
+    x[5], x[7, 1] = float("nan"), float("nan")
+    y[one[0]:one[1]] = float("nan")
+    for workspace in ("auto", None):
+        out, lse = A.arrol_attention(x, k, v, cu_q, cu_k, causal=causal, workspace=workspace)
+        torch.cuda.synchronize()
+        spoiled = torch.zeros(q.shape[0], H, dtype=torch.bool)
+        spoiled[5], spoiled[7, 1] = True, True
+        assert torch.equal(torch.isnan(out).all(2).cpu(), spoiled) and torch.equal(torch.isnan(lse).t().cpu(), spoiled), workspace
+        good = ~spoiled.numpy()
+        agree("out", out[~spoiled.to(DEV)], val["out"][good], tol["out"][good])
+        agree("lse", lse.t()[~spoiled.to(DEV)], val["lse"].T[good], tol["lse"].T[good])
+        out, lse = A.arrol_attention(q, y, v, cu_q, cu_k, causal=causal, workspace=workspace)
+        torch.cuda.synchronize()
+        assert bool(torch.isnan(out[:nq[0]]).all()) and bool(torch.isnan(lse[:, :nq[0]]).all()), workspace
+        agree("out", out[nq[0]:], val["out"][nq[0]:], tol["out"][nq[0]:])
