@@ -80,8 +80,8 @@ struct Output {
 };
 
 // O of a wavefront's rows over the keys [from, to), once more and by themselves: key by key, so that a key takes no part in a row that does not see it.  Where
-// all rows see all keys, or V is finite, the matrix instructions give the same; but the product of a hidden key's weight, 0, and an
-// infinity or NaN of its value is NaN.  Only rows that hold such values come here.
+// all rows see all keys of whole tiles, or V is finite, the matrix instructions give the same; but the product of a hidden key's weight, 0, and an
+// infinity or NaN of its value is NaN, and so is that of a place past the last key, which holds this one's value once more.  Only rows that hold such values come here.
 template <int HD, class Block>
 __device__ __forceinline__ void repair_rows(const Problem& a, const Block& w, const bf16x8 (&qf)[HD / 16], int kvh, int from, int to, float base, int lane, f32x16 (&o)[HD / 32]) {
     const int half = lane >> 5;
@@ -276,8 +276,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
         tiles_ready();
     }
     l = half_sum(l);
-    // An output that is no number: is it from a value that some of the rows do not see?
-    const int hidden = w.sees_least > t_lo * BK ? w.sees_least : t_lo * BK, end = (t_lo + needed) * BK < w.nk ? (t_lo + needed) * BK : w.nk;
+    // An output that is no number: is it from a value that some of the rows do not see, or from the last key's, whose place in the last tile's end it has as
+    // well (Stream), with weights 0?
+    const int end = (t_lo + needed) * BK < w.nk ? (t_lo + needed) * BK : w.nk, least = end < (t_lo + needed) * BK && w.sees_least >= end ? end - 1 : w.sees_least;
+    const int hidden = least > t_lo * BK ? least : t_lo * BK;
     if (hidden < end) {
         float odd = 0.f;
 #pragma unroll

@@ -383,3 +383,23 @@ def test_nan_is_not_lost_between_ranges(A, nq, nk, H, KV, hd, one, causal):
         torch.cuda.synchronize()
         assert bool(torch.isnan(out[:nq[0]]).all()) and bool(torch.isnan(lse[:, :nq[0]]).all()), workspace
         agree("out", out[nq[0]:], val["out"][nq[0]:], tol["out"][nq[0]:])
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("nq,nk,causal", [([1], [70], True), ([40], [70], False), ([1, 9], [129, 33], True), ([33], [2601], False), ([3], [2], False)])
+@pytest.mark.parametrize("hd", [64, 72, 128])
+def test_an_infinite_value_gives_an_infinite_output(A, nq, nk, causal, hd, bad):
+    """Also where it is the last key's, which stands for the missing ones of a tile: their weight is 0, and 0 times infinity would be NaN."""
+    print("[case] attention, infinite values, nq=%s nk=%s causal=%d hd=%d" % (nq, nk, causal, hd), flush=True)
+    q, k, v, _, cu_q, cu_k = make(nq, nk, 4, 2, hd, 66)
+    val, tol = reference(q, k, v, cu_q, cu_k, causal, hd ** -0.5)
+    v[nk[0] - 1, 1, 3::5] = bad                                     # the first sequence's last key, second kv head
+    expect = np.zeros(val["out"].shape, bool)
+    expect[nq[0] - 1 if causal else 0:nq[0], 2:, 3::5] = True
+    for workspace in ("auto", None):
+        out, lse = A.arrol_attention(q, k, v, cu_q, cu_k, causal=causal, workspace=workspace)
+        torch.cuda.synchronize()
+        got = f64(out)
+        assert np.array_equal(np.isinf(got), expect) and np.all(got[expect] == bad), workspace
+        agree("out", out[torch.from_numpy(~expect).to(DEV)], val["out"][~expect], tol["out"][~expect])
+        agree("lse", lse, val["lse"], tol["lse"])
