@@ -136,9 +136,20 @@ struct Rows {
             l += e;
             w[i] = static_cast<__bf16>(e);      // weights in bf16 for the product with V, their sum l in fp32 of the unrounded ones
         }
-        if (there)
+        if (there == ~0u) {
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = mfma16(ValueTile<HD>::by_column(values, d, lane), w, o[d]);
+        } else if (there) {      // what lies in the places of tokens that do not exist is another one's value: infinity, it would be NaN with their weight of 0
+            u32x4 exists;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t two = there >> (16 * (i >> 1) + 4 * g + 2 * (i & 1));
+                exists[i] = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                o[d] = mfma16(__builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, ValueTile<HD>::by_column(values, d, lane)) & exists), w, o[d]);
+        }
     }
     __device__ __forceinline__ float sum() const {
         const auto add = [](float x, float y) { return x + y; };
@@ -147,7 +158,7 @@ struct Rows {
 };
 
 // Where a step's 32 tokens lie: page id of token t + lane % 32, and its place in the pool.  A token that does not exist (past the range, or a page id out of
-// range) takes the place of one of the step that does: its weight is 0, and that one's NaN would be in every sum anyway.  Of a step of none nothing is added.
+// range) takes the place of one of the step that does, so nothing else is read; its score and its value are put aside.  Of a step of none nothing is added.
 struct Places {
     const int32_t* table;
     int t1, page;

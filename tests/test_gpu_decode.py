@@ -349,3 +349,24 @@ def test_nan_reaches_the_rollout_that_sees_it(A, sizes, prefix, H, KV, hd):
     b.kv[1, 0, torch.from_numpy(ids).to(DEV), torch.from_numpy(at).to(DEV)] = nan
     got = b.run(A, want_weight=True)
     assert bool(torch.isnan(got["out"][2:]).all()) and bool(torch.isnan(got["lse"][2:]).all()) and torch.equal(got["out"][:2], clean["out"][:2])
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("sizes,prefix,H", [([2, 1], [33, 65], 4), ([2, 1], [1000, 545], 40)])
+def test_an_infinite_value_gives_an_infinite_output(A, sizes, prefix, H, hd, bad):
+    """Also where it is the one token whose place the missing ones of a step of 32 take: their weight is 0, and 0 times infinity would be NaN."""
+    print("[case] decode, infinite values, hd=%d heads=%d" % (hd, H), flush=True)
+    b = Batch(sizes, prefix, [1, 33, 40], H, 2, hd, 16, 63)
+    want = b.reference()["out"]
+    expect = np.zeros((3, H, hd), bool)
+    spoiled = [(b.table, 0, 1, 0, [0]), (b.table, 1, 33, 32, [1]), (b.ptable, 1, prefix[1], prefix[1] // 32 * 32, [2])]      # row, its length, token, who sees it
+    for table, row, n, token, seen_by in spoiled:
+        ids, at = b.places(table, row, n)
+        b.kv[1, 1, ids[token], at[token], 1, 3::5] = bad            # the second kv head's
+        for r in seen_by:
+            expect[r, H // 2:, 3::5] = True
+    got = b.run(A, want_weight=True)["out"].cpu().double().numpy()
+    assert np.array_equal(np.isinf(got), expect) and np.all(got[expect] == bad)
+    rest = ~expect
+    assert np.all(np.abs(got[rest] - want[0][rest]) <= want[1][rest])
