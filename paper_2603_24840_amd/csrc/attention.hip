@@ -155,12 +155,12 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
     const unsigned lds0 = lds_address(lds), row_at = T::row_base(lane), column_at = T::column_base(lane);
     const auto fetch_k = [&](int t) {
         if (t == whole) ks.point(static_cast<unsigned>(a.k_stride) * 2, keys - t * BK, a.hd, wave, lane);
-        ks.issue(kp, lds0 + (t & 1) * 2 * kTileBytes, wave);
+        ks.issue(kp, lds0 + (t & 1) * 2 * kTileBytes, a.hd, wave);
         kp += BK * a.k_stride;
     };
     const auto fetch_v = [&](int t) {
         if (t == whole) vs.point(static_cast<unsigned>(a.v_stride) * 2, keys - t * BK, a.hd, wave, lane);
-        vs.issue(vp, lds0 + ((t & 1) * 2 + 1) * kTileBytes, wave);
+        vs.issue(vp, lds0 + ((t & 1) * 2 + 1) * kTileBytes, a.hd, wave);
         vp += BK * a.v_stride;
     };
     const auto fetch_for = [&](int t) {           // what iteration t + 1 needs
@@ -220,6 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem 
                 for (int d = 0; d < HD / 32; ++d) o[d] = mfma32(T::by_column(columns, 2 * b + e, d, kTileBytes), p, o[d]);
             }
     };
+    clear_tiles<HD>(&lds[0][0][0], sizeof lds, a.hd);
     if (n_tiles > 0) {
         ks.point(static_cast<unsigned>(a.k_stride) * 2, BK, a.hd, wave, lane);
         vs.point(static_cast<unsigned>(a.v_stride) * 2, BK, a.hd, wave, lane);
@@ -458,8 +459,8 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
         }
         const int head = kvh * per + h;
         const unsigned to = lds0 + slot * kSlot;
-        qs.issue(uniform(a.q + (q_begin + i0) * a.q_stride + static_cast<int64_t>(head) * a.hd), to, wave);
-        gs.issue(uniform(go + (q_begin + i0) * go_stride + static_cast<int64_t>(head) * a.hd), to + kTileBytes, wave);
+        qs.issue(uniform(a.q + (q_begin + i0) * a.q_stride + static_cast<int64_t>(head) * a.hd), to, a.hd, wave);
+        gs.issue(uniform(go + (q_begin + i0) * go_stride + static_cast<int64_t>(head) * a.hd), to + kTileBytes, a.hd, wave);
         if (wave < 2) {       // 64 rows' statistics, 4 bytes a lane, one kind a wavefront
             const float* from_row = stats + (wave * a.heads + head) * a.pq.T + q_begin + i0 + (lane < valid ? lane : valid - 1);
             asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from_row), "s"(to + 2 * kTileBytes + wave * 256) : "memory");
@@ -508,6 +509,7 @@ __global__ __launch_bounds__(GROUPS * kThreads, GROUPS == 1 ? 3 : 1) void attent
         }
     };
     const int mine = (total - group + GROUPS - 1) / GROUPS;      // this group's tiles: group, group + GROUPS, ...
+    clear_tiles<HD>(lds, GROUPS * 2 * kSlot, a.hd);
     if (mine > 0) fetch(0);
     tiles_ready();
     for (int t = 0; t < (total + GROUPS - 1) / GROUPS; ++t) {
@@ -612,8 +614,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
     const auto fetch = [&](int t) {
         if (t == whole) point(keys - t * BK);
         const unsigned to = lds0 + (t & 1) * 2 * kTileBytes;
-        ks.issue(kp, to, wave);
-        vs.issue(vp, to + kTileBytes, wave);
+        ks.issue(kp, to, a.hd, wave);
+        vs.issue(vp, to + kTileBytes, a.hd, wave);
         kp += BK * a.k_stride;
         vp += BK * a.v_stride;
     };
@@ -645,6 +647,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_grad_q_kernel(Problem a
             for (int d = 0; d < HD / 32; ++d) gq[d] = mfma32(T::by_column(columns, e, d, 0), ds, gq[d]);
         }
     };
+    clear_tiles<HD>(&lds[0][0][0], sizeof lds, a.hd);
     if (n_tiles > 0) {
         point(BK);
         fetch(0);

@@ -72,31 +72,48 @@ __device__ __forceinline__ unsigned fresh(unsigned v) {
 __device__ __forceinline__ void stay_branch() { asm volatile(""); }
 
 // ROWS rows on their way from memory straight into the LDS (16 bytes a lane, no registers): an instruction fills 1,024 bytes of the tile in order, so
-// the lane that fills a position fetches the chunk that belongs there.  Rows past `valid` (>= 1) are the last valid row once more and
-// chunks past the head the head's last: what is made of them is masked, or multiplied by zeros of the other operand, or not
-// stored, and it is never more than that row's own NaN that goes along.  Addresses are a scalar base and 32-bit offsets in the lanes.
+// the lane that fills a position fetches the chunk that belongs there.  Rows past `valid` (>= 1) are the last valid row once more: what is made of them is masked, or
+// multiplied by zeros of the other operand, or not stored, and it is never more than that row's own NaN that goes along.  Chunks past the head
+// stay what they are, the zeros of clear_tiles: the other operand is 0 there, and 0 times an infinity of the head would be NaN in its products.
+// Addresses are a scalar base and 32-bit offsets in the lanes.
 template <int HD, int ROWS, int WAVES>
 struct Stream {
     static constexpr int kPer = ROWS * Tile<HD>::kRowBytes / 1024 / WAVES;      // instructions of a wavefront
     static_assert(kPer * 1024 * WAVES == ROWS * Tile<HD>::kRowBytes, "whole instructions");
+    static constexpr unsigned kNothing = ~0u;
     unsigned offset[kPer];
     __device__ __forceinline__ void point(unsigned stride_bytes, int valid, int hd, int wave, int lane) {
-        const int last = hd / 8 - 1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int r = (wave * kPer + i) * (64 / Tile<HD>::kChunks) + lane / Tile<HD>::kChunks;
             const int c = (lane % Tile<HD>::kChunks) ^ Tile<HD>::swizzle(r);
-            offset[i] = static_cast<unsigned>(r < valid ? r : valid - 1) * stride_bytes + static_cast<unsigned>(c < last ? c : last) * 16;
+            offset[i] = 8 * c < hd ? static_cast<unsigned>(r < valid ? r : valid - 1) * stride_bytes + static_cast<unsigned>(c) * 16 : kNothing;
         }
     }
-    __device__ __forceinline__ void issue(const uint16_t* base, unsigned lds, int wave) const {
+    __device__ __forceinline__ void issue(const uint16_t* base, unsigned lds, int hd, int wave) const {
+        if (hd == HD) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const unsigned to = lds + (wave * kPer + i) * 1024;
-            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset[i]), "s"(base), "s"(to) : "memory");
+            for (int i = 0; i < kPer; ++i) load(base, lds, i, wave);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (offset[i] != kNothing) load(base, lds, i, wave);
         }
+    }
+
+private:
+    __device__ __forceinline__ void load(const uint16_t* base, unsigned lds, int i, int wave) const {
+        const unsigned to = lds + (wave * kPer + i) * 1024;
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset[i]), "s"(base), "s"(to) : "memory");
     }
 };
+// Zeros where no load will write: before the first load of a head shorter than the tile's rows.
+template <int HD>
+__device__ __forceinline__ void clear_tiles(unsigned char* lds, int bytes, int hd) {
+    if (hd == HD) return;
+    for (int i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16) *reinterpret_cast<u32x4*>(lds + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+}
 
 __device__ __forceinline__ unsigned lds_address(const void* p) {
     return static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p));

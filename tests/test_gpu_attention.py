@@ -403,3 +403,27 @@ def test_an_infinite_value_gives_an_infinite_output(A, nq, nk, causal, hd, bad):
         assert np.array_equal(np.isinf(got), expect) and np.all(got[expect] == bad), workspace
         agree("out", out[torch.from_numpy(~expect).to(DEV)], val["out"][~expect], tol["out"][~expect])
         agree("lse", lse, val["lse"], tol["lse"])
+
+
+@pytest.mark.parametrize("hd", [8, 40, 64, 72, 120, 128])
+@pytest.mark.parametrize("nq,nk", [([40, 3], [150, 64]), ([30], [2600])])
+def test_a_key_of_minus_infinity_has_no_weight(A, nq, nk, hd):
+    """Its score is -inf, and nothing else: what a head is padded with counts 0 in the products."""
+    print("[case] attention, keys of -inf, hd=%d nk=%s" % (hd, nk), flush=True)
+    q, k, v, go, cu_q, cu_k = make(nq, nk, 4, 2, hd, 65)
+    q[:, :, hd - 1] = q[:, :, hd - 1].abs() + 0.5
+    hidden = [0, 37, nk[0] - 1]                                     # of the first sequence
+    rest = torch.tensor([j for j in range(k.shape[0]) if j not in hidden], device=DEV)
+    ends = cu([nk[0] - len(hidden)] + nk[1:])
+    val, tol = reference(q, k[rest], v[rest], cu_q, ends, False, hd ** -0.5, go)      # as if they were not there
+    k[hidden, :, hd - 1] = -float("inf")
+    for workspace in ("auto", None):
+        out, lse = A.arrol_attention(q, k, v, cu_q, cu_k, causal=False, workspace=workspace)
+        torch.cuda.synchronize()
+        agree("out", out, val["out"], tol["out"])
+        agree("lse", lse, val["lse"], tol["lse"])
+    grad = A.arrol_attention_grad(q, k, v, out, lse, go, cu_q, cu_k, causal=False)
+    torch.cuda.synchronize()
+    agree("dv", grad["grad_v"][rest], val["dv"], tol["dv"])         # (dq has 0 times infinity in it)
+    agree("dk", grad["grad_k"][rest], val["dk"], tol["dk"])
+    assert not grad["grad_v"][hidden].any() and not grad["grad_k"][hidden].any()
