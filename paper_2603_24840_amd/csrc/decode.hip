@@ -191,8 +191,10 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
     Rows<HD> rows;
     rows.load(a, kvh, first, end, lane);
     const int64_t token_stride = static_cast<int64_t>(a.kv_heads) * a.hd;
-    // chunks past the head are the head's last ones once more (Q is 0 there, and what V gives is not stored)
+    // Chunks past the head are read as the head's last ones once more, but stay the zeros of clear_tiles in the LDS: Q is 0 there, and 0 times an infinity of the
+    // head would be NaN in its score.
     const int last = a.hd / 8 - 1;
+    const bool in_head = lane % VT::kChunks <= last;
     const int64_t in_row = static_cast<int64_t>(kvh) * a.hd + (lane % VT::kChunks < last ? lane % VT::kChunks : last) * 8;
     const uint16_t *k = a.k + in_row, *v = a.v + in_row;
     Places at = {p.table + static_cast<int64_t>(row) * p.per_row, t1, a.page, a.n_pages, 0, 0};
@@ -205,6 +207,7 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
             vx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + row_at));
         }
     };
+    clear_tiles<HD>(&lds[0][0], kWaves * 2 * VT::kBytes, a.hd);
     constexpr int kStride = kWaves * kStep;
     int t = t0 + wave * kStep, id = -1;
     if (t < t1) {
@@ -215,12 +218,13 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
     for (; t < t1; t += kStride) {
         const uint32_t now = at.there;
         wave_lds_exchange();               // the reads of the last step are done
+        if (in_head)
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const int r = i * (64 / VT::kChunks) + lane / VT::kChunks, c = lane % VT::kChunks;
-            *reinterpret_cast<u32x4*>(tile + KeyTile<HD>::at(r, c)) = kx[i];
-            *reinterpret_cast<u32x4*>(tile + VT::kBytes + VT::at(r, c)) = vx[i];
-        }
+            for (int i = 0; i < VL; ++i) {
+                const int r = i * (64 / VT::kChunks) + lane / VT::kChunks, c = lane % VT::kChunks;
+                *reinterpret_cast<u32x4*>(tile + KeyTile<HD>::at(r, c)) = kx[i];
+                *reinterpret_cast<u32x4*>(tile + VT::kBytes + VT::at(r, c)) = vx[i];
+            }
         wave_lds_exchange();
         if (t + kStride < t1) {
             at.resolve(t + kStride, id, lane);
@@ -285,8 +289,10 @@ __device__ __forceinline__ void many_rows(const Decode& a, const Pages& p, int r
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
         const int r = (wave * VL + i) * (64 / VT::kChunks) + lane / VT::kChunks, c = lane % VT::kChunks, ck = c ^ KeyTile<HD>::swizzle(r), cv = c ^ VT::swizzle(r);
-        from_k[i] = (ck < last ? ck : last) * 8, from_v[i] = (cv < last ? cv : last) * 8;
+        from_k[i] = ck <= last ? ck * 8 : -1, from_v[i] = cv <= last ? cv * 8 : -1;        // -1: past the head, left as it is (as in few_rows).
+        // (An instruction has every chunk of its rows, so none of them goes out without a lane, and the waits count them all.)
     }
+    clear_tiles<HD>(lds, 4 * 2 * VT::kBytes, a.hd);
     for (int start = t0; start < t1; start += kPlaces) {
         const int count = t1 - start < kPlaces ? t1 - start : kPlaces, n = (count + kStep - 1) / kStep;
         __syncthreads();                                 // the last places and steps are read
@@ -305,8 +311,8 @@ __device__ __forceinline__ void many_rows(const Decode& a, const Pages& p, int r
                 const int64_t at = __shfl(place, (wave * VL + i) * (64 / VT::kChunks) + lane / VT::kChunks) * token_stride;
                 const uint16_t *key = k + at + from_k[i], *value = v + at + from_v[i];
                 const unsigned to = lds0 + (step & 3) * 2 * VT::kBytes + (wave * VL + i) * 1024;
-                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(key), "s"(to) : "memory");
-                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(value), "s"(to + VT::kBytes) : "memory");
+                if (a.hd == HD || from_k[i] >= 0) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(key), "s"(to) : "memory");
+                if (a.hd == HD || from_v[i] >= 0) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(value), "s"(to + VT::kBytes) : "memory");
             }
         };
         for (int i = 0; i < kAhead && i < n; ++i) issue(i);

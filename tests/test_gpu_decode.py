@@ -370,3 +370,20 @@ def test_an_infinite_value_gives_an_infinite_output(A, sizes, prefix, H, hd, bad
     assert np.array_equal(np.isinf(got), expect) and np.all(got[expect] == bad)
     rest = ~expect
     assert np.all(np.abs(got[rest] - want[0][rest]) <= want[1][rest])
+
+
+@pytest.mark.parametrize("hd", [8, 40, 64, 72, 120, 128])
+@pytest.mark.parametrize("sizes,prefix,H", [([2, 1], [50, 90], 4), ([2, 1], [700, 90], 40)])
+def test_a_key_of_minus_infinity_has_no_weight(A, sizes, prefix, H, hd):
+    """Its score is -inf, and nothing else: what a head is padded with counts 0 in the products."""
+    print("[case] decode, keys of -inf, hd=%d heads=%d" % (hd, H), flush=True)
+    b = Batch(sizes, prefix, [3, 40, 70], H, 2, hd, 16, 62)
+    b.q[:, :, hd - 1] = b.q[:, :, hd - 1].abs() + 0.5
+    for table, lens in ((b.table, b.lengths), (b.ptable, b.prefix)):
+        for row, n in enumerate(lens):
+            ids, at = b.places(table, row, n)
+            b.kv[1, 0, ids[-1], at[-1], :, hd - 1] = -float("inf")
+    got = b.run(A, want_weight=True)
+    b.lengths, b.prefix = [n - 1 for n in b.lengths], [n - 1 for n in b.prefix]      # as if the last tokens were not there
+    for name, (val, tol) in b.reference().items():
+        assert np.all(np.abs(got[name].cpu().double().numpy() - val) <= tol + 1e-30), name
