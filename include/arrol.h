@@ -517,6 +517,8 @@ int arrol_attention_grad(const void* q, int64_t q_stride, const void* k, int64_t
  *   The _out may be the _in.  Called for every layer with the same buffers they gather over the layers.
  * n_heads a multiple of layout.n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0;
  *   n_pages * page_tokens below 2^31; a table row's tokens (max_pages_per_* * page_tokens) below 2^31 - 4096; n_groups at most 2^20; with weights, fewer than 2^30 tokens in all rows of both tables together.
+ *   A launch has a workgroup per kv head, tile of 16 or 64 query rows and range of tokens (of up to 2,048 each, at most 128 of a table row); sizes that would
+ *   need 2^24 of them, or with more than 8 ranges of both kinds together have n * n_heads >= 2^24, are refused (ARROL_EINVAL), and their workspace is given as 0.
  * fp32 scores, sums and lse; the weights are rounded to bf16 for the product with v.  No atomics: bit-reproducible run to run.
  * workspace: arrol_decode_attention_workspace_bytes(...) bytes, 16-byte aligned (want_weight: 1 where weight_out or prefix_weight_out is given).
  */
@@ -540,7 +542,8 @@ int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads, const void
  *   weight_out[r][t] = weight of the token now in slot t, 0 for t >= n;
  *   position_out[r][t] = position[r][slot it came from] (position NULL: that slot itself), -1 for t >= n.
  * weight, weight_out fp32 and position (NULL allowed), position_out int32, all [n_rows, max_pages_per_seq * page_tokens].  Each _out may be its input.
- * A token on a page id outside [0, n_pages) is not copied.  n_kv_heads * head_dim a multiple of 8; n_first + n_recent <= budget.
+ * A token on a page id outside [0, n_pages) is not copied.  n_kv_heads * head_dim a multiple of 8; n_first + n_recent <= budget;
+ *   n_rows below 2^22 (from there on the workspace is given as 0); a table row's tokens at most 2^31 - 1025.
  * workspace: arrol_evict_workspace_bytes(...) bytes, 16-byte aligned.  n_rows == 0 is a no-op.
  */
 size_t arrol_evict_workspace_bytes(int32_t n_rows, int32_t max_pages_per_seq, int32_t page_tokens, int32_t budget);

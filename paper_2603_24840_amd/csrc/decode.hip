@@ -536,20 +536,36 @@ struct Plan {
     int own_chunk, own_splits, pre_chunk, pre_splits;
     int64_t own_cap, pre_cap;
     size_t ml, o, lse2, own_scores, pre_scores, total;
+    Tiles tiles;
+    int64_t blocks, join_blocks, own_weight_blocks, pre_weight_blocks;      // workgroups of the launches; of the weights', a row's
+    bool fits;                      // lanes of a launch are counted in 32 bits
 };
+constexpr int64_t kMostBlocks = (int64_t{1} << 32) / kThreads;
 
 // Query rows that a workgroup takes where a rollout's heads, or an average group, has `rows` of them and up to `tokens` tokens to read: 64 where 16
 // would leave the same tokens to several, but not so few of them that four wavefronts side by side are done sooner (8 rollouts of 32 heads over 8 behind
 // 200 tokens: 9.3 us, with 64 rows 10.3).
 int rows_of(int64_t rows, int64_t tokens) { return rows > 16 && tokens > 512 ? 64 : 16; }
+// Wavefronts that share a row's ranges in the join.
+int join_waves(int slots) { return slots > 8 ? 4 : 1; }
 
 Plan plan(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_pages, int64_t pre_pages, int64_t n_groups, bool weights) {
     Plan p{};
     const int64_t own = own_pages * page, pre = n_groups > 0 ? pre_pages * page : 0;
-    const int64_t per = heads / kv_heads, own_rows = rows_of(per, own), pre_rows = n_groups > 0 ? rows_of(n * per / n_groups, pre) : 16;
-    const int64_t blocks = n * kv_heads * ((per + own_rows - 1) / own_rows) + (pre > 0 ? (n * per / pre_rows + n_groups) * kv_heads : 0);
+    const int64_t per = heads / kv_heads;
+    Tiles& w = p.tiles;
+    w.own_rows = rows_of(per, own), w.own_tiles = static_cast<int>((per + w.own_rows - 1) / w.own_rows);
+    w.prefix_rows = n_groups > 0 ? rows_of(n * per / n_groups, pre) : 16;
+    const int64_t blocks = n * kv_heads * w.own_tiles + (pre > 0 ? (n * per / w.prefix_rows + n_groups) * kv_heads : 0);
     cut(own, blocks, p.own_chunk, p.own_splits);
     cut(pre, blocks, p.pre_chunk, p.pre_splits);
+    w.prefix_tiles = tile_bound(n * per, static_cast<int>(n_groups), w.prefix_rows);
+    w.prefix_blocks = w.prefix_tiles * p.pre_splits * kv_heads;
+    p.blocks = n > 0 ? w.prefix_blocks + n * w.own_tiles * p.own_splits * kv_heads : 0;
+    p.join_blocks = join_waves(p.own_splits + p.pre_splits) > 1 ? n * heads : (n * heads + kWaves - 1) / kWaves;
+    p.own_weight_blocks = (own + 256 * kWaves - 1) / (256 * kWaves), p.pre_weight_blocks = (pre + 255) / 256;
+    p.fits = p.blocks < kMostBlocks && p.join_blocks < kMostBlocks &&
+             (!weights || (n * own + n_groups * pre < int64_t{1} << 30 && n * p.own_weight_blocks + n_groups * p.pre_weight_blocks < kMostBlocks));
     p.own_cap = ((own + kStep - 1) / kStep | 1) * kStep, p.pre_cap = ((pre + kStep - 1) / kStep | 1) * kStep;      // odd, so that rows begin on all channels
     const size_t rows = static_cast<size_t>(n) * heads, slots = p.own_splits + p.pre_splits;
     size_t at = 0;
@@ -568,22 +584,15 @@ Plan plan(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_page
 }
 
 bool shape_ok(int64_t n, int heads, int kv_heads, int hd, int page, int64_t own_pages, int64_t pre_pages, int64_t n_groups) {
-    if (n < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || hd < 8 || hd > 128 || hd % 8 || page < 1 || own_pages < 1 || n_groups < 0) return false;
+    if (n < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || hd < 8 || hd > 128 || hd % 8 || page < 1 || own_pages < 1 || n_groups < 0 || n_groups > (1 << 20)) return false;
     if (n_groups > 0 && pre_pages < 1) return false;
     const int64_t most = 0x7fffffff - kPastTheEnd;
     return own_pages <= most / page && (n_groups == 0 || pre_pages <= most / page) && n <= most / heads;
 }
 
 template <int HD, bool SCORES>
-void launch(const Decode& a, hipStream_t st) {
-    const int64_t per = a.heads / a.kv_heads;
-    Tiles w;
-    w.own_rows = rows_of(per, static_cast<int64_t>(a.own.per_row) * a.page), w.own_tiles = static_cast<int>((per + w.own_rows - 1) / w.own_rows);
-    w.prefix_rows = a.groups.n > 0 ? rows_of(a.n * per / a.groups.n, static_cast<int64_t>(a.pre.per_row) * a.page) : 16;
-    w.prefix_tiles = tile_bound(a.n * per, a.groups.n, w.prefix_rows);
-    w.prefix_blocks = w.prefix_tiles * a.pre.splits * a.kv_heads;
-    const int64_t own = static_cast<int64_t>(a.n) * w.own_tiles * a.own.splits * a.kv_heads;
-    arrol_launch(decode_kernel<HD, SCORES>, dim3(static_cast<unsigned>(w.prefix_blocks + own)), dim3(kThreads), 0, st, a, w);
+void launch(const Decode& a, const Plan& p, hipStream_t st) {
+    arrol_launch(decode_kernel<HD, SCORES>, dim3(static_cast<unsigned>(p.blocks)), dim3(kThreads), 0, st, a, p.tiles);
 }
 
 }  // namespace
@@ -591,7 +600,8 @@ void launch(const Decode& a, hipStream_t st) {
 extern "C" size_t arrol_decode_attention_workspace_bytes(int32_t n, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_tokens,
                                                          int32_t max_pages_per_seq, int32_t max_pages_per_prefix, int32_t n_groups, int32_t want_weight) {
     if (n == 0 || !shape_ok(n, n_heads, n_kv_heads, head_dim, page_tokens, max_pages_per_seq, max_pages_per_prefix, n_groups)) return 0;
-    return plan(n, n_heads, n_kv_heads, head_dim, page_tokens, max_pages_per_seq, max_pages_per_prefix, n_groups, want_weight != 0).total;
+    const Plan p = plan(n, n_heads, n_kv_heads, head_dim, page_tokens, max_pages_per_seq, max_pages_per_prefix, n_groups, want_weight != 0);
+    return p.fits ? p.total : 0;
 }
 
 extern "C" int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads, const void* kv, arrol_kv_layout layout, int32_t layer,
@@ -605,11 +615,11 @@ extern "C" int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads,
     if (n == 0 && n_groups == 0) return ARROL_OK;
     const bool weights = weight_out || prefix_weight_out;
     if ((!weight_out && weight_in) || (!prefix_weight_out && prefix_weight_in) || (n_groups == 0 && prefix_weight_out)) return ARROL_EINVAL;
-    if (n_groups > 0 && (!prefix_table || !prefix_len || !group_offsets || n_groups > (1 << 20))) return ARROL_EINVAL;
+    if (n_groups > 0 && (!prefix_table || !prefix_len || !group_offsets)) return ARROL_EINVAL;
     if (n > 0 && (!q || !out || !block_table || !seq_len || !arrol_aligned16(q) || !arrol_aligned16(out))) return ARROL_EINVAL;
     if (layout.n_pages > 0 && (!kv || !arrol_aligned16(kv))) return ARROL_EINVAL;
-    if (weights && (static_cast<int64_t>(n) * max_pages_per_seq + static_cast<int64_t>(n_groups) * max_pages_per_prefix) * layout.page_tokens >= int64_t{1} << 30) return ARROL_EINVAL;
     const Plan p = plan(n, n_heads, layout.n_kv_heads, layout.head_dim, layout.page_tokens, max_pages_per_seq, max_pages_per_prefix, n_groups, weights);
+    if (!p.fits) return ARROL_EINVAL;
     if (n > 0 && (!workspace || !arrol_aligned16(workspace) || workspace_bytes < p.total)) return ARROL_EWORKSPACE;
     auto* ws = static_cast<unsigned char*>(workspace);
     Decode a;
@@ -625,22 +635,19 @@ extern "C" int arrol_decode_attention(const void* q, int32_t n, int32_t n_heads,
              static_cast<int>(p.pre_cap)};
     a.own = {block_table, seq_len, max_pages_per_seq, p.own_chunk, p.own_splits, p.pre_splits, weights ? reinterpret_cast<float*>(ws + p.own_scores) : nullptr,
              static_cast<int>(p.own_cap)};
-    const int64_t tiles = 2 * static_cast<int64_t>(n) * (n_heads / a.kv_heads + 15) / 16 + n + n_groups + 2;      // of query rows, at most
-    if (tiles * (a.slots + 1) * a.kv_heads >= (1 << 24)) return ARROL_EINVAL;      // lanes of a launch are counted in 32 bits
     const auto st = static_cast<hipStream_t>(stream);
     if (n > 0) {
-        if (a.hd <= 64) weights ? launch<64, true>(a, st) : launch<64, false>(a, st);
-        else weights ? launch<128, true>(a, st) : launch<128, false>(a, st);
-        const int64_t rows = static_cast<int64_t>(n) * n_heads;
+        if (a.hd <= 64) weights ? launch<64, true>(a, p, st) : launch<64, false>(a, p, st);
+        else weights ? launch<128, true>(a, p, st) : launch<128, false>(a, p, st);
         auto* o = static_cast<uint16_t*>(out);
-        if (a.slots > 8) arrol_launch(decode_join_kernel<4>, dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, st, a, o, lse_out);
-        else arrol_launch(decode_join_kernel<1>, dim3(static_cast<unsigned>((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, st, a, o, lse_out);
+        const dim3 grid(static_cast<unsigned>(p.join_blocks));
+        if (join_waves(a.slots) > 1) arrol_launch(decode_join_kernel<4>, grid, dim3(kThreads), 0, st, a, o, lse_out);
+        else arrol_launch(decode_join_kernel<1>, grid, dim3(kThreads), 0, st, a, o, lse_out);
     }
     if (weights) {
-        const auto blocks = [&](int64_t pages, int64_t tokens) { return (pages * a.page + tokens - 1) / tokens; };
-        Weights w = {{weight_in, prefix_weight_in}, {weight_out, prefix_weight_out}, {weight_out ? n : 0, prefix_weight_out ? n_groups : 0}, 0, 0, 0};
-        w.own_blocks = blocks(max_pages_per_seq, 256 * kWaves), w.own_total = w.own_blocks * w.rows[0];
-        w.pre_blocks = w.rows[1] ? blocks(max_pages_per_prefix, 256) : 1;
+        Weights w = {{weight_in, prefix_weight_in}, {weight_out, prefix_weight_out}, {weight_out ? n : 0, prefix_weight_out ? n_groups : 0}, p.own_weight_blocks, 0, 1};
+        w.own_total = w.own_blocks * w.rows[0];
+        if (w.rows[1]) w.pre_blocks = p.pre_weight_blocks;
         const int64_t total = w.own_total + w.pre_blocks * w.rows[1];
         if (total > 0) arrol_launch(decode_weight_kernel, dim3(static_cast<unsigned>(total)), dim3(kThreads), 0, st, a, w);
     }

@@ -200,7 +200,7 @@ int64_t most_moves(int64_t cap, int64_t budget) { return cap <= budget ? 0 : cap
 size_t workspace(int64_t rows, int64_t most) { return up(rows * most * sizeof(Move)) + 2 * up(rows * most * 4) + up(rows * 4); }
 
 bool shape_ok(int64_t rows, int64_t per_row, int64_t page, int64_t budget) {
-    return rows >= 0 && per_row >= 1 && page >= 1 && budget >= 0 && per_row <= 0x7fffffff / page - kPlanThreads;
+    return rows >= 0 && rows < (1 << 22) && per_row >= 1 && page >= 1 && budget >= 0 && per_row <= (0x7fffffff - kPlanThreads) / page;
 }
 
 }  // namespace
@@ -217,7 +217,7 @@ extern "C" int arrol_evict(void* kv, arrol_kv_layout layout, const int32_t* bloc
     if (!shape_ok(n_rows, max_pages_per_seq, layout.page_tokens, budget) || layout.n_layers < 1 || layout.n_layers > (1 << 24) || layout.n_kv_heads < 1 || layout.head_dim < 1 || layout.n_pages < 0) return ARROL_EINVAL;
     if (token_bytes % 16 || token_bytes > (1 << 24) || n_first < 0 || n_recent < 0 || static_cast<int64_t>(n_first) + n_recent > budget) return ARROL_EINVAL;
     if (n_rows == 0) return ARROL_OK;
-    if (!block_table || !seq_len || !weight || !block_table_out || !seq_len_out || !weight_out || !position_out || n_rows >= (1 << 22)) return ARROL_EINVAL;
+    if (!block_table || !seq_len || !weight || !block_table_out || !seq_len_out || !weight_out || !position_out) return ARROL_EINVAL;
     if (layout.n_pages > 0 && (!kv || !arrol_aligned16(kv))) return ARROL_EINVAL;
     const int64_t cap = static_cast<int64_t>(max_pages_per_seq) * layout.page_tokens, most = most_moves(cap, budget);
     if (!workspace_ || !arrol_aligned16(workspace_) || workspace_bytes < workspace(n_rows, most)) return ARROL_EWORKSPACE;

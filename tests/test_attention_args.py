@@ -149,3 +149,29 @@ def test_attention_gradient_counts_a_launchs_lanes(L):
     """Workgroups of 512 lanes with heads of more than 64: 2^23 of them are 2^32 lanes."""
     for hd, n, rc in ((128, 2 ** 22 - 3, -2), (128, 2 ** 22 - 2, -1), (72, 2 ** 23 - 3, -1), (64, 2 ** 22 - 2, -2), (64, 2 ** 23 - 3, -2), (64, 2 ** 23 - 2, -1)):
         assert grad(L, ws=None, n=n, H=2, KV=2, hd=hd, ks=256, vs=256) == rc, (hd, n)
+
+
+def test_decode_refuses_what_its_launches_cannot_hold_and_nothing_else(L):
+    """Both sides of the limits on workgroups: of the main launch, of the join where there are more than 8 ranges, of the weights' tokens."""
+    import paper_2603_24840_amd as A
+    size = L.arrol_decode_attention_workspace_bytes
+
+    def takes(n, H, KV, own_pages, pre_pages=0, groups=0, weights=0):
+        need = size(n, H, KV, 64, 16, own_pages, pre_pages, groups, weights)
+        rc = decode(L, lay=A.KVLayout(1, 16, KV, 64, 128), layer=0, n=n, H=H, width=own_pages, pw=pre_pages, groups=groups, ws=None, wout=FAKE if weights else None)
+        assert rc == (-2 if need else -1), (n, H, KV, own_pages, rc, need)       # what has a workspace lacks nothing but that
+        return need > 0
+
+    assert takes(2048, 32, 32, 8192, 8192, 256)                     # tables of 131,072 tokens: 5 million workgroups
+    assert takes(2 ** 24 - 1, 1, 1, 1) and not takes(2 ** 24, 1, 1, 1)                       # a workgroup a rollout
+    assert takes(2 ** 20 - 1, 16, 1, 1152) and not takes(2 ** 20, 16, 1, 1152)               # 9 ranges of 2,048 tokens, a workgroup of the join a query row
+    assert takes(2 ** 26 - 1, 1, 1, 1, weights=0) is False
+    assert takes(2 ** 16 - 1, 1, 1, 1024, weights=1) and not takes(2 ** 16, 1, 1, 1024, weights=1)      # 2^30 tokens
+    assert takes(8, 4, 2, 4, 3, 2 ** 20) and not takes(8, 4, 2, 4, 3, 2 ** 20 + 1)
+
+
+def test_evict_workspace_of_what_is_refused_is_0(L):
+    size = L.arrol_evict_workspace_bytes
+    assert size(2 ** 22 - 1, 4, 16, 32) > 0 and size(2 ** 22, 4, 16, 32) == 0 and evict(L, rows=2 ** 22 - 1, ws=None) == -2 and evict(L, rows=2 ** 22, ws=None) == -1
+    assert size(1, 2 ** 31 - 1025, 1, 32) > 0 and size(1, 2 ** 31 - 1024, 1, 32) == 0
+    assert size(1, 2 ** 27 - 65, 16, 32) > 0 and size(1, 2 ** 27 - 64, 16, 32) == 0
