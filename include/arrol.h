@@ -394,9 +394,9 @@ int arrol_score_grad(const void* hidden, int64_t row_stride_elems, const int64_t
  * loss_out NULL or fp32 [1]; grad_w1 fp32 [m, d]; grad_b1, grad_w2 fp32 [m]; grad_b2 NULL or fp32 [1].
  * delta is rounded to bf16 before the contraction over the rollouts (bf16 products, fp32 accumulation);
  * everything else is fp32; sums in a fixed order (bit-reproducible run to run).
- * delta_terms: 1 = delta as one bf16 value (relative rounding 2^-9 per term of dL/dW1); 2 = delta as the sum
+ * delta_terms: 1 = delta as one bf16 value (relative rounding of up to 2^-8 per term of dL/dW1); 2 = delta as the sum
  * of two bf16 values, hi = bf16(delta) and lo = bf16(delta - hi), both contracted (relative
- * rounding 2^-17: dL/dW1 to fp32 accuracy, at twice the cost of that contraction).  Other values -> ARROL_EINVAL.
+ * rounding of up to 2^-16: dL/dW1 to fp32 accuracy, at twice the cost of that contraction).  Other values -> ARROL_EINVAL.
  * n_rows == 0 writes zeros.
  * workspace: arrol_score_mlp_grad_workspace_bytes(n_rows, d, m, delta_terms) bytes, 256-byte aligned,
  * caller-owned, contents undefined afterwards; too small or NULL -> ARROL_EWORKSPACE.  The size never falls as n_rows
@@ -470,11 +470,13 @@ int arrol_probe_mfma_rate(const void* a_bf16, int64_t n_a, const void* b_bf16, i
  *   fused projection need no copy.  Strides multiples of 8, at least heads*head_dim and at most 2^24, bases 16-byte aligned.
  * cu_seqlens_k NULL: the same as the queries' (and T_k == T_q).   n_heads a multiple of n_kv_heads; head_dim a multiple of 8, 8 .. 128; scale > 0.
  * out bf16 [T_q, n_heads, head_dim];  lse_out NULL or fp32 [n_heads, T_q].
- * bf16 products, fp32 accumulation, maximum, sum and lse; the weights are rounded to bf16 for the product with v (2^-9 each).
+ * bf16 products, fp32 accumulation, maximum, sum and lse; the weights are rounded to bf16 for the product with v (by up to 2^-8 each; their sum
+ * is of the unrounded ones).
  * T_q == 0 is a no-op.  (T / 128 + n_seq + 2) * n_heads has to stay below 2^24, else ARROL_EINVAL.
  * workspace: optional.  Given the queried size (16-byte aligned; the query returns 0 where this does not apply) the keys of a sequence are cut into ranges
  * where few queries read many keys, and the ranges joined in a fixed order by a second launch; without it one workgroup walks over all of them.
- * The results differ by fp32 rounding of the joining only.
+ * Every range rounds its weights relative to its own maximum, so the two results differ by roundings of weights to bf16, as either does from the exact one. Whether
+ * and into how many ranges keys are cut depends on the whole batch's sizes: given the workspace, a row's last bits may depend on what it is batched with.
  */
 size_t arrol_attention_workspace_bytes(int64_t T_q, int64_t T_k, int32_t n_seq, int32_t n_heads, int32_t head_dim);
 int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -488,8 +490,8 @@ int arrol_attention(const void* q, int64_t q_stride, const void* k, int64_t k_st
  *   dv_j = sum_i p_ij do_i,  dk_j = scale sum_i ds_ij q_i (sums over all query heads of the kv head),  dq_i = scale sum_j ds_ij k_j
  * grad_q bf16 [T_q, n_heads, head_dim], grad_k and grad_v bf16 [T_k, n_kv_heads, head_dim], each rounded once from fp32 sums (p and ds are
  * rounded to bf16 for their products).  No atomics: bit-reproducible run to run.  Rows of no sequence get zeros.
- * Other sequences' rows take no part, whatever they hold; a NaN or infinity of a row, though, may reach the gradients of the 32 rows around it in
- * its own sequence, whether or not they see it.
+ * Other sequences' rows take no part, whatever they hold. Within a sequence products are made of 32 queries and 32 keys at a time, so a NaN or infinity of a row
+ * may also reach gradients of up to 62 rows beyond those that see it: a query's the keys that follow its last visible one, a key's the queries before its first.
  * Sizes as above; with head_dim > 64 also (T_k / 128 + n_seq + 2) * n_kv_heads below 2^23.
  * workspace: arrol_attention_grad_workspace_bytes(...) bytes of the same sizes, 16-byte aligned.
  */

@@ -427,3 +427,29 @@ def test_a_key_of_minus_infinity_has_no_weight(A, nq, nk, hd):
     agree("dv", grad["grad_v"][rest], val["dv"], tol["dv"])         # (dq has 0 times infinity in it)
     agree("dk", grad["grad_k"][rest], val["dk"], tol["dk"])
     assert not grad["grad_v"][hidden].any() and not grad["grad_k"][hidden].any()
+
+
+@pytest.mark.parametrize("more", [0, 1, 31, 32, 40])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_how_far_nan_reaches_in_the_gradients_of_a_sequence(A, more, hd):
+    """Products are made of 32 queries and 32 keys at a time: a NaN may reach rows that do not see it, up to 62 beyond those that do, and no others."""
+    print("[case] attention gradient, reach of NaN, nk - nq = %d, hd=%d" % (more, hd), flush=True)
+    n = 300
+    q, k, v, go, cu_q, cu_k = make([n], [n + more], 2, 1, hd, 69)
+    for at in (0, 31, 32, 150, 191, n - 1):
+        x, y = go.clone(), k.clone()
+        x[at] = float("nan")                                    # query `at` sees the keys up to at + more
+        out, lse = A.arrol_attention(q, k, v, cu_q, cu_k)
+        grad = A.arrol_attention_grad(q, k, v, out, lse, x, cu_q, cu_k)
+        y[at + more] = float("nan")                             # seen by the queries from `at` on
+        out, lse = A.arrol_attention(q, y, v, cu_q, cu_k)
+        other = A.arrol_attention_grad(q, y, v, out, lse, go, cu_q, cu_k)
+        torch.cuda.synchronize()
+        odd = lambda t: torch.isnan(t).flatten(1).any(1).cpu().numpy()
+        assert np.array_equal(odd(grad["grad_q"]), np.arange(n) == at)
+        for name in ("grad_k", "grad_v"):
+            got = odd(grad[name])
+            assert got[:at + more + 1].all() and not got[at + more + 63:].any(), (name, at)
+        got = odd(other["grad_q"])
+        assert got[at:].all() and not got[:max(0, at - 62)].any(), at
+        assert not np.isnan(f64(out)[:at]).any()
