@@ -453,3 +453,33 @@ def test_how_far_nan_reaches_in_the_gradients_of_a_sequence(A, more, hd):
         got = odd(other["grad_q"])
         assert got[at:].all() and not got[:max(0, at - 62)].any(), at
         assert not np.isnan(f64(out)[:at]).any()
+
+
+def test_gradient_along_itself_agrees_with_differences(A):
+    """The step is the 64-bit gradient, normalised, so the derivative along it is that gradient's norm: central differences in 64 bits (h = 1e-4) give that to
+    1e-6, and the kernel's gradient lies, in norm, within its elements' tolerances.  A gradient of zeros, half of it or its negative is further off than those."""
+    print("[case] attention gradient along itself", flush=True)
+    q, k, v, go, cu_q, cu_k = make([40, 33], [70, 50], 4, 2, 64, 12)
+    out, lse = A.arrol_attention(q, k, v, cu_q, cu_k)
+    grad = A.arrol_attention_grad(q, k, v, out, lse, go, cu_q, cu_k)
+    torch.cuda.synchronize()
+    along_itself({name: f64(x) for name, x in grad.items()}, q, k, v, go, cu_q, cu_k)
+
+
+def along_itself(grad, q, k, v, go, cu_q, cu_k):
+    val, tol = reference(q, k, v, cu_q, cu_k, True, 0.125, go)
+    loss = lambda *x: float(np.sum(f64(go) * reference(*x, cu_q, cu_k, True, 0.125)[0]["out"]))
+    base = [t.double().cpu() for t in (q, k, v)]
+    for which, name, short in ((0, "grad_q", "dq"), (1, "grad_k", "dk"), (2, "grad_v", "dv")):
+        norm = float(np.linalg.norm(val[short]))
+        step = torch.from_numpy(val[short] / norm)
+        side = []
+        for sign in (1, -1):
+            x = list(base)
+            x[which] = base[which] + sign * 1e-4 * step
+            side.append(loss(*x))
+        assert abs((side[0] - side[1]) / 2e-4 - norm) <= 1e-6 * norm, name
+        allowed = float(np.linalg.norm(tol[short]))
+        assert np.linalg.norm(grad[name] - val[short]) <= allowed, name
+        for wrong in (0.0, 0.5, -1.0):
+            assert np.linalg.norm(wrong * val[short] - val[short]) > allowed, (name, wrong)
