@@ -483,3 +483,30 @@ def along_itself(grad, q, k, v, go, cu_q, cu_k):
         assert np.linalg.norm(grad[name] - val[short]) <= allowed, name
         for wrong in (0.0, 0.5, -1.0):
             assert np.linalg.norm(wrong * val[short] - val[short]) > allowed, (name, wrong)
+
+
+@pytest.mark.parametrize("H,KV,hd,T", [(4, 2, 64, 300), (2, 1, 128, 900)])
+def test_bad_offsets_leave_what_lies_around_the_buffers(A, H, KV, hd, T):
+    """Every output and both workspaces inside larger allocations whose other bytes stay as they were."""
+    print("[case] attention and its gradient, bad offsets, guarded buffers, T=%d" % T, flush=True)
+    q, k, v, go, _, _ = make([T], None, H, KV, hd, 2)
+    L, pad, mark = A.lib(), 4096, 0x5A
+
+    def inside(nbytes):
+        whole = torch.full((pad + nbytes + pad,), mark, dtype=torch.uint8, device=DEV)
+        return whole, whole[pad:pad + nbytes]
+
+    for bad in ([-5, 100, 10 ** 12], [T, 200, 0], [0, -2 ** 62, 2 ** 62, 17], [2 ** 62, -1], [0, T + 1], [T // 2, T // 2, 10 ** 9, 3]):
+        offsets = torch.tensor(bad, dtype=torch.int64, device=DEV)
+        n = len(bad) - 1
+        need = L.arrol_attention_workspace_bytes(T, T, n, H, hd), L.arrol_attention_grad_workspace_bytes(T, T, n, H, KV, hd)
+        buffers = [inside(x) for x in (T * H * hd * 2, H * T * 4, need[0], T * H * hd * 2, T * KV * hd * 2, T * KV * hd * 2, need[1])]
+        out, lse, ws, gq, gk, gv, gws = (x.data_ptr() if x.numel() else None for _, x in buffers)
+        st = torch.cuda.current_stream().cuda_stream
+        ends = (offsets.data_ptr(), None, T, T, n, H, KV, hd, 1, 0.125)
+        rows = (q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0))
+        assert L.arrol_attention(*rows, *ends, out, lse, ws, need[0], st) == 0
+        assert L.arrol_attention_grad(*rows, out, lse, go.data_ptr(), *ends, gq, gk, gv, gws, need[1], st) == 0
+        torch.cuda.synchronize()
+        for whole, part in buffers:
+            assert bool((whole[:pad] == mark).all()) and bool((whole[pad + part.numel():] == mark).all()), bad
