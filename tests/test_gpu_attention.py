@@ -510,3 +510,28 @@ def test_bad_offsets_leave_what_lies_around_the_buffers(A, H, KV, hd, T):
         torch.cuda.synchronize()
         for whole, part in buffers:
             assert bool((whole[:pad] == mark).all()) and bool((whole[pad + part.numel():] == mark).all()), bad
+
+
+def test_batches_past_2_31_elements(A):
+    """Rows whose offsets into a fused projection, the output and the gradients pass 2^31 elements (2^32 bytes): the last sequences as if they were alone."""
+    print("[case] attention, 6.5e9 elements of a projection", flush=True)
+    H, hd, short = 64, 128, [64, 33, 70]
+    q, k, v, go, cu_q, _ = make(short, None, H, H, hd, 67)
+    want, want_lse = A.arrol_attention(q, k, v, cu_q, workspace=None)
+    grads = A.arrol_attention_grad(q, k, v, want, want_lse, go, cu_q)
+    n = 4150
+    lengths = [64] * n + short
+    T, last = sum(lengths), sum(short)
+    qkv = torch.zeros(T, 3 * H, hd, dtype=torch.bfloat16, device=DEV)
+    many = qkv[:, :H], qkv[:, H:2 * H], qkv[:, 2 * H:]
+    for x, y in zip(many, (q, k, v)):
+        x[T - last:] = y
+    many_go = torch.zeros(T, H, hd, dtype=torch.bfloat16, device=DEV)
+    many_go[T - last:] = go
+    assert T * H * hd > 2 ** 31
+    out, lse = A.arrol_attention(*many, cu(lengths))
+    got = A.arrol_attention_grad(*many, out, lse, many_go, cu(lengths))
+    torch.cuda.synchronize()
+    assert torch.equal(out[T - last:], want) and torch.equal(lse[:, T - last:], want_lse) and not out[:T - last].any()
+    for name in got:
+        assert torch.equal(got[name][T - last:], grads[name]) and not got[name][:T - last].any(), name
