@@ -387,3 +387,10 @@ def test_a_key_of_minus_infinity_has_no_weight(A, sizes, prefix, H, hd):
     b.lengths, b.prefix = [n - 1 for n in b.lengths], [n - 1 for n in b.prefix]      # as if the last tokens were not there
     for name, (val, tol) in b.reference().items():
         assert np.all(np.abs(got[name].cpu().double().numpy() - val) <= tol + 1e-30), name
+
+
+@pytest.mark.parametrize("H,KV,hd", [(8, 2, 64), (40, 2, 128)])
+def test_tables_much_wider_than_their_rows(A, H, KV, hd):
+    """Ranges are cut from what a table could hold; a row takes part in as many as its length reaches."""
+    print("[case] decode, tables of 40,000 tokens, heads=%d/%d" % (H, KV), flush=True)
+    Batch([3, 2], [700, 33], [1, 500, 64, 2500, 129], H, KV, hd, 16, 68, spare=2500).check(A, want_weight=True)
