@@ -744,6 +744,14 @@ def _heads(t, name):
     return t.stride(0) if rows > 1 else max(h * hd, t.stride(0) // 8 * 8)
 
 
+def _int32(x, name):
+    """ctypes would pass the lower 32 bits on: a budget of 2**32 would be one of 0."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError("%s does not fit 32 bits" % name)
+    return x
+
+
 def _packed_args(q, k, v, cu_seqlens, cu_seqlens_k, causal, scale):
     strides = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     if k.shape != v.shape or k.shape[2] != q.shape[2]:
@@ -844,7 +852,7 @@ def _py_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None, 
     if q.dim() != 3 or block_table.dim() != 2 or block_table.shape[0] != q.shape[0] or seq_len.numel() != q.shape[0]:
         raise ValueError("q must be [n, n_heads, head_dim], block_table [n, pages], seq_len [n]")
     n, H, hd = q.shape
-    lay = kv_layout_of(kv)
+    lay, layer = kv_layout_of(kv), _int32(layer, "layer")
     if lay.head_dim != hd:
         raise ValueError("q and the KV pool disagree on head_dim")
     given = [x is not None for x in (prefix_table, prefix_len, group_offsets)]
@@ -872,7 +880,7 @@ def _py_decode_attention(q, kv, layer, block_table, seq_len, prefix_table=None, 
     out = torch.empty((n, H, hd), dtype=torch.bfloat16, device=dev)
     lse = torch.empty((n, H), dtype=torch.float32, device=dev)
     rc = lib().arrol_decode_attention(
-        _ptr(q, torch.bfloat16, "q"), n, H, _ptr(kv, torch.bfloat16, "kv"), lay, int(layer), _ptr(block_table, torch.int32, "block_table"),
+        _ptr(q, torch.bfloat16, "q"), n, H, _ptr(kv, torch.bfloat16, "kv"), lay, layer, _ptr(block_table, torch.int32, "block_table"),
         _ptr(seq_len, torch.int32, "seq_len"), width, _ptr(prefix_table if groups else None, torch.int32, "prefix_table"),
         _ptr(prefix_len if groups else None, torch.int32, "prefix_len"), prefix_width, _ptr(group_offsets if groups else None, torch.int64, "group_offsets"),
         groups, float(hd ** -0.5 if scale is None else scale), out.data_ptr(), lse.data_ptr(), _ptr(weight, torch.float32, "weight"),
@@ -898,6 +906,7 @@ def arrol_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0,
 def _py_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, position=None, out=None, workspace=None, stream=None):
     if block_table.dim() != 2 or seq_len.numel() != block_table.shape[0]:
         raise ValueError("block_table must be [rows, pages], seq_len [rows]")
+    budget, n_first, n_recent = _int32(budget, "budget"), _int32(n_first, "n_first"), _int32(n_recent, "n_recent")
     rows, width = block_table.shape
     lay, dev = kv_layout_of(kv), kv.device
     shape = (rows, width * lay.page_tokens)
@@ -909,9 +918,9 @@ def _py_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, p
     elif out["block_table"].shape != (rows, width) or out["seq_len"].numel() != rows or out["weight"].shape != shape or out["position"].shape != shape:
         raise ValueError("the outputs must have the shapes of their inputs")
     if workspace is None:
-        workspace = torch.empty(max(lib().arrol_evict_workspace_bytes(rows, width, lay.page_tokens, int(budget)), 16), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(lib().arrol_evict_workspace_bytes(rows, width, lay.page_tokens, budget), 16), dtype=torch.uint8, device=dev)
     rc = lib().arrol_evict(_ptr(kv, torch.bfloat16, "kv"), lay, _ptr(block_table, torch.int32, "block_table"), _ptr(seq_len, torch.int32, "seq_len"), rows, width,
-                           _ptr(weight, torch.float32, "weight"), _ptr(position, torch.int32, "position"), int(budget), int(n_first), int(n_recent),
+                           _ptr(weight, torch.float32, "weight"), _ptr(position, torch.int32, "position"), budget, n_first, n_recent,
                            _ptr(out["block_table"], torch.int32, "block_table"), _ptr(out["seq_len"], torch.int32, "seq_len"),
                            _ptr(out["weight"], torch.float32, "weight"), _ptr(out["position"], torch.int32, "position"),
                            _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))

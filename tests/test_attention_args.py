@@ -175,3 +175,19 @@ def test_evict_workspace_of_what_is_refused_is_0(L):
     assert size(2 ** 22 - 1, 4, 16, 32) > 0 and size(2 ** 22, 4, 16, 32) == 0 and evict(L, rows=2 ** 22 - 1, ws=None) == -2 and evict(L, rows=2 ** 22, ws=None) == -1
     assert size(1, 2 ** 31 - 1025, 1, 32) > 0 and size(1, 2 ** 31 - 1024, 1, 32) == 0
     assert size(1, 2 ** 27 - 65, 16, 32) > 0 and size(1, 2 ** 27 - 64, 16, 32) == 0
+
+
+def test_binding_refuses_integers_of_more_than_32_bits():
+    """ctypes passes the lower 32 bits on: without a look at them these would run with 0 or 1."""
+    import paper_2603_24840_amd as A
+    q, kv = torch.zeros(4, 4, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 4, 16, 2, 64, dtype=torch.bfloat16)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for big in (2 ** 32, 2 ** 32 + 1, 2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError, match="32 bits"):
+            A.arrol_evict(kv, i32(4, 1), i32(4), torch.zeros(4, 16), big)
+        with pytest.raises(ValueError, match="32 bits"):
+            A.arrol_evict(kv, i32(4, 1), i32(4), torch.zeros(4, 16), 8, n_first=big)
+        with pytest.raises(ValueError, match="32 bits"):
+            A.arrol_evict(kv, i32(4, 1), i32(4), torch.zeros(4, 16), 8, n_recent=big)
+        with pytest.raises(ValueError, match="32 bits"):
+            A.arrol_decode_attention(q, kv, big, i32(4, 1), i32(4))
