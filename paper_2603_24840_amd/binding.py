@@ -741,7 +741,7 @@ def _heads(t, name):
     rows, h, hd = t.shape
     if (hd > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != hd):
         raise ValueError("%s: the heads of a row must be contiguous" % name)
-    return t.stride(0) if rows > 1 else max(h * hd, t.stride(0) // 8 * 8)
+    return t.stride(0) if rows > 1 else h * hd      # a single row's stride leads nowhere
 
 
 def _int32(x, name):

@@ -472,7 +472,7 @@ struct Heads {
         const int64_t h = t.size(1), d = t.size(2);
         if (a.refuse((d > 1 && t.stride(2) != 1) || (h > 1 && t.stride(1) != d) || h > INT32_MAX || d > INT32_MAX)) return;
         n = t.size(0), heads = static_cast<int32_t>(h), hd = static_cast<int32_t>(d);
-        stride = n > 1 ? t.stride(0) : (h * d > t.stride(0) / 8 * 8 ? h * d : t.stride(0) / 8 * 8);
+        stride = n > 1 ? t.stride(0) : h * d;
     }
 };
 

@@ -97,3 +97,19 @@ def test_native_marshalling_leaves_cpu_tensors_to_python():
     for name, cases in calls("cpu").items():
         with pytest.raises((TypeError, ValueError)):
             getattr(A, "arrol_" + name)(*cases[0][0], **cases[0][1])
+
+
+@pytest.mark.gpu
+def test_the_stride_of_a_single_row_does_not_matter():
+    """A view of one row of something large: there is no second row that its stride leads to."""
+    print("[case] marshal, one row of any stride", flush=True)
+    c = calls(DEV)
+    q, k, v = (x[:1].contiguous() for x in c["attention"][0][0][:3])
+    cu, far = torch.tensor([0, 1], device=DEV), lambda x: x.as_strided(x.shape, (2 ** 25 + 4, x.shape[2], 1))
+    want = A.arrol_attention(q, k, v, cu)
+    go = q.flip(2).contiguous()
+    want_grad = A.arrol_attention_grad(q, k, v, *want, go, cu)
+    for got in (A.arrol_attention(far(q), far(k), far(v), cu), binding._py_attention(far(q), far(k), far(v), cu)):
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    for got in (A.arrol_attention_grad(far(q), far(k), far(v), *want, go, cu), binding._py_attention_grad(far(q), far(k), far(v), *want, go, cu)):
+        assert all(torch.equal(got[x], want_grad[x]) for x in got)
