@@ -692,10 +692,6 @@ Problem problem(const void* q, int64_t q_stride, const void* k, int64_t k_stride
     return a;
 }
 
-
-}  // namespace
-
-namespace {
 // Heads of a kv head that a workgroup takes.
 int heads_together(int per) { return per % 4 == 0 ? 4 : per % 2 == 0 ? 2 : 1; }
 int64_t query_tiles(int64_t T, int n_seq, int per) { return tile_bound(T, n_seq, kOwn / heads_together(per)); }
