@@ -33,7 +33,7 @@ __device__ __forceinline__ int clamp32(int64_t n) { return uniform(static_cast<i
 
 // Where a workgroup's queries lie, and which keys they see.  Its four wavefronts have 32 rows each: 32 rows of HEADS = 4 heads of a kv head, 64 of 2, or
 // 128 of one - as many heads as share it, so that few rows (short or ragged sequences) fill the workgroup, and its wavefronts see the same keys: 64 prompts
-// of up to 512 tokens, 32 heads over 8, 69 us, with one head a workgroup 79.
+// of up to 512 tokens, 32 heads over 8, 70 us, with one head a workgroup 77.
 template <int HEADS>
 struct QueryBlock {
     static constexpr int kRows = kOwn / HEADS;
@@ -118,8 +118,8 @@ __device__ __forceinline__ void repair_rows(const Problem& a, const Block& w, co
 // Forward pass: a workgroup walks over the keys in tiles of 64, a wavefront with 32 queries of a head.
 // S^T = K Q^T and O^T += V^T P^T, so that a query's statistics are its lane's.  The tiles that come next are on their way into the other halves of the
 // LDS.  With heads of 128, whose registers leave two wavefronts to a SIMD, the scores of the next tile are formed while the exponentials of this one
-// are (K runs a tile ahead of V): 4 survivors of up to 4,096 tokens, 32 heads over 8, 298 us against 355.  With heads of 64 four fit, which
-// do that for each other: 64 prompts of up to 512 tokens 83 us, and 108 the other way.
+// are (K runs a tile ahead of V): 4 survivors of up to 4,096 tokens, 32 heads over 8, 297 us against 331.  With heads of 64 four fit, which
+// do that for each other: 64 prompts of up to 512 tokens 70 us, and 84 the other way.
 template <int HD, int HEADS>
 __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(Problem a, int64_t tiles, Output to) {
     constexpr int BK = 64;
@@ -389,8 +389,8 @@ __global__ __launch_bounds__(kThreads) void attention_grad_join_kernel(const flo
 // of the keys (K and V as fragments in registers); the sum over the shared heads is made in registers, in a fixed order.
 // With heads of 128, whose registers leave two wavefronts to a SIMD, these are two groups of four of one workgroup: each takes every other tile (with its own
 // part of the LDS), and their sums are added at the end.  That halves the longest walk - the first keys of a long sequence, all heads - which
-// bounds the launch where there are few sequences: 4 survivors of up to 4,096 tokens, 32 heads over 8, 1,268 us for the whole gradient with one group and
-// 1,069 with two.  With heads of 64 three workgroups of one group fit: 16 survivors of up to 1,000 tokens 206 us, and 218 with two groups.
+// bounds the launch where there are few sequences: 4 survivors of up to 4,096 tokens, 32 heads over 8, 1,130 us for the whole gradient with one group and
+// 1,030 with two.  With heads of 64 three workgroups of one group fit: 16 survivors of up to 1,000 tokens 199.6 us, and 203 with two groups.
 // S = Q K^T and dP = dO V^T have the own key as column and start from -lse / scale and -D of their rows, so that z / scale - lse / scale and
 // dp - D come out of the matrix cores (a row that sees nothing has lse = -inf, and is masked everywhere); dV^T += dO^T P, dK^T += Q^T dS.
 template <int HD, int GROUPS>

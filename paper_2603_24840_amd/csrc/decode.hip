@@ -265,8 +265,8 @@ __device__ __forceinline__ void few_rows(const Decode& a, const Pages& p, int ro
 
 // A workgroup with up to 64 query rows, 16 a wavefront: keys and values of 32 tokens are read once for all of them, straight into the LDS, three such steps ahead of
 // the one that is worked on.  The tokens' places are looked up for up to kPlaces at a time, so that no load stands between those: the wait for it would be a
-// wait for all of them.  4 prompts of 9,000 to 16,384 tokens, 16 rollouts of 32 heads over 8 each: 96 us, of which the loads alone are 54 and the products alone
-// 66 (one workgroup to a compute unit: they overlap little); with the scores stored 134.
+// wait for all of them.  4 prompts of 9,000 to 16,384 tokens, 16 rollouts of 32 heads over 8 each: the launch takes 112 us, without the products 72
+// and without the loads 82 (one workgroup to a compute unit: they overlap little); with the scores stored 123.
 constexpr int kPlaces = 2048, kAhead = 3;
 template <int N>
 __device__ __forceinline__ void steps_ready() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
@@ -519,7 +519,7 @@ constexpr int kPastTheEnd = 4096;
 static_assert(kPastTheEnd >= kPlaces + kStep && kPastTheEnd >= 3 * kWaves * kStep, "tokens are counted in 32 bits");
 
 // Ranges of a row of `cap` tokens where `blocks` workgroups (of both kinds) would take whole rows: as many as give 2,048 workgroups, of at most
-// 2,048 tokens (384 rollouts of up to 2,000 tokens: 355 us a call, in ranges of 1,024 403).
+// 2,048 tokens (384 rollouts of up to 2,000 tokens: 356 us a call, in ranges of 1,024 404).
 void cut(int64_t cap, int64_t blocks, int& chunk, int& splits) {
     int64_t want = blocks <= 0 ? 1 : (2048 + blocks - 1) / blocks, c = (cap + want - 1) / want;
     if (c > kMaxRange) c = kMaxRange;
@@ -544,7 +544,7 @@ constexpr int64_t kMostBlocks = (int64_t{1} << 32) / kThreads;
 
 // Query rows that a workgroup takes where a rollout's heads, or an average group, has `rows` of them and up to `tokens` tokens to read: 64 where 16
 // would leave the same tokens to several, but not so few of them that four wavefronts side by side are done sooner (8 rollouts of 32 heads over 8 behind
-// 200 tokens: 9.3 us, with 64 rows 10.3).
+// 200 tokens: 9.2 us, with 64 rows 10.9).
 int rows_of(int64_t rows, int64_t tokens) { return rows > 16 && tokens > 512 ? 64 : 16; }
 // Wavefronts that share a row's ranges in the join.
 int join_waves(int slots) { return slots > 8 ? 4 : 1; }

@@ -50,8 +50,8 @@ __device__ __forceinline__ int rank_in_block(bool flag, int* totals, int& total)
     return before + __popcll(votes & ((uint64_t{1} << lane) - 1));
 }
 
-// THREADS: 256 for rows of up to 512 tokens, whose barriers are the time (32 rows of 64: 9.2 us a call, with 1,024 threads 9.9), 1,024 for longer ones
-// (128 rows of 1,024: 224 us, with 256 threads 226).
+// THREADS: 256 for rows of up to 512 tokens, whose barriers are the time (32 rows of 64: 9.0 us a call, with 1,024 threads 9.5), 1,024 for longer ones
+// (128 rows of 1,024: 225 us, with 256 threads 227.5).
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_plan_kernel(Evict a) {
     constexpr int kWaves = THREADS / ARROL_WAVE;
