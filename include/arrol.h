@@ -21,6 +21,8 @@
  *   arrol_attention, arrol_attention_grad                      attention over packed sequences (prompts, survivors) and its gradient
  *   arrol_decode_attention                                     one token per rollout over the paged pool, a group's prompt read once
  *   arrol_evict                                                rollouts' caches cut to a budget of tokens by their attention weight
+ *   arrol_rotary, arrol_rotary_frequencies                     queries and keys of packed rows turned by their positions, and back
+ *   arrol_append                                               new tokens' keys and values into the paged pool, turned on the way
  *
  * Conventions common to every call
  *   - Every data pointer is a DEVICE pointer owned by the caller (the library never
@@ -553,6 +555,47 @@ int arrol_evict(void* kv, arrol_kv_layout layout, const int32_t* block_table, co
                 int32_t max_pages_per_seq, const float* weight, const int32_t* position, int32_t budget, int32_t n_first,
                 int32_t n_recent, int32_t* block_table_out, int32_t* seq_len_out, float* weight_out, int32_t* position_out,
                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Between a model's projections and the attention calls: positions, and new tokens into the pool -----------------------------------
+ * Queries and keys of packed rows turned by their positions.  Of every head the first rotary_dim elements are pairs (x, y): elements i and
+ * i + rotary_dim/2, or with interleaved != 0 elements 2i and 2i + 1 (i < rotary_dim/2); with a = position[t] * inv_freq[i]
+ *   x' = magnitude (x cos a - y sin a),  y' = magnitude (x sin a + y cos a);  inverse != 0: by -a, which makes the gradient of q and k out of that of q' and k'
+ * and the elements from rotary_dim on are handed on as they are.
+ * q bf16, row t of head h at q + t*q_stride + h*head_dim (elements), as in arrol_attention; k likewise with n_kv_heads, or NULL with n_kv_heads == 0 (and
+ *   k_out NULL).  The outputs have strides of their own; each may be its input (same base and stride), and otherwise overlaps nothing.
+ * position int32 [T], of any sign and size; inv_freq fp64 [rotary_dim/2], radians a position.  Angles are formed in 64 bits, the rest in 32, results rounded once.
+ * head_dim a multiple of 8, 8 .. 256; rotary_dim even, 2 .. head_dim; strides multiples of 8, at least heads*head_dim and at most 2^24; bases 16-byte
+ *   aligned; T below 2^25.  T == 0 is a no-op.
+ */
+int arrol_rotary(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const int32_t* position, const double* inv_freq,
+                 int64_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t rotary_dim, int32_t interleaved,
+                 int32_t inverse, float magnitude, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+/*
+ * A host computation on a HOST array: inv_freq[i] = f (s + (1 - s)/factor), f = base^(-2i/rotary_dim), i < rotary_dim/2.  With original_context C a pair
+ * turns C f / 2 pi times in it: those that turn `high` times or more keep their frequency (s = 1), those that turn `low` times or less have it divided by
+ * factor (s = 0), between them s rises linearly.  original_context 0 and high > 0: all are divided.  factor 1: none.
+ * rotary_dim even, 2 .. 256; base, factor > 0; original_context >= 0; low <= high; all finite, else ARROL_EINVAL.
+ */
+int arrol_rotary_frequencies(int32_t rotary_dim, double base, double factor, double original_context, double low, double high,
+                             double* inv_freq);
+/*
+ * New tokens into one layer of the paged pool (layout and block tables as in arrol_decode_attention), their keys - and queries, where given - turned on the way.
+ * Row t is token j of sequence s: cu_seqlens NULL: s = t and j = 0, one token a row of the table (T == n_seq); otherwise int64 [n_seq+1], ascending, clamped into
+ * [0, T], s the sequence with cu_seqlens[s] <= t < cu_seqlens[s+1] and j = t - cu_seqlens[s].  Its slot is start[s] + j, that is token slot % page_tokens of
+ * page block_table[s][slot / page_tokens]; k' and v are written there, k' and q' being arrol_rotary's of k and q by position[t] (NULL: by the slot).
+ * k, v bf16 with n_kv_heads heads and strides as in arrol_rotary; q NULL (n_heads == 0, q_out NULL) or n_heads heads of head_dim; q_out as there; k_out NULL or where
+ *   k' goes besides (the attention over packed rows reads it there).  inv_freq NULL: nothing is turned, and rotary_dim and position have no meaning.
+ * start int32 [n_seq]; position int32 [T]; block_table int32 [n_seq, max_pages_per_seq].
+ * Nothing else of the pool is touched.  A token whose slot is negative or past its table's row, or on a page id outside [0, n_pages), is not written; of two
+ * tokens with one slot either may stay.  A row of no sequence is not written to the pool, and its q_out and k_out rows are its q and k as they are.
+ * Sizes as in arrol_rotary; n_pages * page_tokens below 2^31.  T == 0 is a no-op.
+ */
+int arrol_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                 const int64_t* cu_seqlens, const int32_t* start, const int32_t* position, const double* inv_freq, int64_t T,
+                 int32_t n_seq, int32_t n_heads, int32_t rotary_dim, int32_t interleaved, float magnitude, void* kv,
+                 arrol_kv_layout layout, int32_t layer, const int32_t* block_table, int32_t max_pages_per_seq, void* q_out,
+                 int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
 
 #ifdef __cplusplus
 }

@@ -104,6 +104,10 @@ _SIGNATURES = {
     "arrol_evict_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32]),
     "arrol_evict": (ctypes.c_int, [_vp, KVLayout, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz,
                                    _vp]),
+    "arrol_rotary": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _f32, _vp, _i64, _vp, _i64, _vp]),
+    "arrol_rotary_frequencies": (ctypes.c_int, [_i32] + [ctypes.c_double] * 5 + [_vp]),
+    "arrol_append": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _f32, _vp, KVLayout, _i32, _vp, _i32,
+                                    _vp, _i64, _vp, _i64, _vp]),
     "arrol_probe_mfma_rate": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp, _vp]),
 }
 
@@ -139,7 +143,7 @@ class _NoMarshal:
         return None
 
 
-MARSHAL_INTERFACE = 3    # of setup() and the calls and argument lists of marshal.cpp; 1 was without a number
+MARSHAL_INTERFACE = 4    # of setup() and the calls and argument lists of marshal.cpp; 1 was without a number
 
 
 def built_for():
@@ -926,6 +930,98 @@ def _py_evict(kv, block_table, seq_len, weight, budget, n_first=0, n_recent=0, p
                            _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
     _check("arrol_evict", rc)
     return out
+
+
+def _out_rows(out, like, name):
+    """An output of rotated heads: a given one, whose rows may be strided as the input's may, or a new one."""
+    if out is None:
+        out = torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
+    elif out.shape != like.shape:
+        raise ValueError("%s must have the shape of its input" % name)
+    return out, _heads(out, name)
+
+
+def arrol_rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, original_context=0, low=1.0, high=4.0, device="cuda"):
+    """Radians a position of every pair, fp64 [rotary_dim/2] on `device`: base^(-2i/rotary_dim), divided by `factor` for a longer context - in full for pairs that turn at
+    most `low` times in the original context, not at all for those that turn `high` times or more, in part between them (original_context 0: all in full)."""
+    rotary_dim = _int32(rotary_dim, "rotary_dim")
+    host = (ctypes.c_double * max(rotary_dim // 2, 1))()
+    rc = lib().arrol_rotary_frequencies(rotary_dim, float(base), float(factor), float(original_context), float(low), float(high), host)
+    _check("arrol_rotary_frequencies", rc)
+    return torch.tensor(list(host), dtype=torch.float64, device=device)
+
+
+def arrol_rotary(q, k, position, inv_freq, interleaved=False, inverse=False, magnitude=1.0, out_q=None, out_k=None, *, stream=None):
+    """Queries and keys turned by their positions: q bf16 [T, n_heads, head_dim], k bf16 [T, n_kv_heads, head_dim] or None (rows may be strided), position
+    int32 [T], inv_freq fp64 [rotary_dim/2].  Pairs are elements i and i + rotary_dim/2 or, interleaved, 2i and 2i + 1.  inverse turns back: from the gradients of the
+    results to those of q and k.  out_q and out_k (None: new) may be q and k.  -> (q, k) turned; k None without one."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).rotary(q, k, position, inv_freq, interleaved, inverse, magnitude, out_q, out_k)
+        if result is not None:
+            return result
+        return _py_rotary.__wrapped__(q, k, position, inv_freq, interleaved, inverse, magnitude, out_q, out_k)
+    return _py_rotary(q, k, position, inv_freq, interleaved, inverse, magnitude, out_q, out_k, stream=stream)
+
+
+@_on_stream
+def _py_rotary(q, k, position, inv_freq, interleaved=False, inverse=False, magnitude=1.0, out_q=None, out_k=None, stream=None):
+    strides = _heads(q, "q"), (0 if k is None else _heads(k, "k"))
+    if k is not None and (k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]):
+        raise ValueError("k must have the rows and the head_dim of q")
+    if k is None and out_k is not None:
+        raise ValueError("out_k is given without k")
+    if position.numel() != q.shape[0]:
+        raise ValueError("position must be [T]")
+    out_q, q_out_stride = _out_rows(out_q, q, "out_q")
+    out_k, k_out_stride = (None, 0) if k is None else _out_rows(out_k, k, "out_k")
+    rc = lib().arrol_rotary(q.data_ptr(), strides[0], None if k is None else k.data_ptr(), strides[1], _ptr(position, torch.int32, "position"),
+                            _ptr(inv_freq, torch.float64, "inv_freq"), q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], 2 * inv_freq.numel(),
+                            int(bool(interleaved)), int(bool(inverse)), float(magnitude), out_q.data_ptr(), q_out_stride,
+                            None if k is None else out_k.data_ptr(), k_out_stride, _stream(stream))
+    _check("arrol_rotary", rc)
+    return out_q, out_k
+
+
+def arrol_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, position=None, inv_freq=None, interleaved=False, magnitude=1.0, want_k=False,
+                 out_q=None, out_k=None, *, stream=None):
+    """New tokens into one layer of the paged pool (kv is modified in place): k, v bf16 [T, n_kv_heads, head_dim] (rows may be strided), block_table int32 [n, pages],
+    start int32 [n] the slot of every row's first new token.  One token a row, or with cu_seqlens int64 [n+1] packed sequences.  With inv_freq fp64 [rotary_dim/2] keys and
+    queries q bf16 [T, n_heads, head_dim] (None: none) are turned as by arrol_rotary, by position int32 [T] (None: the slots).  want_k: the turned keys
+    as packed rows too.  out_q and out_k (None: new) may be q and k.  -> dict(q, k), None where there is none."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).append(k, v, kv, layer, block_table, start, cu_seqlens, q, position, inv_freq, interleaved, magnitude, want_k, out_q, out_k)
+        if result is not None:
+            return result
+        return _py_append.__wrapped__(k, v, kv, layer, block_table, start, cu_seqlens, q, position, inv_freq, interleaved, magnitude, want_k, out_q, out_k)
+    return _py_append(k, v, kv, layer, block_table, start, cu_seqlens, q, position, inv_freq, interleaved, magnitude, want_k, out_q, out_k, stream=stream)
+
+
+@_on_stream
+def _py_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, position=None, inv_freq=None, interleaved=False, magnitude=1.0, want_k=False,
+               out_q=None, out_k=None, stream=None):
+    strides = _heads(k, "k"), _heads(v, "v"), (0 if q is None else _heads(q, "q"))
+    lay, layer = kv_layout_of(kv), _int32(layer, "layer")
+    if k.shape != v.shape or k.shape[1:] != (lay.n_kv_heads, lay.head_dim):
+        raise ValueError("k and v must be [T, n_kv_heads, head_dim] with the pool's heads")
+    if q is not None and (q.shape[0] != k.shape[0] or q.shape[2] != lay.head_dim):
+        raise ValueError("q must have the rows and the head_dim of k")
+    if (q is None and out_q is not None) or (not want_k and out_k is not None):
+        raise ValueError("out_q is given without q, or out_k while turned keys are not wanted")
+    n, T = start.numel(), k.shape[0]
+    if block_table.dim() != 2 or block_table.shape[0] != n or (n != T if cu_seqlens is None else cu_seqlens.numel() != n + 1):
+        raise ValueError("block_table must be [n, pages], start [n], cu_seqlens [n+1]; without cu_seqlens there is a row of k for each")
+    if position is not None and position.numel() != T:
+        raise ValueError("position must be [T]")
+    out_q, q_out_stride = (None, 0) if q is None else _out_rows(out_q, q, "out_q")
+    out_k, k_out_stride = (None, 0) if not want_k else _out_rows(out_k, k, "out_k")
+    rc = lib().arrol_append(k.data_ptr(), strides[0], v.data_ptr(), strides[1], None if q is None else q.data_ptr(), strides[2],
+                            _ptr(cu_seqlens, torch.int64, "cu_seqlens"), _ptr(start, torch.int32, "start"), _ptr(position, torch.int32, "position"),
+                            _ptr(inv_freq, torch.float64, "inv_freq"), T, n, 0 if q is None else q.shape[1], 0 if inv_freq is None else 2 * inv_freq.numel(),
+                            int(bool(interleaved)), float(magnitude), _ptr(kv, torch.bfloat16, "kv"), lay, layer, _ptr(block_table, torch.int32, "block_table"),
+                            block_table.shape[1], None if q is None else out_q.data_ptr(), q_out_stride, None if out_k is None else out_k.data_ptr(), k_out_stride,
+                            _stream(stream))
+    _check("arrol_append", rc)
+    return dict(q=out_q, k=out_k)
 
 
 @_on_stream

@@ -658,6 +658,93 @@ PyObject* evict(Args& a) {
     return d;
 }
 
+// Heads that are written: a given tensor of the shape of `like`, or a new one, which is contiguous.
+struct HeadsOut {
+    at::Tensor own;
+    void* p = nullptr;
+    int64_t stride = 0;
+    bool wanted = false;
+    HeadsOut(Args& a, int i, const Heads& like, bool want) {
+        if (a.odd || a.refuse(!want && a.given(i))) return;
+        if (a.given(i)) {
+            const Heads h(a, i);
+            if (a.odd || a.refuse(h.t.sizes() != like.t.sizes())) return;
+            p = data(h.t), stride = h.stride;
+        } else {
+            wanted = want;
+            stride = static_cast<int64_t>(like.heads) * like.hd;
+        }
+    }
+    void get(const Heads& like) {            // without the interpreter lock
+        if (wanted) p = made(own, like.t.sizes(), at::kBFloat16, like.t);
+    }
+    PyObject* object(Args& a, int i) { return own.defined() ? wrap(std::move(own)) : keep(a[i]); }     // the given one, or None
+};
+
+// q, k, position, inv_freq, interleaved, inverse, magnitude, out_q, out_k
+PyObject* rotary(Args& a) {
+    const Heads q(a, 0);
+    const bool keys = a.given(1);
+    const Heads k(a, keys ? 1 : 0);
+    if (a.odd || a.refuse(k.n != q.n || k.hd != q.hd)) return nullptr;
+    const int32_t* position = a.ptr<int32_t>(2, at::kInt, q.n);
+    const at::Tensor& f = a.tensor(3, at::kDouble);
+    const bool interleaved = a.truth(4), inverse = a.truth(5);
+    const float magnitude = static_cast<float>(a.number(6));
+    if (a.odd || a.refuse(!position || f.numel() > 1024)) return nullptr;
+    HeadsOut oq(a, 7, q, true), ok(a, 8, k, keys);
+    if (a.odd) return nullptr;
+    void* st = stream(a, q.t);
+    if (a.odd) return nullptr;
+    if (failed("arrol_rotary", launch([&] {
+            oq.get(q);
+            ok.get(k);
+            return arrol_rotary(data(q.t), q.stride, keys ? data(k.t) : nullptr, keys ? k.stride : 0, position, static_cast<const double*>(data(f)), q.n, q.heads,
+                                keys ? k.heads : 0, q.hd, static_cast<int32_t>(2 * f.numel()), interleaved, inverse, magnitude, oq.p, oq.stride, ok.p, ok.stride, st);
+        })))
+        return nullptr;
+    return tuple(oq.object(a, 7), ok.object(a, 8));
+}
+
+// k, v, kv, layer, block_table, start, cu_seqlens, q, position, inv_freq, interleaved, magnitude, want_k, out_q, out_k
+PyObject* append(Args& a) {
+    const Heads k(a, 0), v(a, 1);
+    const Pool kv(a, 2);
+    const int32_t layer = a.integer(3);
+    const Table t(a, 4, 5);
+    if (a.odd || a.refuse(k.t.sizes() != v.t.sizes() || k.heads != kv.layout.n_kv_heads || k.hd != kv.layout.head_dim)) return nullptr;
+    if (a.refuse(!a.given(6) && k.n != t.rows)) return nullptr;
+    const int64_t* cu = a.ptr<int64_t>(6, at::kLong, t.rows + int64_t{1});
+    const bool queries = a.given(7), turned = a.given(9);
+    const Heads q(a, queries ? 7 : 0);
+    if (a.odd || a.refuse(q.n != k.n || q.hd != k.hd)) return nullptr;
+    const int32_t* position = a.ptr<int32_t>(8, at::kInt, k.n);
+    const double* f = a.ptr<double>(9, at::kDouble);
+    const bool interleaved = a.truth(10), want = a.truth(12);
+    const float magnitude = static_cast<float>(a.number(11));
+    if (a.odd) return nullptr;
+    const int64_t pairs = turned ? a.tensor(9).numel() : 0;
+    HeadsOut oq(a, 13, q, queries), ok(a, 14, k, want);
+    if (a.odd || a.refuse(pairs > 1024)) return nullptr;
+    void* st = stream(a, k.t);
+    if (a.odd) return nullptr;
+    if (failed("arrol_append", launch([&] {
+            oq.get(q);
+            ok.get(k);
+            return arrol_append(data(k.t), k.stride, data(v.t), v.stride, queries ? data(q.t) : nullptr, queries ? q.stride : 0, cu, t.len, position, f, k.n, t.rows,
+                                queries ? q.heads : 0, static_cast<int32_t>(2 * pairs), interleaved, magnitude, data(kv.t), kv.layout, layer, t.ids, t.width, oq.p,
+                                oq.stride, ok.p, ok.stride, st);
+        })))
+        return nullptr;
+    PyObject* d = PyDict_New();
+    if (!d) return nullptr;
+    if (!put(d, "q", oq.object(a, 13)) || !put(d, "k", ok.object(a, 14))) {
+        Py_DECREF(d);
+        return nullptr;
+    }
+    return d;
+}
+
 template <PyObject* (*F)(Args&), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -703,7 +790,7 @@ PyMethodDef methods[] = {
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&setup)), METH_FASTCALL, nullptr},
     ENTRY(score, 7), ENTRY(score_mlp, 7), ENTRY(score_grad, 6), ENTRY(score_mlp_grad, 9), ENTRY(adamw_step, 11), ENTRY(select, 7),
     ENTRY(weighted_vote, 5), ENTRY(histogram, 3), ENTRY(calibrate, 3), ENTRY(prune_bernoulli, 4), ENTRY(grpo_advantage, 4),
-    ENTRY(grpo_objective, 10), ENTRY(attention, 9), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10),
+    ENTRY(grpo_objective, 10), ENTRY(attention, 9), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10), ENTRY(rotary, 9), ENTRY(append, 15),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
