@@ -21,6 +21,7 @@
  *   arrol_attention, arrol_attention_grad                      attention over packed sequences (prompts, survivors) and its gradient
  *   arrol_decode_attention                                     one token per rollout over the paged pool, a group's prompt read once
  *   arrol_evict                                                rollouts' caches cut to a budget of tokens by their attention weight
+ *   arrol_logprob_grad                                         gradient of arrol_logprob: hidden states and LM head
  *   arrol_rotary, arrol_rotary_frequencies                     queries and keys of packed rows turned by their positions, and back
  *   arrol_append                                               new tokens' keys and values into the paged pool, turned on the way
  *
@@ -228,6 +229,26 @@ int arrol_logprob_kernel(int64_t T, int32_t V, int32_t d, int32_t n_splits, int3
                          int32_t* tile_tokens, int32_t* splits);
 /* In the same manner: *streamed is 1 where the lm_head is loaded past the caches (kernel 2, one token block, an lm_head beyond 288 MiB). */
 int arrol_logprob_streamed(int64_t T, int32_t V, int32_t d, int32_t n_splits, int32_t* streamed);
+
+/*
+ * The gradient of arrol_logprob with respect to hidden states and LM head, given lse (arrol_logprob's lse_out of the same hidden and lm_head) and
+ * grad_logp = dL/dlogprob fp32 [T] (arrol_grpo_objective's grad_logp, for instance; its sign is the caller's):
+ *   dz_tv = grad_logp_t ([v = y_t] - exp(z_tv - lse_t)),  dL/dh_t = sum_v dz_tv W_v,  dL/dW_v = sum_t dz_tv h_t
+ * The logits are formed again in pieces of the vocabulary and the tokens; of a piece only dz is kept, in bf16 (rounded by up to 2^-8 each); products accumulate in fp32.
+ * A token whose grad_logp is 0, or whose target lies outside [0, V), takes no part, whatever its hidden state, lse and grad_logp hold (NaN and infinities, too): its
+ * grad_hidden is 0.  No products are spent on such tokens.
+ * hidden, lm_head, targets as in arrol_logprob; d at most 16384, V at most 2^24, T below 2^40.
+ * grad_hidden   NULL or bf16 [T, d], rounded once from fp32 sums.
+ * grad_lm_head  NULL or bf16 [V, d], likewise;  lm_head_sum  NULL or fp32 [V, d], to which the gradient is ADDED (for several calls on parts of a batch).  One of the
+ *               two at most, and one output at least; an output overlaps no input.  16-byte aligned.
+ * No atomics: bit-reproducible run to run.  T == 0 writes zeros to grad_lm_head and nothing else.
+ * workspace: arrol_logprob_grad_workspace_bytes(T, V, d, want_lm_head) bytes, 16-byte aligned, want_lm_head != 0 where grad_lm_head is given.  The size never falls
+ *            as T grows, and from 16,384 tokens on it does not grow either, but for the sums of grad_lm_head (4 V d bytes beyond them).
+ */
+size_t arrol_logprob_grad_workspace_bytes(int64_t T, int32_t V, int32_t d, int32_t want_lm_head);
+int arrol_logprob_grad(const void* hidden, const void* lm_head, const int32_t* targets, const float* lse, const float* grad_logp,
+                       int64_t T, int32_t V, int32_t d, void* grad_hidden, void* grad_lm_head, float* lm_head_sum,
+                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Stage 5 -- rank-weighted vote (Sec. 4.4: candidates are sorted by head score and their

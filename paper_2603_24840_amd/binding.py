@@ -76,6 +76,8 @@ _SIGNATURES = {
                                              _vp, _sz, _vp]),
     "arrol_logprob_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "arrol_logprob": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "arrol_logprob_grad_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "arrol_logprob_grad": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "arrol_logprob_kernel": (ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
     "arrol_logprob_streamed": (ctypes.c_int, [_i64, _i32, _i32, _i32, _vp]),
     "arrol_token_confidence_workspace_bytes": (_sz, [_i32, _i32]),
@@ -1022,6 +1024,42 @@ def _py_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, pos
                             _stream(stream))
     _check("arrol_append", rc)
     return dict(q=out_q, k=out_k)
+
+
+def arrol_logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden=True, want_lm_head=True, lm_head_sum=None, workspace=None, *, stream=None):
+    """Gradient of arrol_logprob: hidden bf16 [T, d], lm_head bf16 [V, d], targets int32 [T], lse fp32 [T] (arrol_logprob's), grad_logp = dL/dlogprob fp32 [T]
+    -> dict(grad_hidden bf16 [T, d], grad_lm_head bf16 [V, d]), None where not wanted.  lm_head_sum fp32 [V, d]: the LM head's gradient is added to it instead, and
+    grad_lm_head is None.  Tokens with grad_logp 0 or a target outside the vocabulary take no part."""
+    if stream is None:
+        result = (_marshal or _load_marshal()).logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden, want_lm_head, lm_head_sum, workspace)
+        if result is not None:
+            return result
+        return _py_logprob_grad.__wrapped__(hidden, lm_head, targets, lse, grad_logp, want_hidden, want_lm_head, lm_head_sum, workspace)
+    return _py_logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden, want_lm_head, lm_head_sum, workspace, stream=stream)
+
+
+@_on_stream
+def _py_logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden=True, want_lm_head=True, lm_head_sum=None, workspace=None, stream=None):
+    if hidden.dim() != 2 or lm_head.dim() != 2 or hidden.shape[1] != lm_head.shape[1]:
+        raise ValueError("hidden must be [T, d] and lm_head [V, d]")
+    (T, d), V, dev = hidden.shape, lm_head.shape[0], hidden.device
+    if targets.numel() != T or lse.numel() != T or grad_logp.numel() != T:
+        raise ValueError("targets, lse and grad_logp must be [T]")
+    if lm_head_sum is not None and lm_head_sum.shape != lm_head.shape:
+        raise ValueError("lm_head_sum must be [V, d]")
+    if not want_hidden and not want_lm_head and lm_head_sum is None:
+        raise ValueError("no gradient is wanted")
+    grads = dict(grad_hidden=torch.empty((T, d), dtype=torch.bfloat16, device=dev) if want_hidden else None,
+                 grad_lm_head=torch.empty((V, d), dtype=torch.bfloat16, device=dev) if want_lm_head and lm_head_sum is None else None)
+    if workspace is None:
+        need = lib().arrol_logprob_grad_workspace_bytes(T, V, d, int(grads["grad_lm_head"] is not None))
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    rc = lib().arrol_logprob_grad(_ptr(hidden, torch.bfloat16, "hidden"), _ptr(lm_head, torch.bfloat16, "lm_head"), _ptr(targets, torch.int32, "targets"),
+                                  _ptr(lse, torch.float32, "lse"), _ptr(grad_logp, torch.float32, "grad_logp"), T, V, d, _ptr(grads["grad_hidden"]),
+                                  _ptr(grads["grad_lm_head"]), _ptr(lm_head_sum, torch.float32, "lm_head_sum"), _ptr(workspace, torch.uint8, "workspace"),
+                                  workspace.numel(), _stream(stream))
+    _check("arrol_logprob_grad", rc)
+    return grads
 
 
 @_on_stream

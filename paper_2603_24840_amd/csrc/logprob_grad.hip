@@ -1,0 +1,467 @@
+// Gradient of the per-token log-probability with respect to hidden states and LM head (gfx950, wave64).
+//
+//   logp_t = z_t[y_t] - lse_t,  z_t = W h_t;  with g_t = dL/dlogp_t
+//   dz_tv = g_t ([v = y_t] - exp(z_tv - lse_t)),   dL/dh_t = sum_v dz_tv W_v,   dL/dW_v = sum_t dz_tv h_t
+//
+// Three contractions of 2 T V d flop; the logits are formed again, a piece of the vocabulary at a time, and of each piece only dz is kept, in bf16, as the operand of
+// the two others.  Per piece of up to kPieceRows tokens:
+//   gather     tokens that take part (g_t != 0 and a target inside the vocabulary) are counted and their hidden states put next to each other; the others' gradients are
+//              zeros.  Whatever such a token's hidden state holds takes no part, and no product is spent on it
+//   per piece of the vocabulary:
+//   dz         256 x 256 tiles of W h, dz in the epilogue, stored token-major through the LDS in whole lines
+//   products   tiles of dL/dh (dz as it lies, W read in place down its rows) and of dL/dW (dz and the hidden states both read down their rows), in one launch, so that
+//              the long walks of the first and the many short ones of the second fill the chip together
+//   join       the slabs of dL/dh, where there are several, added in order
+// No atomics: sums have a fixed order.
+#include "common.h"
+#include "ring_nt.h"
+
+namespace {
+
+using ring_nt::bf16x8;
+using ring_nt::f32x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kXcds = 8, kRound = 256;
+constexpr int64_t kPieceRows = 16384;              // tokens of a piece
+constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
+constexpr int kGatherRows = 16;
+
+typedef ring_nt::RingTile<256, 256, 2, 4> Tile;
+constexpr int BM = Tile::BM, BN = Tile::BN, TI = Tile::TI, TJ = Tile::TJ;
+
+struct Grad {
+    const uint16_t* W;              // of the vocabulary piece
+    const uint16_t* H;              // gathered hidden states [n_active, d]
+    uint16_t* dz;                   // [tokens][v_stride]
+    const float *g, *lse;           // gathered
+    const int32_t *target, *row;
+    const int32_t* n_active;
+    int d, v0, n_v;                 // first row of the piece, and how many
+    int v_stride;                   // of dz, a multiple of 256
+    // dL/dh
+    float* slabs;                   // [n_slabs][slab rows][d], NULL: straight to grad_hidden
+    int64_t slab_stride;
+    int n_slabs, k64_per_slab, add; // add: to what the slabs hold of pieces before
+    uint16_t* grad_hidden;
+    int grid_h;                     // workgroups of dL/dh
+    // dL/dW of the piece
+    float* sum;                     // fp32 sums, read and / or written
+    uint16_t* grad_w;
+    int read_sum, write_sum;
+};
+
+// Place in a work order in which every round of 256 workgroups gives each XCD (workgroup ids congruent mod 8) 32 that follow each other.  false: none.
+__device__ __forceinline__ bool place(int id, int64_t total, int64_t& pos) {
+    const int64_t round0 = id / kRound * kRound, left = total - round0;
+    const int in_round = left < kRound ? static_cast<int>(left) : kRound, within = id % kRound;
+    if (in_round <= 0) return false;
+    const int per_xcd = (in_round + kXcds - 1) / kXcds, p = within % kXcds * per_xcd + within / kXcds;
+    pos = round0 + p;
+    return within / kXcds < per_xcd && p < in_round;
+}
+// Tile (row, col) of `rows` x `cols` at a position: bands of up to `most` rows, through which the columns run, so that neighbours share operands.
+__device__ __forceinline__ void patch(int64_t pos, int rows, int cols, int most, int& row, int& col) {
+    const int bands = (rows + most - 1) / most, size = (rows + bands - 1) / bands;
+    const int b = static_cast<int>(pos / (static_cast<int64_t>(size) * cols));
+    const int r = static_cast<int>(pos - static_cast<int64_t>(b) * size * cols), mine = rows - b * size < size ? rows - b * size : size;
+    col = __builtin_amdgcn_readfirstlane(r / mine);      // in scalar registers, as the walk wants its bases
+    row = __builtin_amdgcn_readfirstlane(b * size + r - col * mine);
+}
+
+__device__ __forceinline__ bool takes_part(float g, int32_t target, int V) { return g != 0.f && target >= 0 && target < V; }      // NaN does
+
+// Tokens that take part, packed.  A workgroup has kGatherRows tokens and counts those before them itself.
+struct Gather {
+    const uint16_t* hidden;
+    const int32_t* targets;
+    const float *lse, *grad_logp;
+    uint16_t *H, *grad_hidden;
+    float *g, *lse_out;
+    int32_t *target, *row, *n_active;
+    int T, V, d;
+};
+__global__ __launch_bounds__(256) void gather_kernel(Gather a) {
+    __shared__ int before[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kGatherRows;
+    int n = 0;
+    for (int t = tid; t < t0; t += 256) n += __popcll(__ballot(takes_part(a.grad_logp[t], a.targets[t], a.V)));       // t0 is a multiple of 16: lanes beyond it are off
+    // a wavefront's lanes of one iteration are counted by each active one: lane 0 is active whenever any is
+    if (lane == 0) before[wave] = n;
+    const int mine = t0 + lane;
+    const bool in = lane < kGatherRows && mine < a.T;
+    const float g = in ? a.grad_logp[mine] : 0.f;
+    const int32_t y = in ? a.targets[mine] : -1;
+    const uint64_t active = __ballot(in && takes_part(g, y, a.V));
+    __syncthreads();
+    const int first = before[0] + before[1] + before[2] + before[3];
+    if (wave == 0 && ((active >> lane) & 1)) {
+        const int r = first + __popcll(active & ((uint64_t{1} << lane) - 1));
+        a.g[r] = g;
+        a.lse_out[r] = a.lse[mine];
+        a.target[r] = y;
+        a.row[r] = mine;
+    }
+    if (tid == 0 && t0 + kGatherRows >= a.T) *a.n_active = first + __popcll(active);
+    const int r = tid / 16, c0 = tid % 16, vecs = a.d / 8;
+    if (t0 + r >= a.T) return;
+    const uint16_t* from = a.hidden + static_cast<int64_t>(t0 + r) * a.d;
+    if ((active >> r) & 1) {
+        uint16_t* to = a.H + static_cast<int64_t>(first + __popcll(active & ((uint64_t{1} << r) - 1))) * a.d;
+        for (int c = c0; c < vecs; c += 16) *reinterpret_cast<u32x4*>(to + c * 8) = *reinterpret_cast<const u32x4*>(from + c * 8);
+    } else if (a.grad_hidden) {
+        uint16_t* to = a.grad_hidden + static_cast<int64_t>(t0 + r) * a.d;
+        for (int c = c0; c < vecs; c += 16) *reinterpret_cast<u32x4*>(to + c * 8) = u32x4{0, 0, 0, 0};
+    }
+}
+
+// acc[i][j][v] = z of vocabulary row 16 i + 4 (lane / 16) + v and token 16 j + lane % 16 of the wavefront's part of the tile -> dz, by way of the LDS (free, and all
+// wavefronts past a barrier).  There a token's row of 256 values has its 16-byte chunk c at position c ^ (token % 16): the 8-byte writes of a wavefront, 16 tokens x 4, and
+// the reads along a row take every bank equally often.
+__device__ __forceinline__ void store_dz(const Grad& a, f32x4 (&acc)[TI][TJ], unsigned char* lds, int vt, int tb, int n_active) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
+    const int v_first = vt * BM + wm * (BM / Tile::WM), t_first = tb * BN + wn * (BN / Tile::WN);
+    const bool hangs = v_first + BM / Tile::WM > a.n_v;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+        const int t = t_first + j * 16 + l15;
+        const bool live = t < n_active;
+        const float g = live ? a.g[t] : 0.f, at = live ? -a.lse[t] * kLog2e : 0.f;
+        const int y = live ? a.target[t] - a.v0 - v_first - 4 * lq : -1;        // of this lane's rows: 16 i + v
+        const bool mine = y >= 0 && y < BM / Tile::WM && (y & 12) == 0;
+        unsigned char* to = lds + (t_first - tb * BN + j * 16 + l15) * 512 + (lq & 1) * 8;
+        const int chunk = (wm * (BM / Tile::WM) >> 3) + (lq >> 1);
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[v] = -g * __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, at));
+            if (__any(mine && y >> 4 == i)) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (mine && y == 16 * i + v) x[v] += g;
+            }
+            if (hangs) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    if (v_first + 16 * i + 4 * lq + v >= a.n_v) x[v] = 0.f;
+            }
+            if (!live) x = f32x4{0.f, 0.f, 0.f, 0.f};
+            *reinterpret_cast<bf16x4*>(to + (((chunk + 2 * i) ^ l15) << 4)) = __builtin_convertvector(x, bf16x4);
+        }
+    }
+    __syncthreads();
+    uint16_t* out = a.dz + static_cast<int64_t>(tb) * BN * a.v_stride + static_cast<int64_t>(vt) * BM;
+    for (int r = tid >> 5; r < BN; r += Tile::NT / 32) {
+        const int c = tid & 31;
+        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(r) * a.v_stride + c * 8) = *reinterpret_cast<const u32x4*>(lds + r * 512 + ((c ^ (r & 15)) << 4));
+    }
+}
+
+__device__ __forceinline__ bool dz_tile(const Grad& a, int n_active, int& vt, int& tb) {
+    const int n_tb = (n_active + BN - 1) / BN, n_vt = (a.n_v + BM - 1) / BM;
+    int64_t pos;
+    if (!place(blockIdx.x, static_cast<int64_t>(n_tb) * n_vt, pos)) return false;
+    patch(pos, n_tb, n_vt, 6, tb, vt);
+    return true;
+}
+
+__global__ __launch_bounds__(Tile::NT) void dz_ring_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    int vt, tb;
+    if (!dz_tile(a, n_active, vt, tb)) return;
+    ring_nt::Walk w = {};
+    const int64_t row = static_cast<int64_t>(a.d) * 2;
+    w.a_base = reinterpret_cast<const char*>(a.W) + vt * BM * row;
+    w.b_base = reinterpret_cast<const char*>(a.H) + tb * BN * row;
+    w.a_stride = w.b_stride = static_cast<unsigned>(row);
+    w.a_rows = a.n_v - vt * BM;
+    w.b_rows = n_active - tb * BN < BN ? n_active - tb * BN : BN;
+    w.n_k64 = a.d / 64;
+    f32x4 acc[TI][TJ];
+    ring_nt::walk<Tile>(w, lds, acc);
+    store_dz(a, acc, lds, vt, tb, n_active);
+}
+
+// Any d that is a multiple of 8: K64 steps by way of registers, zeros behind the end of a row.  16-byte chunk c of tile row r lies at c ^ (r / 2) % 8.
+__global__ __launch_bounds__(Tile::NT) void dz_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    int vt, tb;
+    if (!dz_tile(a, n_active, vt, tb)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
+    constexpr int kRows = (BM + BN) / (Tile::NT / 8);         // of a lane: one chunk of each
+    const int c = tid & 7;
+    const uint16_t* from[kRows];
+#pragma unroll
+    for (int p = 0; p < kRows; ++p) {
+        const int r = (tid >> 3) + p * (Tile::NT / 8);
+        const int v = vt * BM + r < a.n_v ? vt * BM + r : a.n_v - 1, t = tb * BN + r - BM < n_active ? tb * BN + r - BM : n_active - 1;
+        from[p] = (r < BM ? a.W + static_cast<int64_t>(v) * a.d : a.H + static_cast<int64_t>(t) * a.d) + c * 8;
+    }
+    f32x4 acc[TI][TJ];
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < a.d; k += 64) {
+        u32x4 x[kRows];
+#pragma unroll
+        for (int p = 0; p < kRows; ++p) x[p] = k + c * 8 < a.d ? *reinterpret_cast<const u32x4*>(from[p] + k) : u32x4{0, 0, 0, 0};
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < kRows; ++p) {
+            const int r = (tid >> 3) + p * (Tile::NT / 8);
+            *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ ((r >> 1) & 7)) << 4)) = x[p];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 fb[TJ];
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const int r = BM + wn * (BN / Tile::WN) + j * 16 + l15;
+                fb[j] = *reinterpret_cast<const bf16x8*>(lds + r * 128 + (((kk * 4 + lq) ^ ((r >> 1) & 7)) << 4));
+            }
+#pragma unroll
+            for (int i = 0; i < TI; ++i) {
+                const int r = wm * (BM / Tile::WM) + i * 16 + l15;
+                const bf16x8 fa = *reinterpret_cast<const bf16x8*>(lds + r * 128 + (((kk * 4 + lq) ^ ((r >> 1) & 7)) << 4));
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+    __syncthreads();
+    store_dz(a, acc, lds, vt, tb, n_active);
+}
+
+__device__ __forceinline__ uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
+
+__global__ __launch_bounds__(Tile::NT) void products_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
+    const int n_db = (a.d + BN - 1) / BN;
+    const int64_t row = static_cast<int64_t>(a.d) * 2;
+    ring_nt::Walk w = {};
+    f32x4 acc[TI][TJ];
+    int64_t pos;
+    int at, db;
+    if (static_cast<int>(blockIdx.x) < a.grid_h) {
+        // dL/dh: 256 tokens x 256 columns, K = the vocabulary piece or a part of it
+        const int n_tb = (n_active + BM - 1) / BM;
+        const int64_t tiles = static_cast<int64_t>(n_tb) * n_db;
+        if (!place(blockIdx.x, tiles * a.n_slabs, pos)) return;
+        const int s = __builtin_amdgcn_readfirstlane(static_cast<int>(pos / tiles));
+        patch(pos - s * tiles, n_db, n_tb, 8, db, at);
+        const int n_k64 = (a.n_v + 63) / 64, k_lo = s * a.k64_per_slab, k_hi = k_lo + a.k64_per_slab < n_k64 ? k_lo + a.k64_per_slab : n_k64;
+        w.a_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * BM * a.v_stride) + static_cast<int64_t>(k_lo) * 128;
+        w.a_stride = static_cast<unsigned>(a.v_stride) * 2;
+        w.a_rows = n_active - at * BM;
+        w.b_base = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(k_lo) * 64 * row + db * BN * 2;
+        w.b_stride = static_cast<unsigned>(row);
+        w.b_rows = a.d - db * BN < BN ? a.d - db * BN : BN;
+        w.b_k_rows = a.n_v - k_lo * 64;
+        w.n_k64 = k_hi > k_lo ? k_hi - k_lo : 0;
+        ring_nt::walk<Tile, true, false>(w, lds, acc);
+        float* slab = a.slabs ? a.slabs + s * a.slab_stride : nullptr;
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int t = at * BM + wm * (BM / Tile::WM) + i * 16 + lq * 4 + v;
+                if (t >= n_active) continue;
+                float* to = slab + static_cast<int64_t>(t) * a.d;
+                uint16_t* out = slab ? nullptr : a.grad_hidden + static_cast<int64_t>(a.row[t]) * a.d;
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) {
+                    const int c = db * BN + wn * (BN / Tile::WN) + j * 16 + l15;
+                    if (c >= a.d) continue;
+                    if (slab) to[c] = a.add ? to[c] + acc[i][j][v] : acc[i][j][v];
+                    else out[c] = narrow(acc[i][j][v]);
+                }
+            }
+        return;
+    }
+    // dL/dW: 256 rows of the piece x 256 columns, K = the tokens
+    const int n_vt = (a.n_v + BM - 1) / BM;
+    if (!place(blockIdx.x - a.grid_h, static_cast<int64_t>(n_vt) * n_db, pos)) return;
+    patch(pos, n_db, n_vt, 8, db, at);
+    w.a_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * BM);
+    w.a_stride = static_cast<unsigned>(a.v_stride) * 2;
+    w.a_rows = BM;                                   // v_stride is a multiple of 256
+    w.a_k_rows = (n_active + BN - 1) / BN * BN;      // rows of zeros behind n_active
+    w.b_base = reinterpret_cast<const char*>(a.H) + db * BN * 2;
+    w.b_stride = static_cast<unsigned>(row);
+    w.b_rows = a.d - db * BN < BN ? a.d - db * BN : BN;
+    w.b_k_rows = n_active;
+    w.n_k64 = (n_active + 63) / 64;
+    ring_nt::walk<Tile, true, true>(w, lds, acc);
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int u = at * BM + wm * (BM / Tile::WM) + i * 16 + lq * 4 + v;
+            if (u >= a.n_v) continue;
+            const int64_t line = static_cast<int64_t>(u) * a.d;
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const int c = db * BN + wn * (BN / Tile::WN) + j * 16 + l15;
+                if (c >= a.d) continue;
+                float x = acc[i][j][v];
+                if (a.read_sum) x += a.sum[line + c];
+                if (a.write_sum) a.sum[line + c] = x;
+                else a.grad_w[line + c] = narrow(x);
+            }
+        }
+}
+
+// Slabs of dL/dh added in order, rounded, to the tokens' own rows.
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ slabs, int64_t slab_stride, int n_slabs, const int32_t* __restrict__ row, const int32_t* __restrict__ n_active,
+                                                   int d, uint16_t* __restrict__ grad_hidden) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const int vecs = d / 4;
+    const int64_t total = static_cast<int64_t>(*n_active) * vecs;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<int64_t>(t) * vecs) * 4;
+        f32x4 x = *reinterpret_cast<const f32x4*>(slabs + i * 4);
+        for (int s = 1; s < n_slabs; ++s) x += *reinterpret_cast<const f32x4*>(slabs + s * slab_stride + i * 4);
+        *reinterpret_cast<bf16x4*>(grad_hidden + static_cast<int64_t>(row[t]) * d + c) = __builtin_convertvector(x, bf16x4);
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(u32x4* out, int64_t n) {
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) out[i] = u32x4{0, 0, 0, 0};
+}
+
+size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int kMaxSlabs = 32, kSlabTiles = 512;
+
+// Vocabulary rows of a piece: as many as kPieceElements allow.
+struct Pieces {
+    int64_t rows, n_rows;           // tokens of a piece, pieces
+    int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces
+    int slabs;
+};
+Pieces pieces(int64_t T, int64_t V, int64_t d) {
+    Pieces p;
+    p.n_rows = (T + kPieceRows - 1) / kPieceRows;
+    p.rows = (T + p.n_rows - 1) / p.n_rows;
+    const int64_t most = kPieceElements / up256(p.rows) / 256 * 256, all = up256(V);
+    p.n_v = (all + most - 1) / most;
+    p.v = up256((all + p.n_v - 1) / p.n_v);
+    p.n_v = (all + p.v - 1) / p.v;
+    const int64_t tiles = up256(p.rows) / 256 * (up256(d) / 256), k64 = p.v / 64;
+    int64_t s = kSlabTiles / tiles;
+    s = s < kMaxSlabs ? s : kMaxSlabs;
+    s = s < k64 / 4 ? s : k64 / 4;
+    p.slabs = static_cast<int>(s > 1 ? s : 1);
+    return p;
+}
+
+struct Workspace {
+    size_t H, g, lse, target, row, n_active, dz, slabs, sum, bytes;
+};
+// Sizes that no smaller batch exceeds.
+Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
+    Workspace w;
+    const int64_t rows = T < kPieceRows ? T : kPieceRows, all = up256(rows) * up256(V);
+    const int64_t tiles = up256(rows) / 256 * (up256(d) / 256);
+    const int64_t most_tiles = tiles * kMaxSlabs < kSlabTiles ? tiles * kMaxSlabs : tiles > kSlabTiles ? tiles : kSlabTiles;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes); return was; };
+    w.n_active = take(4);
+    w.g = take(rows * 4), w.lse = take(rows * 4), w.target = take(rows * 4), w.row = take(rows * 4);
+    w.H = take(up256(rows) * d * 2);
+    w.dz = take((all < kPieceElements ? all : kPieceElements) * 2);
+    w.slabs = take(most_tiles * 65536 * 4);
+    w.sum = take(lm_head && T > kPieceRows ? V * d * 4 : 0);
+    w.bytes = at;
+    return w;
+}
+
+bool sizes_ok(int64_t T, int64_t V, int64_t d) { return T >= 0 && T < (int64_t{1} << 40) && V >= 1 && V <= (1 << 24) && d >= 8 && d % 8 == 0 && d <= 16384; }
+
+unsigned rounded(int64_t n) { return static_cast<unsigned>((n + kXcds - 1) / kXcds * kXcds); }
+
+}  // namespace
+
+extern "C" size_t arrol_logprob_grad_workspace_bytes(int64_t T, int32_t V, int32_t d, int32_t want_lm_head) {
+    return sizes_ok(T, V, d) && T > 0 ? workspace(T, V, d, want_lm_head != 0).bytes : 0;
+}
+
+extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const int32_t* targets, const float* lse, const float* grad_logp, int64_t T, int32_t V,
+                                  int32_t d, void* grad_hidden, void* grad_lm_head, float* lm_head_sum, void* workspace_, size_t workspace_bytes, void* stream) {
+    if (!sizes_ok(T, V, d) || (!grad_hidden && !grad_lm_head && !lm_head_sum && T > 0) || (grad_lm_head && lm_head_sum)) return ARROL_EINVAL;
+    if (T > 0 && (!hidden || !lm_head || !targets || !lse || !grad_logp)) return ARROL_EINVAL;
+    for (const void* p : {hidden, lm_head, static_cast<const void*>(grad_hidden), static_cast<const void*>(grad_lm_head), static_cast<const void*>(lm_head_sum)})
+        if (!arrol_aligned16(p)) return ARROL_EINVAL;
+    const auto st = static_cast<hipStream_t>(stream);
+    if (T == 0) {
+        if (grad_lm_head) {
+            const int64_t vecs = static_cast<int64_t>(V) * d / 8, blocks = (vecs + 255) / 256;
+            arrol_launch(zero_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, static_cast<u32x4*>(grad_lm_head), vecs);
+        }
+        return arrol_launch_status();
+    }
+    const Workspace ws = workspace(T, V, d, grad_lm_head != nullptr);
+    if (!workspace_ || !arrol_aligned16(workspace_) || workspace_bytes < ws.bytes) return ARROL_EWORKSPACE;
+    static arrol_device_flags ring_ok, general_ok, products_ok;
+    if (!arrol_allow_lds(&dz_ring_kernel, Tile::LDS_BYTES, ring_ok) || !arrol_allow_lds(&dz_kernel, Tile::LDS_BYTES, general_ok) ||
+        !arrol_allow_lds(&products_kernel, Tile::LDS_BYTES, products_ok))
+        return ARROL_EHIP;
+    auto* base = static_cast<unsigned char*>(workspace_);
+    const Pieces p = pieces(T, V, d);
+    Grad a = {};
+    a.H = reinterpret_cast<uint16_t*>(base + ws.H), a.dz = reinterpret_cast<uint16_t*>(base + ws.dz);
+    a.g = reinterpret_cast<float*>(base + ws.g), a.lse = reinterpret_cast<float*>(base + ws.lse);
+    a.target = reinterpret_cast<int32_t*>(base + ws.target), a.row = reinterpret_cast<int32_t*>(base + ws.row);
+    a.n_active = reinterpret_cast<int32_t*>(base + ws.n_active);
+    a.d = d;
+    const int64_t n_db = up256(d) / 256;
+    for (int64_t piece = 0; piece < p.n_rows; ++piece) {
+        const int64_t t0 = piece * p.rows, rows = T - t0 < p.rows ? T - t0 : p.rows;
+        Gather g;
+        g.hidden = static_cast<const uint16_t*>(hidden) + t0 * d, g.targets = targets + t0, g.lse = lse + t0, g.grad_logp = grad_logp + t0;
+        g.H = const_cast<uint16_t*>(a.H), g.grad_hidden = grad_hidden ? static_cast<uint16_t*>(grad_hidden) + t0 * d : nullptr;
+        g.g = const_cast<float*>(a.g), g.lse_out = const_cast<float*>(a.lse), g.target = const_cast<int32_t*>(a.target), g.row = const_cast<int32_t*>(a.row);
+        g.n_active = const_cast<int32_t*>(a.n_active), g.T = static_cast<int>(rows), g.V = V, g.d = d;
+        arrol_launch(gather_kernel, dim3(static_cast<unsigned>((rows + kGatherRows - 1) / kGatherRows)), dim3(256), 0, st, g);
+        const bool direct = p.slabs == 1 && p.n_v == 1;
+        const int64_t n_tb = up256(rows) / 256;
+        a.slab_stride = rows * d;
+        a.slabs = direct ? nullptr : reinterpret_cast<float*>(base + ws.slabs);
+        a.grad_hidden = g.grad_hidden;
+        for (int64_t q = 0; q < p.n_v; ++q) {
+            const int64_t v0 = q * p.v, n_v = V - v0 < p.v ? V - v0 : p.v, n_vt = up256(n_v) / 256;
+            a.W = static_cast<const uint16_t*>(lm_head) + v0 * d, a.v0 = static_cast<int>(v0), a.n_v = static_cast<int>(n_v), a.v_stride = static_cast<int>(p.v);
+            const dim3 grid(rounded(n_tb * n_vt));
+            if (d % 64 == 0) arrol_launch(dz_ring_kernel, grid, dim3(Tile::NT), Tile::LDS_BYTES, st, a);
+            else arrol_launch(dz_kernel, grid, dim3(Tile::NT), Tile::LDS_BYTES, st, a);
+            a.n_slabs = p.slabs, a.k64_per_slab = static_cast<int>((p.v / 64 + p.slabs - 1) / p.slabs), a.add = q > 0;
+            a.grid_h = grad_hidden ? static_cast<int>(rounded(n_tb * n_db * p.slabs)) : 0;
+            int64_t grid_w = 0;
+            if (grad_lm_head || lm_head_sum) {
+                grid_w = rounded(n_vt * n_db);
+                a.sum = (lm_head_sum ? lm_head_sum : reinterpret_cast<float*>(base + ws.sum)) + v0 * d;
+                a.grad_w = grad_lm_head ? static_cast<uint16_t*>(grad_lm_head) + v0 * d : nullptr;
+                a.read_sum = lm_head_sum || piece > 0, a.write_sum = lm_head_sum || piece + 1 < p.n_rows;
+            }
+            arrol_launch(products_kernel, dim3(static_cast<unsigned>(a.grid_h + grid_w)), dim3(Tile::NT), Tile::LDS_BYTES, st, a);
+        }
+        if (grad_hidden && !direct) {
+            const int64_t blocks = (rows * (d / 4) + 255) / 256;
+            arrol_launch(join_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a.slabs, a.slab_stride, p.slabs, a.row, a.n_active,
+                         d, a.grad_hidden);
+        }
+    }
+    return arrol_launch_status();
+}

@@ -745,6 +745,39 @@ PyObject* append(Args& a) {
     return d;
 }
 
+// hidden, lm_head, targets, lse, grad_logp, want_hidden, want_lm_head, lm_head_sum, workspace
+PyObject* logprob_grad(Args& a) {
+    const at::Tensor &h = a.tensor(0, at::kBFloat16), &w = a.tensor(1, at::kBFloat16);
+    if (a.odd || a.refuse(h.dim() != 2 || w.dim() != 2 || h.size(1) != w.size(1) || w.size(0) > INT32_MAX || h.size(1) > INT32_MAX)) return nullptr;
+    const int64_t T = h.size(0);
+    const int32_t V = static_cast<int32_t>(w.size(0)), d = static_cast<int32_t>(h.size(1));
+    const int32_t* targets = a.ptr<int32_t>(2, at::kInt, T);
+    const float *lse = a.ptr<float>(3, at::kFloat, T), *g = a.ptr<float>(4, at::kFloat, T);
+    const bool want_h = a.truth(5), want_w = a.truth(6) && !a.given(7);
+    if (a.odd || a.refuse(!a.given(2) || !a.given(3) || !a.given(4) || (!want_h && !want_w && !a.given(7)))) return nullptr;
+    float* sum = a.ptr<float>(7, at::kFloat);
+    if (a.odd || (a.given(7) && a.refuse(a.tensor(7).sizes() != w.sizes()))) return nullptr;
+    void* st = stream(a, h);
+    if (a.odd) return nullptr;
+    const size_t need = arrol_logprob_grad_workspace_bytes(T, V, d, want_w);
+    Scratch ws(a, 8, need > 16 ? need : 16);
+    if (a.odd) return nullptr;
+    at::Tensor gh, gw;
+    if (failed("arrol_logprob_grad", launch([&] {
+            ws.get(h);
+            void *ph = want_h ? made(gh, h.sizes(), at::kBFloat16, h) : nullptr, *pw = want_w ? made(gw, w.sizes(), at::kBFloat16, h) : nullptr;
+            return arrol_logprob_grad(data(h), data(w), targets, lse, g, T, V, d, ph, pw, sum, ws.p, ws.bytes, st);
+        })))
+        return nullptr;
+    PyObject* out = PyDict_New();
+    if (!out) return nullptr;
+    if (!put(out, "grad_hidden", gh.defined() ? wrap(std::move(gh)) : keep(Py_None)) || !put(out, "grad_lm_head", gw.defined() ? wrap(std::move(gw)) : keep(Py_None))) {
+        Py_DECREF(out);
+        return nullptr;
+    }
+    return out;
+}
+
 template <PyObject* (*F)(Args&), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -790,7 +823,7 @@ PyMethodDef methods[] = {
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&setup)), METH_FASTCALL, nullptr},
     ENTRY(score, 7), ENTRY(score_mlp, 7), ENTRY(score_grad, 6), ENTRY(score_mlp_grad, 9), ENTRY(adamw_step, 11), ENTRY(select, 7),
     ENTRY(weighted_vote, 5), ENTRY(histogram, 3), ENTRY(calibrate, 3), ENTRY(prune_bernoulli, 4), ENTRY(grpo_advantage, 4),
-    ENTRY(grpo_objective, 10), ENTRY(attention, 9), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10), ENTRY(rotary, 9), ENTRY(append, 15),
+    ENTRY(grpo_objective, 10), ENTRY(attention, 9), ENTRY(attention_grad, 11), ENTRY(decode_attention, 15), ENTRY(evict, 10), ENTRY(rotary, 9), ENTRY(append, 15), ENTRY(logprob_grad, 9),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -36,6 +36,9 @@
 // consecutive b-values of k-row e, and lane j receives the four k-values of b-value j (layout measured on
 // the device).  16-byte chunk c of k-row r sits at chunk position c ^ 4 (r % 4) ^ 2 ((r / 8) % 2) of its row: the 32
 // lanes of a half-wave, which a 64-bit read serves together, then fall on 32 different 8-byte bank pairs.
+//
+// A_KMAJOR = true is the same for A: row k of A holds the tile's 256 a-values, starts k * a_stride bytes after the base, and the A
+// fragments come out through the transposing read.  With both, acc[a][b] = sum_k A[k][a] * B[k][b].
 #pragma once
 #include <type_traits>
 
@@ -81,13 +84,14 @@ struct Walk {
     int b_k_rows;             // B_KMAJOR only: k-rows of B that exist from b_base on (> 64 * (n_k64 - 1));
                               // b_rows is then the number of valid b-values (a multiple of 8), b_stride the
                               // bytes between k-rows
+    int a_k_rows;             // A_KMAJOR only, in the same way (a_rows: valid a-values, a multiple of 8)
 };
 
 // Accumulates one tile into the caller's `acc` (cleared here first): acc[i][j][v] belongs to A row
 // wm * (BM / WM) + 16 i + 4 (lane / 16) + v and B row wn * (BN / WN) + 16 j + lane % 16 of the tile, with
 // wm = wave / WN, wn = wave % WN.  On return every load into LDS and every fragment read has finished and the
 // workgroup has passed a barrier, so LDS is free for the caller.
-template <class C, bool B_KMAJOR = false>
+template <class C, bool B_KMAJOR = false, bool A_KMAJOR = false>
 __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ]) {
     constexpr int BM = C::BM, BN = C::BN, TI = C::TI, TJ = C::TJ, RING = C::RING;
     typedef __attribute__((address_space(3))) void* lds_ptr_t;
@@ -135,7 +139,17 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
             b_voff[g] = static_cast<unsigned>(r) * w.b_stride + ld_kb;
         }
     }
-    {
+    int a_lrow[C::G];   // A_KMAJOR: as b_lrow
+    if constexpr (A_KMAJOR) {
+        const int chunks_valid = (w.a_rows < BM ? w.a_rows : BM) >> 3;
+#pragma unroll
+        for (int g = 0; g < C::G; ++g) {
+            a_lrow[g] = (wave * C::G + g) * 2 + (lane >> 5);
+            int c = (lane & 31) ^ ((a_lrow[g] & 3) << 2) ^ (((a_lrow[g] >> 3) & 1) << 1);
+            c = c < chunks_valid ? c : chunks_valid - 1;
+            a_voff[g] = static_cast<unsigned>(c) * 16;
+        }
+    } else {
         const int rows_valid = w.a_rows < BM ? w.a_rows : BM;
 #pragma unroll
         for (int g = 0; g < C::G; ++g) {
@@ -171,6 +185,13 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
             voff += static_cast<unsigned>(r) * w.b_stride;
             base = b_base;
         }
+        if constexpr (A_KMAJOR && !is_b) {
+            const int left = w.a_k_rows - a_k64 * 64;
+            int r = h * 32 + a_lrow[g];
+            r = r < left ? r : left - 1;
+            voff += static_cast<unsigned>(r) * w.a_stride;
+            base = a_base;
+        }
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(dst) : "memory");
     };
     auto advance = [&](auto stream) {
@@ -184,7 +205,7 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
         } else {
             if (a_k64 + 1 < n_k64) {
                 ++a_k64;
-                a_base += 128;
+                a_base += A_KMAJOR ? static_cast<int64_t>(64) * w.a_stride : 128;
             }
             a_slot = a_slot + 2 >= RING ? a_slot + 2 - RING : a_slot + 2;
         }
@@ -212,9 +233,25 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
         for (int h2 = 0; h2 < 2; ++h2)
             bt_off[h2] = BM * 64 + (8 * lq + 4 * h2 + e) * 512 + ((chunk ^ (e << 2) ^ ((lq & 1) << 1)) << 4) + (q & 1) * 8;
     }
+    int at_off[2] = {0, 0};
+    if constexpr (A_KMAJOR) {
+        const int e = l15 >> 2, q = l15 & 3;
+        const int chunk = wm * (BM / C::WM / 8) + (q >> 1);
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2)
+            at_off[h2] = (8 * lq + 4 * h2 + e) * 512 + ((chunk ^ (e << 2) ^ ((lq & 1) << 1)) << 4) + (q & 1) * 8;
+    }
     bf16x8 fa[TI], fbe[TJ], fbo[TJ];   // A fragments (reloaded row by row), B fragments of even / odd iterations
     auto read_a = [&](const unsigned char* base, int i) {
-        fa[i] = *reinterpret_cast<const bf16x8*>(base + a_off + i * 16 * 64);
+        if constexpr (A_KMAJOR) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(base + (at_off[0] ^ (i << 5))));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(base + (at_off[1] ^ (i << 5))));
+            fa[i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            fa[i] = *reinterpret_cast<const bf16x8*>(base + a_off + i * 16 * 64);
+        }
     };
     auto read_b = [&](bf16x8 (&fb)[TJ], const unsigned char* base, int j) {
         if constexpr (B_KMAJOR) {

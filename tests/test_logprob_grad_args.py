@@ -1,0 +1,55 @@
+"""What the gradient of the log-probabilities refuses on the host, before anything is launched, and its workspace query."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def A():
+    import os
+    import paper_2603_24840_amd as pkg
+    if not os.path.exists(pkg.LIB_PATH):
+        from paper_2603_24840_amd import build
+        build.build(verbose=False)
+    return pkg
+
+
+FAKE = ctypes.c_void_p(0x1000)      # never dereferenced: validation fails first
+ODD = ctypes.c_void_p(0x1008)
+
+
+def grad(A, **kw):
+    a = dict(h=FAKE, w=FAKE, y=FAKE, lse=FAKE, g=FAKE, T=10, V=100, d=64, gh=FAKE, gw=FAKE, sum=None, ws=FAKE, nbytes=1 << 40)
+    a.update(kw)
+    return A.lib().arrol_logprob_grad(*a.values(), None)
+
+
+@pytest.mark.parametrize("bad", [dict(h=None), dict(h=ODD), dict(w=None), dict(w=ODD), dict(y=None), dict(lse=None), dict(g=None), dict(T=-1), dict(T=2 ** 40), dict(V=0), dict(V=-1),
+                                 dict(V=2 ** 24 + 1), dict(d=0), dict(d=4), dict(d=12), dict(d=16392), dict(gh=None, gw=None), dict(gh=ODD), dict(gw=ODD), dict(sum=FAKE),
+                                 dict(gw=None, sum=ODD)])
+def test_refuses(A, bad):
+    assert grad(A, **bad) == -1
+
+
+def test_workspace(A):
+    size = A.lib().arrol_logprob_grad_workspace_bytes
+    need = size(10, 100, 64, 1)
+    assert need > 0 and size(0, 100, 64, 1) == 0 and size(-1, 100, 64, 1) == 0 and size(10, 0, 64, 1) == 0 and size(10, 100, 60, 1) == 0
+    assert grad(A, ws=None) == -2 and grad(A, ws=ODD) == -2 and grad(A, nbytes=need - 1) == -2
+    for V, d in ((100, 64), (4096, 256), (128256, 2048), (151936, 4096)):
+        for want in (0, 1):
+            sizes = [size(T, V, d, want) for T in (1, 2, 63, 64, 65, 200, 255, 256, 257, 511, 513, 1000, 2049, 4096, 5000, 8192, 12000, 16383, 16384, 16385, 20000, 65536, 10 ** 6, 10 ** 9)]
+            assert sizes == sorted(sizes)
+            assert size(10 ** 9, V, d, 0) == size(16384, V, d, 0) and size(10 ** 9, V, d, 1) <= size(16384, V, d, 0) + 4 * V * d + 256
+    assert size(4096, 151936, 4096, 1) < 4096 * 151936 * 4 // 2        # less than half of the logits in 32 bits
+    assert grad(A, T=0, ws=None, nbytes=0, h=None, w=None, y=None, lse=None, g=None, gw=None) == 0
+
+
+def test_binding_refuses(A):
+    h, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(10, 64, dtype=torch.bfloat16)
+    y, f = torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    for args, kw in (((h, w, y, f, f), {}), ((h, w[:, :32], y, f, f), {}), ((h, w, y[:3], f, f), {}), ((h, w, y, f[:3], f), {}), ((h, w, y, f, f[:3]), {}),
+                     ((h, w, y, f, f), dict(lm_head_sum=torch.zeros(9, 64))), ((h, w, y, f, f), dict(want_hidden=False, want_lm_head=False)), ((h[0], w, y, f, f), {})):
+        with pytest.raises((TypeError, ValueError)):
+            A.arrol_logprob_grad(*args, **kw)
