@@ -14,6 +14,7 @@
 //   join       the slabs of dL/dh, where there are several, added in order
 // No atomics: sums have a fixed order.
 #include "common.h"
+#include "mid_nt.h"
 #include "ring_nt.h"
 
 namespace {
@@ -27,8 +28,21 @@ constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
 constexpr int kGatherRows = 16;
 
-typedef ring_nt::RingTile<256, 256, 2, 4> Tile;
-constexpr int BM = Tile::BM, BN = Tile::BN, TI = Tile::TI, TJ = Tile::TJ;
+// The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
+struct Ring {
+    typedef ring_nt::RingTile<256, 256, 2, 4> C;
+    template <bool B_KMAJOR, bool A_KMAJOR>
+    __device__ static __forceinline__ void walk(const ring_nt::Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int = 8) { ring_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc); }
+};
+template <int BM, int BN, int NS>
+struct Mid {
+    typedef mid_nt::Tile<BM, BN, 2, 2, NS> C;
+    template <bool B_KMAJOR, bool A_KMAJOR>
+    __device__ static __forceinline__ void walk(const ring_nt::Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8) { mid_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc, tail); }
+};
+typedef Mid<128, 128, 2> Mid128;
+typedef Mid<128, 64, 3> MidFew;
+typedef Mid<64, 64, 4> Mid64;
 
 struct Grad {
     const uint16_t* W;              // of the vocabulary piece
@@ -115,26 +129,62 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
     }
 }
 
-// acc[i][j][v] = z of vocabulary row 16 i + 4 (lane / 16) + v and token 16 j + lane % 16 of the wavefront's part of the tile -> dz, by way of the LDS (free, and all
-// wavefronts past a barrier).  There a token's row of 256 values has its 16-byte chunk c at position c ^ (token % 16): the 8-byte writes of a wavefront, 16 tokens x 4, and
-// the reads along a row take every bank equally often.
-__device__ __forceinline__ void store_dz(const Grad& a, f32x4 (&acc)[TI][TJ], unsigned char* lds, int vt, int tb, int n_active) {
+// A wavefront's results, 4 consecutive values of a row in a lane, as bf16: lanes of neighbouring quarters exchange halves of two blocks, so that each stores 16 bytes and the
+// 16 lanes' rows get 64 bytes at a time.  x, y: blocks i and i + 1 of the row; the lane's 8 values start at 16 (i + lq % 2) + 4 (lq & 2).
+__device__ __forceinline__ u32x4 exchange(f32x4 x, f32x4 y) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
-    const int v_first = vt * BM + wm * (BM / Tile::WM), t_first = tb * BN + wn * (BN / Tile::WN);
-    const bool hangs = v_first + BM / Tile::WM > a.n_v;
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), b = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    return u32x4{lo[0], hi[0], lo[1], hi[1]};
+}
+
+struct Lane {
+    int lane, wave, l15, lq;
+    __device__ __forceinline__ Lane() : lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), l15(lane & 15), lq(lane >> 4) {}
+    __device__ __forceinline__ int place(int i) const { return 16 * (i + (lq & 1)) + 4 * (lq & 2); }      // of exchange()'s values
+};
+
+template <class C>
+__device__ __forceinline__ bool dz_tile(const Grad& a, int n_active, int& vt, int& tb) {
+    const int n_tb = (n_active + C::BN - 1) / C::BN, n_vt = (a.n_v + C::BM - 1) / C::BM;
+    int64_t pos;
+    if (!place(blockIdx.x, static_cast<int64_t>(n_tb) * n_vt, pos)) return false;
+    patch(pos, n_tb, n_vt, 6, tb, vt);
+    return true;
+}
+
+// acc[i][j][v] = z of vocabulary row 16 i + 4 (lane / 16) + v and token 16 j + lane % 16 of the wavefront's part of the tile.  dz of rows past the vocabulary and of
+// tokens past the last are zeros: the products' K extents are whole steps of 64.
+template <class F>
+__global__ __launch_bounds__(F::C::NT) void dz_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    typedef typename F::C C;
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    int vt, tb;
+    if (!dz_tile<C>(a, n_active, vt, tb)) return;
+    const Lane me;
+    ring_nt::Walk w = {};
+    const int64_t row = static_cast<int64_t>(a.d) * 2;
+    w.a_base = reinterpret_cast<const char*>(a.W) + vt * C::BM * row;
+    w.b_base = reinterpret_cast<const char*>(a.H) + tb * C::BN * row;
+    w.a_stride = w.b_stride = static_cast<unsigned>(row);
+    w.a_rows = a.n_v - vt * C::BM;
+    w.b_rows = n_active - tb * C::BN < C::BN ? n_active - tb * C::BN : C::BN;
+    w.n_k64 = (a.d + 63) / 64;
+    f32x4 acc[C::TI][C::TJ];
+    F::template walk<false, false>(w, lds, acc, (a.d & 63) ? (a.d & 63) / 8 : 8);
+    const int v_first = vt * C::BM + me.wave / C::WN * (C::BM / C::WM), t_first = tb * C::BN + me.wave % C::WN * (C::BN / C::WN);
+    const bool hangs = v_first + C::BM / C::WM > a.n_v;
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-        const int t = t_first + j * 16 + l15;
+    for (int j = 0; j < C::TJ; ++j) {
+        const int t = t_first + j * 16 + me.l15;
         const bool live = t < n_active;
         const float g = live ? a.g[t] : 0.f, at = live ? -a.lse[t] * kLog2e : 0.f;
-        const int y = live ? a.target[t] - a.v0 - v_first - 4 * lq : -1;        // of this lane's rows: 16 i + v
-        const bool mine = y >= 0 && y < BM / Tile::WM && (y & 12) == 0;
-        unsigned char* to = lds + (t_first - tb * BN + j * 16 + l15) * 512 + (lq & 1) * 8;
-        const int chunk = (wm * (BM / Tile::WM) >> 3) + (lq >> 1);
-#pragma unroll
-        for (int i = 0; i < TI; ++i) {
+        const int y = live ? a.target[t] - a.v0 - v_first - 4 * me.lq : -1;        // of this lane's rows: 16 i + v
+        const bool mine = y >= 0 && y < C::BM / C::WM && (y & 12) == 0;
+        uint16_t* to = a.dz + static_cast<int64_t>(t) * a.v_stride + v_first;
+        auto dz = [&](int i) {
             f32x4 x;
 #pragma unroll
             for (int v = 0; v < 4; ++v) x[v] = -g * __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, at));
@@ -146,180 +196,94 @@ __device__ __forceinline__ void store_dz(const Grad& a, f32x4 (&acc)[TI][TJ], un
             if (hangs) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    if (v_first + 16 * i + 4 * lq + v >= a.n_v) x[v] = 0.f;
+                    if (v_first + 16 * i + 4 * me.lq + v >= a.n_v) x[v] = 0.f;
             }
-            if (!live) x = f32x4{0.f, 0.f, 0.f, 0.f};
-            *reinterpret_cast<bf16x4*>(to + (((chunk + 2 * i) ^ l15) << 4)) = __builtin_convertvector(x, bf16x4);
-        }
-    }
-    __syncthreads();
-    uint16_t* out = a.dz + static_cast<int64_t>(tb) * BN * a.v_stride + static_cast<int64_t>(vt) * BM;
-    for (int r = tid >> 5; r < BN; r += Tile::NT / 32) {
-        const int c = tid & 31;
-        *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(r) * a.v_stride + c * 8) = *reinterpret_cast<const u32x4*>(lds + r * 512 + ((c ^ (r & 15)) << 4));
+            return live ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+        };
+#pragma unroll
+        for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(to + me.place(i)) = exchange(dz(i), dz(i + 1));
     }
 }
 
-__device__ __forceinline__ bool dz_tile(const Grad& a, int n_active, int& vt, int& tb) {
-    const int n_tb = (n_active + BN - 1) / BN, n_vt = (a.n_v + BM - 1) / BM;
-    int64_t pos;
-    if (!place(blockIdx.x, static_cast<int64_t>(n_tb) * n_vt, pos)) return false;
-    patch(pos, n_tb, n_vt, 6, tb, vt);
-    return true;
-}
-
-__global__ __launch_bounds__(Tile::NT) void dz_ring_kernel(Grad a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
-    int vt, tb;
-    if (!dz_tile(a, n_active, vt, tb)) return;
-    ring_nt::Walk w = {};
-    const int64_t row = static_cast<int64_t>(a.d) * 2;
-    w.a_base = reinterpret_cast<const char*>(a.W) + vt * BM * row;
-    w.b_base = reinterpret_cast<const char*>(a.H) + tb * BN * row;
-    w.a_stride = w.b_stride = static_cast<unsigned>(row);
-    w.a_rows = a.n_v - vt * BM;
-    w.b_rows = n_active - tb * BN < BN ? n_active - tb * BN : BN;
-    w.n_k64 = a.d / 64;
-    f32x4 acc[TI][TJ];
-    ring_nt::walk<Tile>(w, lds, acc);
-    store_dz(a, acc, lds, vt, tb, n_active);
-}
-
-// Any d that is a multiple of 8: K64 steps by way of registers, zeros behind the end of a row.  16-byte chunk c of tile row r lies at c ^ (r / 2) % 8.
-__global__ __launch_bounds__(Tile::NT) void dz_kernel(Grad a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
-    int vt, tb;
-    if (!dz_tile(a, n_active, vt, tb)) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
-    constexpr int kRows = (BM + BN) / (Tile::NT / 8);         // of a lane: one chunk of each
-    const int c = tid & 7;
-    const uint16_t* from[kRows];
+// The epilogue of both products: acc[i][j][v] belongs to column c0 + 16 i + 4 lq + v of row r0 + 16 j + l15.  sum: fp32, read and / or written; else bf16.
+template <class C, class RowOf>
+__device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int r0, int rows, int c0, int d, float* sum, bool read, bool write, uint16_t* out, RowOf row_of) {
 #pragma unroll
-    for (int p = 0; p < kRows; ++p) {
-        const int r = (tid >> 3) + p * (Tile::NT / 8);
-        const int v = vt * BM + r < a.n_v ? vt * BM + r : a.n_v - 1, t = tb * BN + r - BM < n_active ? tb * BN + r - BM : n_active - 1;
-        from[p] = (r < BM ? a.W + static_cast<int64_t>(v) * a.d : a.H + static_cast<int64_t>(t) * a.d) + c * 8;
-    }
-    f32x4 acc[TI][TJ];
+    for (int j = 0; j < C::TJ; ++j) {
+        const int r = r0 + j * 16 + me.l15;
+        const bool live = r < rows;
+        const int64_t line = static_cast<int64_t>(live ? r : 0) * d;
+        uint16_t* to = write ? nullptr : out + static_cast<int64_t>(live ? row_of(r) : 0) * d;
+        auto value = [&](int i) {
+            const int c = c0 + 16 * i + 4 * me.lq;
+            return read && live && c < d ? *reinterpret_cast<const f32x4*>(sum + line + c) + acc[i][j] : acc[i][j];
+        };
 #pragma unroll
-    for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < a.d; k += 64) {
-        u32x4 x[kRows];
-#pragma unroll
-        for (int p = 0; p < kRows; ++p) x[p] = k + c * 8 < a.d ? *reinterpret_cast<const u32x4*>(from[p] + k) : u32x4{0, 0, 0, 0};
-        __syncthreads();
-#pragma unroll
-        for (int p = 0; p < kRows; ++p) {
-            const int r = (tid >> 3) + p * (Tile::NT / 8);
-            *reinterpret_cast<u32x4*>(lds + r * 128 + ((c ^ ((r >> 1) & 7)) << 4)) = x[p];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 fb[TJ];
-#pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                const int r = BM + wn * (BN / Tile::WN) + j * 16 + l15;
-                fb[j] = *reinterpret_cast<const bf16x8*>(lds + r * 128 + (((kk * 4 + lq) ^ ((r >> 1) & 7)) << 4));
-            }
-#pragma unroll
-            for (int i = 0; i < TI; ++i) {
-                const int r = wm * (BM / Tile::WM) + i * 16 + l15;
-                const bf16x8 fa = *reinterpret_cast<const bf16x8*>(lds + r * 128 + (((kk * 4 + lq) ^ ((r >> 1) & 7)) << 4));
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < C::TI; i += 2) {
+            const f32x4 x = value(i), y = value(i + 1);
+            if (write) {
+                const int c = c0 + 16 * i + 4 * me.lq;
+                if (live && c < d) *reinterpret_cast<f32x4*>(sum + line + c) = x;
+                if (live && c + 16 < d) *reinterpret_cast<f32x4*>(sum + line + c + 16) = y;
+            } else {
+                const u32x4 packed = exchange(x, y);      // by all lanes
+                const int c = c0 + me.place(i);
+                if (live && c < d) *reinterpret_cast<u32x4*>(to + c) = packed;
             }
         }
     }
-    __syncthreads();
-    store_dz(a, acc, lds, vt, tb, n_active);
 }
 
-__device__ __forceinline__ uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
-
-__global__ __launch_bounds__(Tile::NT) void products_kernel(Grad a) {
+template <class FH, class FW>
+__global__ __launch_bounds__(FH::C::NT) void products_kernel(Grad a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / Tile::WN, wn = wave % Tile::WN, l15 = lane & 15, lq = lane >> 4;
-    const int n_db = (a.d + BN - 1) / BN;
+    const Lane me;
     const int64_t row = static_cast<int64_t>(a.d) * 2;
     ring_nt::Walk w = {};
-    f32x4 acc[TI][TJ];
     int64_t pos;
     int at, db;
     if (static_cast<int>(blockIdx.x) < a.grid_h) {
-        // dL/dh: 256 tokens x 256 columns, K = the vocabulary piece or a part of it
-        const int n_tb = (n_active + BM - 1) / BM;
+        // dL/dh: columns of W, which is read down its rows, times tokens' rows of dz; K = the vocabulary piece or a part of it
+        typedef typename FH::C C;
+        const int n_tb = (n_active + C::BN - 1) / C::BN, n_db = (a.d + C::BM - 1) / C::BM;
         const int64_t tiles = static_cast<int64_t>(n_tb) * n_db;
         if (!place(blockIdx.x, tiles * a.n_slabs, pos)) return;
         const int s = __builtin_amdgcn_readfirstlane(static_cast<int>(pos / tiles));
         patch(pos - s * tiles, n_db, n_tb, 8, db, at);
         const int n_k64 = (a.n_v + 63) / 64, k_lo = s * a.k64_per_slab, k_hi = k_lo + a.k64_per_slab < n_k64 ? k_lo + a.k64_per_slab : n_k64;
-        w.a_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * BM * a.v_stride) + static_cast<int64_t>(k_lo) * 128;
-        w.a_stride = static_cast<unsigned>(a.v_stride) * 2;
-        w.a_rows = n_active - at * BM;
-        w.b_base = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(k_lo) * 64 * row + db * BN * 2;
-        w.b_stride = static_cast<unsigned>(row);
-        w.b_rows = a.d - db * BN < BN ? a.d - db * BN : BN;
-        w.b_k_rows = a.n_v - k_lo * 64;
+        w.a_base = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(k_lo) * 64 * row + db * C::BM * 2;
+        w.a_stride = static_cast<unsigned>(row);
+        w.a_rows = a.d - db * C::BM;
+        w.a_k_rows = a.n_v - k_lo * 64;
+        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * C::BN * a.v_stride) + static_cast<int64_t>(k_lo) * 128;
+        w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
+        w.b_rows = n_active - at * C::BN < C::BN ? n_active - at * C::BN : C::BN;
         w.n_k64 = k_hi > k_lo ? k_hi - k_lo : 0;
-        ring_nt::walk<Tile, true, false>(w, lds, acc);
-        float* slab = a.slabs ? a.slabs + s * a.slab_stride : nullptr;
-#pragma unroll
-        for (int i = 0; i < TI; ++i)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int t = at * BM + wm * (BM / Tile::WM) + i * 16 + lq * 4 + v;
-                if (t >= n_active) continue;
-                float* to = slab + static_cast<int64_t>(t) * a.d;
-                uint16_t* out = slab ? nullptr : a.grad_hidden + static_cast<int64_t>(a.row[t]) * a.d;
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) {
-                    const int c = db * BN + wn * (BN / Tile::WN) + j * 16 + l15;
-                    if (c >= a.d) continue;
-                    if (slab) to[c] = a.add ? to[c] + acc[i][j][v] : acc[i][j][v];
-                    else out[c] = narrow(acc[i][j][v]);
-                }
-            }
+        f32x4 acc[C::TI][C::TJ];
+        FH::template walk<false, true>(w, lds, acc);
+        store_rows<C>(me, acc, at * C::BN + me.wave % C::WN * (C::BN / C::WN), n_active, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d,
+                      a.slabs + s * a.slab_stride, a.add, a.slabs != nullptr, a.grad_hidden, [&](int t) { return a.row[t]; });
         return;
     }
-    // dL/dW: 256 rows of the piece x 256 columns, K = the tokens
-    const int n_vt = (a.n_v + BM - 1) / BM;
+    // dL/dW: columns of the hidden states times the piece's rows, both read down the tokens
+    typedef typename FW::C C;
+    const int n_vt = (a.n_v + C::BN - 1) / C::BN, n_db = (a.d + C::BM - 1) / C::BM;
     if (!place(blockIdx.x - a.grid_h, static_cast<int64_t>(n_vt) * n_db, pos)) return;
     patch(pos, n_db, n_vt, 8, db, at);
-    w.a_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * BM);
-    w.a_stride = static_cast<unsigned>(a.v_stride) * 2;
-    w.a_rows = BM;                                   // v_stride is a multiple of 256
-    w.a_k_rows = (n_active + BN - 1) / BN * BN;      // rows of zeros behind n_active
-    w.b_base = reinterpret_cast<const char*>(a.H) + db * BN * 2;
-    w.b_stride = static_cast<unsigned>(row);
-    w.b_rows = a.d - db * BN < BN ? a.d - db * BN : BN;
-    w.b_k_rows = n_active;
+    w.a_base = reinterpret_cast<const char*>(a.H) + db * C::BM * 2;
+    w.a_stride = static_cast<unsigned>(row);
+    w.a_rows = a.d - db * C::BM;
+    w.a_k_rows = n_active;
+    w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * C::BN);
+    w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
+    w.b_rows = C::BN;                                // v_stride is a multiple of 256, and zeros follow the piece's last row up to a multiple of 64
     w.n_k64 = (n_active + 63) / 64;
-    ring_nt::walk<Tile, true, true>(w, lds, acc);
-#pragma unroll
-    for (int i = 0; i < TI; ++i)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int u = at * BM + wm * (BM / Tile::WM) + i * 16 + lq * 4 + v;
-            if (u >= a.n_v) continue;
-            const int64_t line = static_cast<int64_t>(u) * a.d;
-#pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                const int c = db * BN + wn * (BN / Tile::WN) + j * 16 + l15;
-                if (c >= a.d) continue;
-                float x = acc[i][j][v];
-                if (a.read_sum) x += a.sum[line + c];
-                if (a.write_sum) a.sum[line + c] = x;
-                else a.grad_w[line + c] = narrow(x);
-            }
-        }
+    w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
+    f32x4 acc[C::TI][C::TJ];
+    FW::template walk<true, true>(w, lds, acc);
+    store_rows<C>(me, acc, at * C::BN + me.wave % C::WN * (C::BN / C::WN), a.n_v, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.sum, a.read_sum, a.write_sum,
+                  a.grad_w, [](int r) { return r; });
 }
 
 // Slabs of dL/dh added in order, rounded, to the tokens' own rows.
@@ -343,14 +307,25 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4* out, int64_t n) {
 size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// Which forms a piece takes, of dz and of the products.
+enum Form { kRing, kMid128, kMidFew, kMid64, kForms };
+struct Size { int bm, bn, bm_w, bn_w, nt; };       // of dz and dL/dh, and of dL/dW
+constexpr Size kSize[kForms] = {{256, 256, 256, 256, 512}, {128, 128, 128, 128, 256}, {128, 64, 128, 128, 256}, {64, 64, 64, 64, 256}};
+
 constexpr int kMaxSlabs = 32, kSlabTiles = 512;
 
-// Vocabulary rows of a piece: as many as kPieceElements allow.
 struct Pieces {
     int64_t rows, n_rows;           // tokens of a piece, pieces
-    int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces
+    int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces: as many as kPieceElements allow
+    Form dz, products;
     int slabs;
 };
+void choose_forms(Pieces& p, int64_t d) {
+    if (p.rows <= 64) p.dz = p.products = kMidFew;
+    if (p.rows < 1024 || p.v < 4096 || d % 64) p.dz = p.products = kMid128;
+    if (p.rows * p.v < 4000000 || d < 128) p.dz = p.products = kMid64;
+}
+int64_t tiles_of(int64_t n, int64_t m, int bn, int bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); }
 Pieces pieces(int64_t T, int64_t V, int64_t d) {
     Pieces p;
     p.n_rows = (T + kPieceRows - 1) / kPieceRows;
@@ -359,7 +334,9 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
     p.n_v = (all + most - 1) / most;
     p.v = up256((all + p.n_v - 1) / p.n_v);
     p.n_v = (all + p.v - 1) / p.v;
-    const int64_t tiles = up256(p.rows) / 256 * (up256(d) / 256), k64 = p.v / 64;
+    p.dz = p.products = kRing;
+    choose_forms(p, d);
+    const int64_t tiles = tiles_of(p.rows, d, kSize[p.products].bn, kSize[p.products].bm), k64 = p.v / 64;
     int64_t s = kSlabTiles / tiles;
     s = s < kMaxSlabs ? s : kMaxSlabs;
     s = s < k64 / 4 ? s : k64 / 4;
@@ -374,15 +351,14 @@ struct Workspace {
 Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     Workspace w;
     const int64_t rows = T < kPieceRows ? T : kPieceRows, all = up256(rows) * up256(V);
-    const int64_t tiles = up256(rows) / 256 * (up256(d) / 256);
-    const int64_t most_tiles = tiles * kMaxSlabs < kSlabTiles ? tiles * kMaxSlabs : tiles > kSlabTiles ? tiles : kSlabTiles;
+    const int64_t one = rows * d, many = kMaxSlabs * one < kSlabTiles * 65536 ? kMaxSlabs * one : kSlabTiles * int64_t{65536};      // one slab, or kSlabTiles tiles at most
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes); return was; };
     w.n_active = take(4);
     w.g = take(rows * 4), w.lse = take(rows * 4), w.target = take(rows * 4), w.row = take(rows * 4);
     w.H = take(up256(rows) * d * 2);
     w.dz = take((all < kPieceElements ? all : kPieceElements) * 2);
-    w.slabs = take(most_tiles * 65536 * 4);
+    w.slabs = take((one > many ? one : many) * 4);
     w.sum = take(lm_head && T > kPieceRows ? V * d * 4 : 0);
     w.bytes = at;
     return w;
@@ -390,9 +366,38 @@ Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
 
 bool sizes_ok(int64_t T, int64_t V, int64_t d) { return T >= 0 && T < (int64_t{1} << 40) && V >= 1 && V <= (1 << 24) && d >= 8 && d % 8 == 0 && d <= 16384; }
 
+template <class F>
+bool dz_of(unsigned grid, const Grad& a, hipStream_t st) {
+    static arrol_device_flags ok;
+    if (!arrol_allow_lds(&dz_kernel<F>, F::C::LDS_BYTES, ok)) return false;
+    arrol_launch(dz_kernel<F>, dim3(grid), dim3(F::C::NT), F::C::LDS_BYTES, st, a);
+    return true;
+}
+template <class FH, class FW>
+bool products_of(unsigned grid, const Grad& a, hipStream_t st) {
+    constexpr int kBytes = FH::C::LDS_BYTES > FW::C::LDS_BYTES ? FH::C::LDS_BYTES : FW::C::LDS_BYTES;
+    static_assert(FH::C::NT == FW::C::NT, "one launch");
+    static arrol_device_flags ok;
+    if (!arrol_allow_lds(&products_kernel<FH, FW>, kBytes, ok)) return false;
+    arrol_launch(products_kernel<FH, FW>, dim3(grid), dim3(FH::C::NT), kBytes, st, a);
+    return true;
+}
+bool launch_dz(Form f, unsigned grid, const Grad& a, hipStream_t st) {
+    return f == kRing ? dz_of<Ring>(grid, a, st) : f == kMid128 ? dz_of<Mid128>(grid, a, st) : f == kMidFew ? dz_of<MidFew>(grid, a, st) : dz_of<Mid64>(grid, a, st);
+}
+bool launch_products(Form f, unsigned grid, const Grad& a, hipStream_t st) {
+    return f == kRing ? products_of<Ring, Ring>(grid, a, st) : f == kMid128 ? products_of<Mid128, Mid128>(grid, a, st)
+         : f == kMidFew ? products_of<MidFew, Mid128>(grid, a, st) : products_of<Mid64, Mid64>(grid, a, st);
+}
+
 unsigned rounded(int64_t n) { return static_cast<unsigned>((n + kXcds - 1) / kXcds * kXcds); }
 
 }  // namespace
+
+static int refused() {
+    arrol_launch_status();      // empties the slot of earlier launches
+    return ARROL_EHIP;
+}
 
 extern "C" size_t arrol_logprob_grad_workspace_bytes(int64_t T, int32_t V, int32_t d, int32_t want_lm_head) {
     return sizes_ok(T, V, d) && T > 0 ? workspace(T, V, d, want_lm_head != 0).bytes : 0;
@@ -414,10 +419,6 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
     }
     const Workspace ws = workspace(T, V, d, grad_lm_head != nullptr);
     if (!workspace_ || !arrol_aligned16(workspace_) || workspace_bytes < ws.bytes) return ARROL_EWORKSPACE;
-    static arrol_device_flags ring_ok, general_ok, products_ok;
-    if (!arrol_allow_lds(&dz_ring_kernel, Tile::LDS_BYTES, ring_ok) || !arrol_allow_lds(&dz_kernel, Tile::LDS_BYTES, general_ok) ||
-        !arrol_allow_lds(&products_kernel, Tile::LDS_BYTES, products_ok))
-        return ARROL_EHIP;
     auto* base = static_cast<unsigned char*>(workspace_);
     const Pieces p = pieces(T, V, d);
     Grad a = {};
@@ -426,7 +427,7 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
     a.target = reinterpret_cast<int32_t*>(base + ws.target), a.row = reinterpret_cast<int32_t*>(base + ws.row);
     a.n_active = reinterpret_cast<int32_t*>(base + ws.n_active);
     a.d = d;
-    const int64_t n_db = up256(d) / 256;
+    const Size& size = kSize[p.products];
     for (int64_t piece = 0; piece < p.n_rows; ++piece) {
         const int64_t t0 = piece * p.rows, rows = T - t0 < p.rows ? T - t0 : p.rows;
         Gather g;
@@ -436,26 +437,23 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
         g.n_active = const_cast<int32_t*>(a.n_active), g.T = static_cast<int>(rows), g.V = V, g.d = d;
         arrol_launch(gather_kernel, dim3(static_cast<unsigned>((rows + kGatherRows - 1) / kGatherRows)), dim3(256), 0, st, g);
         const bool direct = p.slabs == 1 && p.n_v == 1;
-        const int64_t n_tb = up256(rows) / 256;
         a.slab_stride = rows * d;
         a.slabs = direct ? nullptr : reinterpret_cast<float*>(base + ws.slabs);
         a.grad_hidden = g.grad_hidden;
         for (int64_t q = 0; q < p.n_v; ++q) {
-            const int64_t v0 = q * p.v, n_v = V - v0 < p.v ? V - v0 : p.v, n_vt = up256(n_v) / 256;
+            const int64_t v0 = q * p.v, n_v = V - v0 < p.v ? V - v0 : p.v;
             a.W = static_cast<const uint16_t*>(lm_head) + v0 * d, a.v0 = static_cast<int>(v0), a.n_v = static_cast<int>(n_v), a.v_stride = static_cast<int>(p.v);
-            const dim3 grid(rounded(n_tb * n_vt));
-            if (d % 64 == 0) arrol_launch(dz_ring_kernel, grid, dim3(Tile::NT), Tile::LDS_BYTES, st, a);
-            else arrol_launch(dz_kernel, grid, dim3(Tile::NT), Tile::LDS_BYTES, st, a);
+            if (!launch_dz(p.dz, rounded(tiles_of(rows, n_v, kSize[p.dz].bn, kSize[p.dz].bm)), a, st)) return refused();
             a.n_slabs = p.slabs, a.k64_per_slab = static_cast<int>((p.v / 64 + p.slabs - 1) / p.slabs), a.add = q > 0;
-            a.grid_h = grad_hidden ? static_cast<int>(rounded(n_tb * n_db * p.slabs)) : 0;
+            a.grid_h = grad_hidden ? static_cast<int>(rounded(tiles_of(rows, d, size.bn, size.bm) * p.slabs)) : 0;
             int64_t grid_w = 0;
             if (grad_lm_head || lm_head_sum) {
-                grid_w = rounded(n_vt * n_db);
+                grid_w = rounded(tiles_of(n_v, d, size.bn_w, size.bm_w));
                 a.sum = (lm_head_sum ? lm_head_sum : reinterpret_cast<float*>(base + ws.sum)) + v0 * d;
                 a.grad_w = grad_lm_head ? static_cast<uint16_t*>(grad_lm_head) + v0 * d : nullptr;
                 a.read_sum = lm_head_sum || piece > 0, a.write_sum = lm_head_sum || piece + 1 < p.n_rows;
             }
-            arrol_launch(products_kernel, dim3(static_cast<unsigned>(a.grid_h + grid_w)), dim3(Tile::NT), Tile::LDS_BYTES, st, a);
+            if (!launch_products(p.products, static_cast<unsigned>(a.grid_h + grid_w), a, st)) return refused();
         }
         if (grad_hidden && !direct) {
             const int64_t blocks = (rows * (d / 4) + 255) / 256;
