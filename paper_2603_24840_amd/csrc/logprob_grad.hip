@@ -26,7 +26,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kXcds = 8, kRound = 256;
 constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
-constexpr int kGatherRows = 16;
 
 // The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
 struct Ring {
@@ -42,7 +41,7 @@ struct Mid {
 };
 typedef Mid<128, 128, 2> Mid128;
 typedef Mid<128, 64, 3> MidFew;
-typedef Mid<64, 64, 4> Mid64;
+typedef Mid<64, 64, 3> Mid64;
 
 struct Grad {
     const uint16_t* W;              // of the vocabulary piece
@@ -85,7 +84,7 @@ __device__ __forceinline__ void patch(int64_t pos, int rows, int cols, int most,
 
 __device__ __forceinline__ bool takes_part(float g, int32_t target, int V) { return g != 0.f && target >= 0 && target < V; }      // NaN does
 
-// Tokens that take part, packed.  A workgroup has kGatherRows tokens and counts those before them itself.
+// Tokens that take part, packed.  A workgroup has ROWS tokens, a wavefront ROWS / 4 of them, and counts those before them itself.
 struct Gather {
     const uint16_t* hidden;
     const int32_t* targets;
@@ -95,37 +94,62 @@ struct Gather {
     int32_t *target, *row, *n_active;
     int T, V, d;
 };
+template <int ROWS>
 __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
+    constexpr int kInFlight = 8;
     __shared__ int before[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kGatherRows;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), t0 = blockIdx.x * ROWS;
+    const bool in = lane < ROWS && t0 + lane < a.T;
+    const float g = in ? a.grad_logp[t0 + lane] : 0.f;
+    const int32_t y = in ? a.targets[t0 + lane] : -1;
     int n = 0;
-    for (int t = tid; t < t0; t += 256) n += __popcll(__ballot(takes_part(a.grad_logp[t], a.targets[t], a.V)));       // t0 is a multiple of 16: lanes beyond it are off
-    // a wavefront's lanes of one iteration are counted by each active one: lane 0 is active whenever any is
+    for (int base = 0; base < t0; base += 256 * kInFlight) {
+        float gs[kInFlight];
+        int32_t ys[kInFlight];
+#pragma unroll
+        for (int i = 0; i < kInFlight; ++i) {
+            const int t = base + i * 256 + tid;
+            gs[i] = a.grad_logp[t < t0 ? t : 0];
+            ys[i] = t < t0 ? a.targets[t] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kInFlight; ++i) n += __popcll(__ballot(takes_part(gs[i], ys[i], a.V)));
+    }
     if (lane == 0) before[wave] = n;
-    const int mine = t0 + lane;
-    const bool in = lane < kGatherRows && mine < a.T;
-    const float g = in ? a.grad_logp[mine] : 0.f;
-    const int32_t y = in ? a.targets[mine] : -1;
-    const uint64_t active = __ballot(in && takes_part(g, y, a.V));
+    const uint64_t active = __ballot(takes_part(g, y, a.V));      // of the workgroup's tokens, in every wavefront
     __syncthreads();
     const int first = before[0] + before[1] + before[2] + before[3];
     if (wave == 0 && ((active >> lane) & 1)) {
         const int r = first + __popcll(active & ((uint64_t{1} << lane) - 1));
         a.g[r] = g;
-        a.lse_out[r] = a.lse[mine];
+        a.lse_out[r] = a.lse[t0 + lane];
         a.target[r] = y;
-        a.row[r] = mine;
+        a.row[r] = t0 + lane;
     }
-    if (tid == 0 && t0 + kGatherRows >= a.T) *a.n_active = first + __popcll(active);
-    const int r = tid / 16, c0 = tid % 16, vecs = a.d / 8;
-    if (t0 + r >= a.T) return;
-    const uint16_t* from = a.hidden + static_cast<int64_t>(t0 + r) * a.d;
-    if ((active >> r) & 1) {
-        uint16_t* to = a.H + static_cast<int64_t>(first + __popcll(active & ((uint64_t{1} << r) - 1))) * a.d;
-        for (int c = c0; c < vecs; c += 16) *reinterpret_cast<u32x4*>(to + c * 8) = *reinterpret_cast<const u32x4*>(from + c * 8);
-    } else if (a.grad_hidden) {
-        uint16_t* to = a.grad_hidden + static_cast<int64_t>(t0 + r) * a.d;
-        for (int c = c0; c < vecs; c += 16) *reinterpret_cast<u32x4*>(to + c * 8) = u32x4{0, 0, 0, 0};
+    if (tid == 0 && t0 + ROWS >= a.T) *a.n_active = first + __popcll(active);
+    const int vecs = a.d / 8;
+#pragma unroll
+    for (int i = 0; i < ROWS / 4; ++i) {
+        const int r = wave * (ROWS / 4) + i, t = t0 + r;
+        if (t >= a.T) break;
+        const bool on = (active >> r) & 1;
+        const uint16_t* from = a.hidden + static_cast<int64_t>(t) * a.d;
+        uint16_t* to = on ? a.H + static_cast<int64_t>(first + __popcll(active & ((uint64_t{1} << r) - 1))) * a.d
+                          : a.grad_hidden ? a.grad_hidden + static_cast<int64_t>(t) * a.d : nullptr;
+        if (!to) continue;
+        for (int c0 = lane; c0 < vecs; c0 += ARROL_WAVE * kInFlight) {
+            u32x4 x[kInFlight];
+#pragma unroll
+            for (int k = 0; k < kInFlight; ++k) {
+                const int c = c0 + k * ARROL_WAVE;
+                x[k] = on && c < vecs ? *reinterpret_cast<const u32x4*>(from + c * 8) : u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int k = 0; k < kInFlight; ++k) {
+                const int c = c0 + k * ARROL_WAVE;
+                if (c < vecs) *reinterpret_cast<u32x4*>(to + c * 8) = x[k];
+            }
+        }
     }
 }
 
@@ -290,12 +314,20 @@ __global__ __launch_bounds__(FH::C::NT) void products_kernel(Grad a) {
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ slabs, int64_t slab_stride, int n_slabs, const int32_t* __restrict__ row, const int32_t* __restrict__ n_active,
                                                    int d, uint16_t* __restrict__ grad_hidden) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    constexpr int kInFlight = 8;
     const int vecs = d / 4;
     const int64_t total = static_cast<int64_t>(*n_active) * vecs;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<int64_t>(t) * vecs) * 4;
-        f32x4 x = *reinterpret_cast<const f32x4*>(slabs + i * 4);
-        for (int s = 1; s < n_slabs; ++s) x += *reinterpret_cast<const f32x4*>(slabs + s * slab_stride + i * 4);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int s0 = 0; s0 < n_slabs; s0 += kInFlight) {
+            f32x4 y[kInFlight];
+#pragma unroll
+            for (int s = 0; s < kInFlight; ++s) y[s] = *reinterpret_cast<const f32x4*>(slabs + (s0 + s < n_slabs ? s0 + s : s0) * slab_stride + i * 4);
+#pragma unroll
+            for (int s = 0; s < kInFlight; ++s)
+                if (s0 + s < n_slabs) x += y[s];
+        }
         *reinterpret_cast<bf16x4*>(grad_hidden + static_cast<int64_t>(row[t]) * d + c) = __builtin_convertvector(x, bf16x4);
     }
 }
@@ -307,25 +339,58 @@ __global__ __launch_bounds__(256) void zero_kernel(u32x4* out, int64_t n) {
 size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
-// Which forms a piece takes, of dz and of the products.
+// Which forms a piece takes, of dz and of the products: those whose estimated times are the smallest.  Measured, microseconds: what a tile costs beside its K64
+// steps, a step where the chip is full (of every one of the `per_unit` workgroups that a compute unit has at a time) and a step where it is not.  1,024 x 32,000 x 2048:
+// dz 114 / 138 / 179 / 206, products 250 / 242 / 286 / 407; 318 x 4,096 x 256: 14.5 / 9.1 / 6.5 / 6.9 and 17.6 / 8.7 / 7.8 / 7.7; 16 x 151,936 x 2048 (LM head from memory, and
+// its gradient to it): 249 / 221 / 189 / 177 and 306 / 328 / 331 / 330.
 enum Form { kRing, kMid128, kMidFew, kMid64, kForms };
-struct Size { int bm, bn, bm_w, bn_w, nt; };       // of dz and dL/dh, and of dL/dW
-constexpr Size kSize[kForms] = {{256, 256, 256, 256, 512}, {128, 128, 128, 128, 256}, {128, 64, 128, 128, 256}, {64, 64, 64, 64, 256}};
+struct Size {
+    int bm, bn, bm_w, bn_w;         // of dz and dL/dh, and of dL/dW
+    int per_unit;
+    double tile, step, lone, tile_w, step_w, lone_w;
+};
+constexpr Size kSize[kForms] = {{256, 256, 256, 256, 1, 8.7, 1.45, 1.1, 10.0, 1.55, 1.1}, {128, 128, 128, 128, 2, 4.8, 0.95, 0.53, 4.2, 0.95, 0.53},
+                                {128, 64, 128, 128, 2, 1.7, 0.66, 0.33, 4.2, 0.95, 0.53}, {64, 64, 64, 64, 3, 1.4, 0.57, 0.2, 2.0, 0.6, 0.2}};
 
-constexpr int kMaxSlabs = 32, kSlabTiles = 512;
+constexpr int kMaxSlabs = 32, kSlabTiles = 512;     // of 256 x 256
+constexpr double kJoin = 2.5, kJoinBytes = 3e6;      // microseconds; bytes a microsecond
 
 struct Pieces {
     int64_t rows, n_rows;           // tokens of a piece, pieces
     int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces: as many as kPieceElements allow
     Form dz, products;
-    int slabs;
+    int slabs;                      // parts of the vocabulary piece that dL/dh's K extent is cut into
 };
-void choose_forms(Pieces& p, int64_t d) {
-    if (p.rows <= 64) p.dz = p.products = kMidFew;
-    if (p.rows < 1024 || p.v < 4096 || d % 64) p.dz = p.products = kMid128;
-    if (p.rows * p.v < 4000000 || d < 128) p.dz = p.products = kMid64;
-}
 int64_t tiles_of(int64_t n, int64_t m, int bn, int bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); }
+
+double dz_time(const Size& f, int64_t rows, int64_t v, int64_t d) {
+    const double steps = static_cast<double>((d + 63) / 64), r = static_cast<double>(tiles_of(rows, v, f.bn, f.bm)) / (256 * f.per_unit);
+    if (r <= 1) return f.tile + steps * (f.lone > f.step * r ? f.lone : f.step * r);
+    const double up = static_cast<double>(static_cast<int64_t>(r + 0.999));
+    return (up < r + 0.5 ? up : r + 0.5) * (f.tile + steps * f.step);       // of many rounds the last one's workgroups start early
+}
+double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, int slabs) {
+    const double n_h = static_cast<double>(tiles_of(rows, d, f.bn, f.bm) * slabs), n_w = static_cast<double>(tiles_of(v, d, f.bn_w, f.bm_w));
+    const double k_h = static_cast<double>((v / 64 + slabs - 1) / slabs), k_w = static_cast<double>((rows + 63) / 64), places = 256.0 * f.per_unit;
+    const double all = (n_h * (f.tile + k_h * f.step) + n_w * (f.tile_w + k_w * f.step_w)) / places;
+    const double lone_h = f.tile + k_h * f.lone, lone_w = f.tile_w + k_w * f.lone_w, longest = lone_h > lone_w ? lone_h : lone_w;
+    return n_h + n_w <= places ? (all > longest ? all : longest) : all + longest / 2;
+}
+void choose_forms(Pieces& p, int64_t d) {
+    double best_dz = 1e30, best = 1e30;
+    for (int f = 0; f < kForms; ++f) {
+        const Size& size = kSize[f];
+        const double dz = f == kRing && d % 64 ? 1e30 : dz_time(size, p.rows, p.v, d);
+        if (dz < best_dz) best_dz = dz, p.dz = static_cast<Form>(f);
+        const int64_t tile = static_cast<int64_t>(size.bm) * size.bn, tiles = tiles_of(p.rows, d, size.bn, size.bm), k64 = p.v / 64;
+        for (int s = 1; s <= kMaxSlabs; s += s < 4 ? 1 : s / 4) {
+            if (s > 1 && (s > k64 / 2 || s * tiles * tile > kSlabTiles * int64_t{65536})) break;
+            const double join = s > 1 || p.n_v > 1 ? kJoin + 4.0 * s * p.rows * d / kJoinBytes : 0.0;
+            const double t = products_time(size, p.rows, p.v, d, s) + join;
+            if (t < best) best = t, p.products = static_cast<Form>(f), p.slabs = s;
+        }
+    }
+}
 Pieces pieces(int64_t T, int64_t V, int64_t d) {
     Pieces p;
     p.n_rows = (T + kPieceRows - 1) / kPieceRows;
@@ -334,13 +399,7 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
     p.n_v = (all + most - 1) / most;
     p.v = up256((all + p.n_v - 1) / p.n_v);
     p.n_v = (all + p.v - 1) / p.v;
-    p.dz = p.products = kRing;
     choose_forms(p, d);
-    const int64_t tiles = tiles_of(p.rows, d, kSize[p.products].bn, kSize[p.products].bm), k64 = p.v / 64;
-    int64_t s = kSlabTiles / tiles;
-    s = s < kMaxSlabs ? s : kMaxSlabs;
-    s = s < k64 / 4 ? s : k64 / 4;
-    p.slabs = static_cast<int>(s > 1 ? s : 1);
     return p;
 }
 
@@ -435,7 +494,8 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
         g.H = const_cast<uint16_t*>(a.H), g.grad_hidden = grad_hidden ? static_cast<uint16_t*>(grad_hidden) + t0 * d : nullptr;
         g.g = const_cast<float*>(a.g), g.lse_out = const_cast<float*>(a.lse), g.target = const_cast<int32_t*>(a.target), g.row = const_cast<int32_t*>(a.row);
         g.n_active = const_cast<int32_t*>(a.n_active), g.T = static_cast<int>(rows), g.V = V, g.d = d;
-        arrol_launch(gather_kernel, dim3(static_cast<unsigned>((rows + kGatherRows - 1) / kGatherRows)), dim3(256), 0, st, g);
+        if (rows <= 1024) arrol_launch(gather_kernel<4>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, g);
+        else arrol_launch(gather_kernel<16>, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(256), 0, st, g);
         const bool direct = p.slabs == 1 && p.n_v == 1;
         a.slab_stride = rows * d;
         a.slabs = direct ? nullptr : reinterpret_cast<float*>(base + ws.slabs);

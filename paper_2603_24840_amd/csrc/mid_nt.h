@@ -105,15 +105,15 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
     int issued = 0;
     const int chunk = (lane & 7) ^ ((lane >> 3) & 6);         // of every load row by row
     const unsigned past = chunk < tail ? 0 : static_cast<unsigned>(chunk - tail + 1) * 16;
-    auto issue = [&]() {                     // past the last step its lines again, into a stage that nobody reads
-        const unsigned back = kTail && issued >= steps - 1 ? past : 0;
+    auto issue = [&]() {
+        if (issued >= steps) return;
+        const unsigned back = kTail && issued == steps - 1 ? past : 0;
         a.issue(dst, wave, back);
         b.issue(dst + BM * 128, wave, back);
         dst = dst == lds0 + (NS - 1) * C::STAGE_BYTES ? lds0 : dst + C::STAGE_BYTES;
-        if (++issued < steps) {
-            a.advance();
-            b.advance();
-        }
+        ++issued;
+        a.advance();
+        b.advance();
     };
     // fragments: row by row, lane -> row lane % 16, chunk lane / 16 (+ 4 for the step's second half); K-major, lane 16 lq + 4 e + q addresses row 8 lq + 4 h2 + e
     // (+ 32), values 4 q .. + 3 (block i: 16 i on, an exclusive or of the chunk)
@@ -136,8 +136,9 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
     for (int s = 0; s < NS - 1; ++s) issue();
     int slot = 0;
     for (int s = 0; s < steps; ++s) {
-        // this step has landed (the NS - 2 after it may fly), for every wavefront, and all have read the one before
-        wait_vmcnt<(NS - 2) * C::LOADS>();
+        // this step has landed (the NS - 2 after it, where there are so many, may fly), for every wavefront, and all have read the one before
+        if (NS > 2 && steps - s >= NS - 1) wait_vmcnt<(NS - 2) * C::LOADS>();
+        else wait_vmcnt<0>();
         __syncthreads();
         issue();
         const unsigned char* st = lds + slot;
@@ -161,7 +162,6 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
                 for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
         }
     }
-    wait_vmcnt<0>();
 }
 
 }  // namespace mid_nt
