@@ -28,20 +28,16 @@ constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
 
 // The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
-struct Ring {
-    typedef ring_nt::RingTile<256, 256, 2, 4> C;
-    template <bool B_KMAJOR, bool A_KMAJOR>
-    __device__ static __forceinline__ void walk(const ring_nt::Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int = 8) { ring_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc); }
-};
-template <int BM, int BN, int NS>
-struct Mid {
-    typedef mid_nt::Tile<BM, BN, 2, 2, NS> C;
-    template <bool B_KMAJOR, bool A_KMAJOR>
-    __device__ static __forceinline__ void walk(const ring_nt::Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8) { mid_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc, tail); }
-};
+typedef ring_nt::RingTile<256, 256, 2, 4> Ring;
+template <int BM, int BN, int NS> using Mid = mid_nt::Tile<BM, BN, 2, 2, NS>;
 typedef Mid<128, 128, 2> Mid128;
 typedef Mid<128, 64, 3> MidFew;
 typedef Mid<64, 64, 3> Mid64;
+template <class C, bool B_KMAJOR, bool A_KMAJOR>
+__device__ __forceinline__ void multiply(const ring_nt::Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8) {
+    if constexpr (std::is_same_v<C, Ring>) ring_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc);
+    else mid_nt::walk<C, B_KMAJOR, A_KMAJOR>(w, lds, acc, tail);
+}
 
 struct Grad {
     const uint16_t* W;              // of the vocabulary piece
@@ -53,31 +49,29 @@ struct Grad {
     int d, v0, n_v;                 // first row of the piece, and how many
     int v_stride;                   // of dz, a multiple of 256
     // dL/dh
-    float* slabs;                   // [n_slabs][slab rows][d], NULL: straight to grad_hidden
+    float* slabs;                   // [parts][slab rows][d], NULL: straight to grad_hidden
     int64_t slab_stride;
-    int n_slabs, k64_per_slab, add; // add: to what the slabs hold of pieces before
+    int k64_per_slab, add;          // add: to what the slabs hold of pieces before
     uint16_t* grad_hidden;
-    int grid_h;                     // workgroups of dL/dh
+    int grid_h, grid_w;             // workgroups of dL/dh and of dL/dW, 0 where not wanted
     // dL/dW of the piece
     float* sum;                     // fp32 sums, read and / or written
     uint16_t* grad_w;
     int read_sum, write_sum;
 };
 
-// Place in a work order in which every round of 256 workgroups gives each XCD (workgroup ids congruent mod 8) 32 that follow each other.  false: none.
-__device__ __forceinline__ bool place(int id, int64_t total, int64_t& pos) {
-    const int64_t round0 = id / kRound * kRound, left = total - round0;
-    const int in_round = left < kRound ? static_cast<int>(left) : kRound, within = id % kRound;
-    if (in_round <= 0) return false;
+// Place in a work order in which every round of 256 workgroups gives each XCD (workgroup ids congruent mod 8) 32 that follow each other.  -1: none.
+__device__ __forceinline__ int place(int id, int total) {
+    const int round0 = id / kRound * kRound, left = total - round0;
+    const int in_round = left < kRound ? left : kRound, within = id % kRound;
+    if (in_round <= 0) return -1;
     const int per_xcd = (in_round + kXcds - 1) / kXcds, p = within % kXcds * per_xcd + within / kXcds;
-    pos = round0 + p;
-    return within / kXcds < per_xcd && p < in_round;
+    return within / kXcds < per_xcd && p < in_round ? round0 + p : -1;
 }
 // Tile (row, col) of `rows` x `cols` at a position: bands of up to `most` rows, through which the columns run, so that neighbours share operands.
-__device__ __forceinline__ void patch(int64_t pos, int rows, int cols, int most, int& row, int& col) {
+__device__ __forceinline__ void patch(int pos, int rows, int cols, int most, int& row, int& col) {
     const int bands = (rows + most - 1) / most, size = (rows + bands - 1) / bands;
-    const int b = static_cast<int>(pos / (static_cast<int64_t>(size) * cols));
-    const int r = static_cast<int>(pos - static_cast<int64_t>(b) * size * cols), mine = rows - b * size < size ? rows - b * size : size;
+    const int b = pos / (size * cols), r = pos - b * size * cols, mine = rows - b * size < size ? rows - b * size : size;
     col = __builtin_amdgcn_readfirstlane(r / mine);      // in scalar registers, as the walk wants its bases
     row = __builtin_amdgcn_readfirstlane(b * size + r - col * mine);
 }
@@ -169,64 +163,96 @@ struct Lane {
     __device__ __forceinline__ int place(int i) const { return 16 * (i + (lq & 1)) + 4 * (lq & 2); }      // of exchange()'s values
 };
 
+// What the lane's tokens bring with them: of token 16 j + lane % 16 of the wavefront's part.  Fetched before the walk.
 template <class C>
-__device__ __forceinline__ bool dz_tile(const Grad& a, int n_active, int& vt, int& tb) {
-    const int n_tb = (n_active + C::BN - 1) / C::BN, n_vt = (a.n_v + C::BM - 1) / C::BM;
-    int64_t pos;
-    if (!place(blockIdx.x, static_cast<int64_t>(n_tb) * n_vt, pos)) return false;
-    patch(pos, n_tb, n_vt, 6, tb, vt);
-    return true;
-}
+struct Tokens {
+    float g[C::TJ], at[C::TJ];      // at: -lse log2 e
+    int target[C::TJ];              // -1: none
+    __device__ __forceinline__ Tokens(const Grad& a, const Lane& me, int tb, int n_active) {
+#pragma unroll
+        for (int j = 0; j < C::TJ; ++j) {
+            const int t = tb * C::BN + me.wave % C::WN * (C::BN / C::WN) + j * 16 + me.l15;
+            const bool live = t < n_active;
+            g[j] = live ? a.g[t] : 0.f;
+            at[j] = live ? -a.lse[t] * kLog2e : 0.f;
+            target[j] = live ? a.target[t] : -1;
+        }
+    }
+};
 
 // acc[i][j][v] = z of vocabulary row 16 i + 4 (lane / 16) + v and token 16 j + lane % 16 of the wavefront's part of the tile.  dz of rows past the vocabulary and of
 // tokens past the last are zeros: the products' K extents are whole steps of 64.
-template <class F>
-__global__ __launch_bounds__(F::C::NT) void dz_kernel(Grad a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    typedef typename F::C C;
-    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
-    int vt, tb;
-    if (!dz_tile<C>(a, n_active, vt, tb)) return;
-    const Lane me;
-    ring_nt::Walk w = {};
-    const int64_t row = static_cast<int64_t>(a.d) * 2;
-    w.a_base = reinterpret_cast<const char*>(a.W) + vt * C::BM * row;
-    w.b_base = reinterpret_cast<const char*>(a.H) + tb * C::BN * row;
-    w.a_stride = w.b_stride = static_cast<unsigned>(row);
-    w.a_rows = a.n_v - vt * C::BM;
-    w.b_rows = n_active - tb * C::BN < C::BN ? n_active - tb * C::BN : C::BN;
-    w.n_k64 = (a.d + 63) / 64;
-    f32x4 acc[C::TI][C::TJ];
-    F::template walk<false, false>(w, lds, acc, (a.d & 63) ? (a.d & 63) / 8 : 8);
+template <class C>
+__device__ __forceinline__ void store_dz(const Grad& a, const Lane& me, const Tokens<C>& tokens, const f32x4 (&acc)[C::TI][C::TJ], int vt, int tb, int n_active) {
     const int v_first = vt * C::BM + me.wave / C::WN * (C::BM / C::WM), t_first = tb * C::BN + me.wave % C::WN * (C::BN / C::WN);
-    const bool hangs = v_first + C::BM / C::WM > a.n_v;
+    const bool edge = v_first + C::BM / C::WM > a.n_v || t_first + C::BN / C::WN > n_active;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
         const int t = t_first + j * 16 + me.l15;
-        const bool live = t < n_active;
-        const float g = live ? a.g[t] : 0.f, at = live ? -a.lse[t] * kLog2e : 0.f;
-        const int y = live ? a.target[t] - a.v0 - v_first - 4 * me.lq : -1;        // of this lane's rows: 16 i + v
-        const bool mine = y >= 0 && y < C::BM / C::WM && (y & 12) == 0;
+        const float g = tokens.g[j], at = tokens.at[j];
+        const int y = tokens.target[j] - a.v0 - v_first - 4 * me.lq;        // of this lane's rows: 16 i + v
+        const bool mine = t < n_active && y >= 0 && y < C::BM / C::WM && (y & 12) == 0;
         uint16_t* to = a.dz + static_cast<int64_t>(t) * a.v_stride + v_first;
-        auto dz = [&](int i) {
+        auto plain = [&](int i) {
             f32x4 x;
 #pragma unroll
             for (int v = 0; v < 4; ++v) x[v] = -g * __builtin_amdgcn_exp2f(fmaf(acc[i][j][v], kLog2e, at));
-            if (__any(mine && y >> 4 == i)) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (mine && y == 16 * i + v) x[v] += g;
-            }
-            if (hangs) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    if (v_first + 16 * i + 4 * me.lq + v >= a.n_v) x[v] = 0.f;
-            }
-            return live ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+            return x;
         };
+        auto whole = [&](int i) {
+            f32x4 x = plain(i);
 #pragma unroll
-        for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(to + me.place(i)) = exchange(dz(i), dz(i + 1));
+            for (int v = 0; v < 4; ++v) {
+                if (mine && y == 16 * i + v) x[v] += g;
+                if (t >= n_active || v_first + 16 * i + 4 * me.lq + v >= a.n_v) x[v] = 0.f;
+            }
+            return x;
+        };
+        if (edge || __any(mine)) {
+#pragma unroll
+            for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(to + me.place(i)) = exchange(whole(i), whole(i + 1));
+        } else {
+#pragma unroll
+            for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(to + me.place(i)) = exchange(plain(i), plain(i + 1));
+        }
     }
+}
+
+// dz tile (vt, tb).
+template <class C>
+struct DzTiles {
+    const Grad& a;
+    const int n_active, n_tb, n_vt;
+    __device__ __forceinline__ DzTiles(const Grad& a, int n) : a(a), n_active(n), n_tb((n + C::BN - 1) / C::BN), n_vt((a.n_v + C::BM - 1) / C::BM) {}
+    __device__ __forceinline__ int total() const { return n_tb * n_vt; }
+    __device__ __forceinline__ void at(int pos, int& vt, int& tb) const { patch(pos, n_tb, n_vt, 6, tb, vt); }
+    __device__ __forceinline__ ring_nt::Walk walk(int vt, int tb) const {
+        ring_nt::Walk w = {};
+        const int64_t row = static_cast<int64_t>(a.d) * 2;
+        w.a_base = reinterpret_cast<const char*>(a.W) + vt * C::BM * row;
+        w.b_base = reinterpret_cast<const char*>(a.H) + tb * C::BN * row;
+        w.a_stride = w.b_stride = static_cast<unsigned>(row);
+        w.a_rows = a.n_v - vt * C::BM;
+        w.b_rows = n_active - tb * C::BN < C::BN ? n_active - tb * C::BN : C::BN;
+        w.n_k64 = (a.d + 63) / 64;
+        return w;
+    }
+};
+
+template <class C>
+__global__ __launch_bounds__(C::NT) void dz_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    const DzTiles<C> tiles(a, n_active);
+    const int pos = place(blockIdx.x, tiles.total());
+    if (pos < 0) return;
+    int vt, tb;
+    tiles.at(pos, vt, tb);
+    const Lane me;
+    const Tokens<C> tokens(a, me, tb, n_active);
+    f32x4 acc[C::TI][C::TJ];
+    multiply<C, false, false>(tiles.walk(vt, tb), lds, acc, (a.d & 63) ? (a.d & 63) / 8 : 8);
+    store_dz<C>(a, me, tokens, acc, vt, tb, n_active);
 }
 
 // The epilogue of both products: acc[i][j][v] belongs to column c0 + 16 i + 4 lq + v of row r0 + 16 j + l15.  sum: fp32, read and / or written; else bf16.
@@ -258,56 +284,90 @@ __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C:
     }
 }
 
-template <class FH, class FW>
-__global__ __launch_bounds__(FH::C::NT) void products_kernel(Grad a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
-    const Lane me;
-    const int64_t row = static_cast<int64_t>(a.d) * 2;
-    ring_nt::Walk w = {};
-    int64_t pos;
-    int at, db;
-    if (static_cast<int>(blockIdx.x) < a.grid_h) {
-        // dL/dh: columns of W, which is read down its rows, times tokens' rows of dz; K = the vocabulary piece or a part of it
-        typedef typename FH::C C;
-        const int n_tb = (n_active + C::BN - 1) / C::BN, n_db = (a.d + C::BM - 1) / C::BM;
-        const int64_t tiles = static_cast<int64_t>(n_tb) * n_db;
-        if (!place(blockIdx.x, tiles * a.n_slabs, pos)) return;
-        const int s = __builtin_amdgcn_readfirstlane(static_cast<int>(pos / tiles));
-        patch(pos - s * tiles, n_db, n_tb, 8, db, at);
-        const int n_k64 = (a.n_v + 63) / 64, k_lo = s * a.k64_per_slab, k_hi = k_lo + a.k64_per_slab < n_k64 ? k_lo + a.k64_per_slab : n_k64;
+// dL/dh: columns of W, which is read down its rows, times tokens' rows of dz; K = the vocabulary piece or a part of it.  Tile (s, at, db): part, tokens, columns.
+template <class C>
+struct HiddenTiles {
+    const Grad& a;
+    const int n_active, n_tb, n_db, n_k64, n_parts;
+    __device__ __forceinline__ HiddenTiles(const Grad& a, int n)
+        : a(a), n_active(n), n_tb((n + C::BN - 1) / C::BN), n_db((a.d + C::BM - 1) / C::BM), n_k64((a.n_v + 63) / 64), n_parts((n_k64 + a.k64_per_slab - 1) / a.k64_per_slab) {}
+    __device__ __forceinline__ int total() const { return a.grid_h ? n_tb * n_db * n_parts : 0; }
+    __device__ __forceinline__ void at(int pos, int& s, int& tb, int& db) const {
+        s = __builtin_amdgcn_readfirstlane(pos / (n_tb * n_db));
+        patch(pos - s * n_tb * n_db, n_db, n_tb, 8, db, tb);
+    }
+    __device__ __forceinline__ ring_nt::Walk walk(int s, int tb, int db) const {
+        ring_nt::Walk w = {};
+        const int64_t row = static_cast<int64_t>(a.d) * 2;
+        const int k_lo = s * a.k64_per_slab, k_hi = k_lo + a.k64_per_slab < n_k64 ? k_lo + a.k64_per_slab : n_k64;
         w.a_base = reinterpret_cast<const char*>(a.W) + static_cast<int64_t>(k_lo) * 64 * row + db * C::BM * 2;
         w.a_stride = static_cast<unsigned>(row);
         w.a_rows = a.d - db * C::BM;
         w.a_k_rows = a.n_v - k_lo * 64;
-        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * C::BN * a.v_stride) + static_cast<int64_t>(k_lo) * 128;
+        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(tb) * C::BN * a.v_stride) + static_cast<int64_t>(k_lo) * 128;
         w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
-        w.b_rows = n_active - at * C::BN < C::BN ? n_active - at * C::BN : C::BN;
-        w.n_k64 = k_hi > k_lo ? k_hi - k_lo : 0;
-        f32x4 acc[C::TI][C::TJ];
-        FH::template walk<false, true>(w, lds, acc);
-        store_rows<C>(me, acc, at * C::BN + me.wave % C::WN * (C::BN / C::WN), n_active, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d,
-                      a.slabs + s * a.slab_stride, a.add, a.slabs != nullptr, a.grad_hidden, [&](int t) { return a.row[t]; });
+        w.b_rows = n_active - tb * C::BN < C::BN ? n_active - tb * C::BN : C::BN;
+        w.n_k64 = k_hi - k_lo;
+        return w;
+    }
+    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int s, int tb, int db) const {
+        const Grad& a = this->a;
+        store_rows<C>(me, acc, tb * C::BN + me.wave % C::WN * (C::BN / C::WN), n_active, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.slabs + s * a.slab_stride, a.add,
+                      a.slabs != nullptr, a.grad_hidden, [&](int t) { return a.row[t]; });
+    }
+};
+
+// dL/dW: columns of the hidden states times the piece's rows, both read down the tokens.  Tile (vt, db).
+template <class C>
+struct HeadTiles {
+    const Grad& a;
+    const int n_active, n_vt, n_db;
+    __device__ __forceinline__ HeadTiles(const Grad& a, int n) : a(a), n_active(n), n_vt((a.n_v + C::BN - 1) / C::BN), n_db((a.d + C::BM - 1) / C::BM) {}
+    __device__ __forceinline__ int total() const { return n_vt * n_db; }
+    __device__ __forceinline__ void at(int pos, int& vt, int& db) const { patch(pos, n_db, n_vt, 8, db, vt); }
+    __device__ __forceinline__ ring_nt::Walk walk(int vt, int db) const {
+        ring_nt::Walk w = {};
+        const int64_t row = static_cast<int64_t>(a.d) * 2;
+        w.a_base = reinterpret_cast<const char*>(a.H) + db * C::BM * 2;
+        w.a_stride = static_cast<unsigned>(row);
+        w.a_rows = a.d - db * C::BM;
+        w.a_k_rows = n_active;
+        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(vt) * C::BN);
+        w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
+        w.b_rows = C::BN;                                // v_stride is a multiple of 256, and zeros follow the piece's last row up to a multiple of 64
+        w.n_k64 = (n_active + 63) / 64;
+        w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
+        return w;
+    }
+    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int vt, int db) const {
+        store_rows<C>(me, acc, vt * C::BN + me.wave % C::WN * (C::BN / C::WN), a.n_v, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.sum, a.read_sum, a.write_sum,
+                      a.grad_w, [](int r) { return r; });
+    }
+};
+
+template <class CH, class CW>
+__global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    if (static_cast<int>(blockIdx.x) < a.grid_h) {
+        const HiddenTiles<CH> tiles(a, n_active);
+        const int pos = place(blockIdx.x, tiles.total());
+        if (pos < 0) return;
+        int s, tb, db;
+        tiles.at(pos, s, tb, db);
+        f32x4 acc[CH::TI][CH::TJ];
+        multiply<CH, false, true>(tiles.walk(s, tb, db), lds, acc);
+        tiles.store(Lane(), acc, s, tb, db);
         return;
     }
-    // dL/dW: columns of the hidden states times the piece's rows, both read down the tokens
-    typedef typename FW::C C;
-    const int n_vt = (a.n_v + C::BN - 1) / C::BN, n_db = (a.d + C::BM - 1) / C::BM;
-    if (!place(blockIdx.x - a.grid_h, static_cast<int64_t>(n_vt) * n_db, pos)) return;
-    patch(pos, n_db, n_vt, 8, db, at);
-    w.a_base = reinterpret_cast<const char*>(a.H) + db * C::BM * 2;
-    w.a_stride = static_cast<unsigned>(row);
-    w.a_rows = a.d - db * C::BM;
-    w.a_k_rows = n_active;
-    w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(at) * C::BN);
-    w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
-    w.b_rows = C::BN;                                // v_stride is a multiple of 256, and zeros follow the piece's last row up to a multiple of 64
-    w.n_k64 = (n_active + 63) / 64;
-    w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
-    f32x4 acc[C::TI][C::TJ];
-    FW::template walk<true, true>(w, lds, acc);
-    store_rows<C>(me, acc, at * C::BN + me.wave % C::WN * (C::BN / C::WN), a.n_v, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.sum, a.read_sum, a.write_sum,
-                  a.grad_w, [](int r) { return r; });
+    const HeadTiles<CW> tiles(a, n_active);
+    const int pos = place(blockIdx.x - a.grid_h, tiles.total());
+    if (pos < 0) return;
+    int vt, db;
+    tiles.at(pos, vt, db);
+    f32x4 acc[CW::TI][CW::TJ];
+    multiply<CW, true, true>(tiles.walk(vt, db), lds, acc);
+    tiles.store(Lane(), acc, vt, db);
 }
 
 // Slabs of dL/dh added in order, rounded, to the tokens' own rows.
@@ -359,7 +419,7 @@ struct Pieces {
     int64_t rows, n_rows;           // tokens of a piece, pieces
     int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces: as many as kPieceElements allow
     Form dz, products;
-    int slabs;                      // parts of the vocabulary piece that dL/dh's K extent is cut into
+    int slabs, k64_per_slab;        // parts of the vocabulary piece that dL/dh's K extent is cut into, and their steps
 };
 int64_t tiles_of(int64_t n, int64_t m, int bn, int bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); }
 
@@ -400,6 +460,9 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
     p.v = up256((all + p.n_v - 1) / p.n_v);
     p.n_v = (all + p.v - 1) / p.v;
     choose_forms(p, d);
+    const int64_t k64 = ((V < p.v ? V : p.v) + 63) / 64;      // of the first piece, no part of which may be empty
+    p.k64_per_slab = static_cast<int>((k64 + p.slabs - 1) / p.slabs);
+    p.slabs = static_cast<int>((k64 + p.k64_per_slab - 1) / p.k64_per_slab);
     return p;
 }
 
@@ -425,28 +488,27 @@ Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
 
 bool sizes_ok(int64_t T, int64_t V, int64_t d) { return T >= 0 && T < (int64_t{1} << 40) && V >= 1 && V <= (1 << 24) && d >= 8 && d % 8 == 0 && d <= 16384; }
 
-template <class F>
-bool dz_of(unsigned grid, const Grad& a, hipStream_t st) {
+template <void (*KERNEL)(Grad), int NT, int LDS>
+bool start(unsigned grid, const Grad& a, hipStream_t st) {
     static arrol_device_flags ok;
-    if (!arrol_allow_lds(&dz_kernel<F>, F::C::LDS_BYTES, ok)) return false;
-    arrol_launch(dz_kernel<F>, dim3(grid), dim3(F::C::NT), F::C::LDS_BYTES, st, a);
+    if (!arrol_allow_lds(KERNEL, LDS, ok)) return false;
+    arrol_launch(KERNEL, dim3(grid), dim3(NT), LDS, st, a);
     return true;
 }
-template <class FH, class FW>
-bool products_of(unsigned grid, const Grad& a, hipStream_t st) {
-    constexpr int kBytes = FH::C::LDS_BYTES > FW::C::LDS_BYTES ? FH::C::LDS_BYTES : FW::C::LDS_BYTES;
-    static_assert(FH::C::NT == FW::C::NT, "one launch");
-    static arrol_device_flags ok;
-    if (!arrol_allow_lds(&products_kernel<FH, FW>, kBytes, ok)) return false;
-    arrol_launch(products_kernel<FH, FW>, dim3(grid), dim3(FH::C::NT), kBytes, st, a);
-    return true;
+template <class C>
+bool start_dz(unsigned grid, const Grad& a, hipStream_t st) { return start<dz_kernel<C>, C::NT, C::LDS_BYTES>(grid, a, st); }
+template <class CH, class CW>
+bool start_products(unsigned grid, const Grad& a, hipStream_t st) {
+    static_assert(CH::NT == CW::NT, "one launch");
+    return start<products_kernel<CH, CW>, CH::NT, (CH::LDS_BYTES > CW::LDS_BYTES ? CH::LDS_BYTES : CW::LDS_BYTES)>(grid, a, st);
 }
 bool launch_dz(Form f, unsigned grid, const Grad& a, hipStream_t st) {
-    return f == kRing ? dz_of<Ring>(grid, a, st) : f == kMid128 ? dz_of<Mid128>(grid, a, st) : f == kMidFew ? dz_of<MidFew>(grid, a, st) : dz_of<Mid64>(grid, a, st);
+    return f == kRing ? start_dz<Ring>(grid, a, st) : f == kMid128 ? start_dz<Mid128>(grid, a, st) : f == kMidFew ? start_dz<MidFew>(grid, a, st) : start_dz<Mid64>(grid, a, st);
 }
-bool launch_products(Form f, unsigned grid, const Grad& a, hipStream_t st) {
-    return f == kRing ? products_of<Ring, Ring>(grid, a, st) : f == kMid128 ? products_of<Mid128, Mid128>(grid, a, st)
-         : f == kMidFew ? products_of<MidFew, Mid128>(grid, a, st) : products_of<Mid64, Mid64>(grid, a, st);
+bool launch_products(Form f, const Grad& a, hipStream_t st) {
+    const unsigned grid = static_cast<unsigned>(a.grid_h + a.grid_w);
+    return f == kRing ? start_products<Ring, Ring>(grid, a, st) : f == kMid128 ? start_products<Mid128, Mid128>(grid, a, st)
+         : f == kMidFew ? start_products<MidFew, Mid128>(grid, a, st) : start_products<Mid64, Mid64>(grid, a, st);
 }
 
 unsigned rounded(int64_t n) { return static_cast<unsigned>((n + kXcds - 1) / kXcds * kXcds); }
@@ -504,16 +566,16 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
             const int64_t v0 = q * p.v, n_v = V - v0 < p.v ? V - v0 : p.v;
             a.W = static_cast<const uint16_t*>(lm_head) + v0 * d, a.v0 = static_cast<int>(v0), a.n_v = static_cast<int>(n_v), a.v_stride = static_cast<int>(p.v);
             if (!launch_dz(p.dz, rounded(tiles_of(rows, n_v, kSize[p.dz].bn, kSize[p.dz].bm)), a, st)) return refused();
-            a.n_slabs = p.slabs, a.k64_per_slab = static_cast<int>((p.v / 64 + p.slabs - 1) / p.slabs), a.add = q > 0;
+            a.k64_per_slab = p.k64_per_slab, a.add = q > 0;
             a.grid_h = grad_hidden ? static_cast<int>(rounded(tiles_of(rows, d, size.bn, size.bm) * p.slabs)) : 0;
-            int64_t grid_w = 0;
+            a.grid_w = 0;
             if (grad_lm_head || lm_head_sum) {
-                grid_w = rounded(tiles_of(n_v, d, size.bn_w, size.bm_w));
+                a.grid_w = static_cast<int>(rounded(tiles_of(n_v, d, size.bn_w, size.bm_w)));
                 a.sum = (lm_head_sum ? lm_head_sum : reinterpret_cast<float*>(base + ws.sum)) + v0 * d;
                 a.grad_w = grad_lm_head ? static_cast<uint16_t*>(grad_lm_head) + v0 * d : nullptr;
                 a.read_sum = lm_head_sum || piece > 0, a.write_sum = lm_head_sum || piece + 1 < p.n_rows;
             }
-            if (!launch_products(p.products, static_cast<unsigned>(a.grid_h + grid_w), a, st)) return refused();
+            if (!launch_products(p.products, a, st)) return refused();
         }
         if (grad_hidden && !direct) {
             const int64_t blocks = (rows * (d / 4) + 255) / 256;
