@@ -6,14 +6,18 @@
 // whole turns is rounded to 32: at position 10^6 a 32-bit product is off by up to 0.03 radians.  Cosine and sine are those of the remaining half turns; a result is rounded once.
 //
 // A wavefront takes a token, or a part of its heads where tokens are few: it loads first, forms the cosines and sines of the token, one pair to a lane, while the loads are
-// under way, hands them over through its own part of the LDS and stores.  No barrier.  What a lane holds is a unit: VEC elements and their partners (or VEC elements
-// of the rest of the head, or 8 interleaved elements), loaded and stored by that lane alone, so an output may be its input.
+// under way, hands them over through its own part of the LDS and stores.  No barrier.  What a lane holds is a unit: VEC elements and their partners, or 2 VEC
+// elements side by side of the rest of the head or of an interleaved one, loaded and stored by that lane alone, so an output may be its input.
 #include "common.h"
 
 namespace {
 
 constexpr int kWaves = 4;                 // of a workgroup
-constexpr int kInFlight = 4;              // units of a lane
+// Units of a lane in flight, and wavefronts that a launch is cut into where tokens are fewer.  10,000 tokens, 32 + 8 heads of 128, from and to memory: 2 and 65,536 45.3 us
+// (5.0 TB/s), 4 and 8,192 46.8, loads through the caches 50.4; stores past the caches too: 41.2, but the attention behind it 8 longer.  Into the pool, where every wavefront looks
+// for its token's page: 5,172 tokens of 24 + 8 heads of 80, 3 and 8,192 23.8 us, 2 and 65,536 28.3, 4 and 65,536 35.6.
+template <bool POOL> constexpr int kUnits = POOL ? 3 : 2;
+template <bool POOL> constexpr int kWavefronts = POOL ? 8192 : 65536;
 constexpr int kMaxHalf = 128;
 
 struct Turn {
@@ -45,9 +49,15 @@ template <> __device__ __forceinline__ uint16_t at<1>(const uint16_t& x, int) { 
 template <int N> __device__ __forceinline__ void put(typename Elements<N>::type& x, int i, uint16_t v) { x[i] = v; }
 template <> __device__ __forceinline__ void put<1>(uint16_t& x, int, uint16_t v) { x = v; }
 
-// How many of cu[0..n] are at most t, 64 of them to a step: cu ascends, and whatever it holds the answer is in [0, n + 1].
-__device__ __forceinline__ int offsets_up_to(const int64_t* cu, int n, int64_t t, int lane) {
+// A value that is the same in all lanes and that no kernel of the call writes, by way of the scalar cache: its wait is not one for the vector loads under way.
+template <class T>
+__device__ __forceinline__ T fetch(const T* p) { return *(const __attribute__((address_space(4))) T*)p; }
+
+// How many of cu[0..n] are at most t, 64 of them to a step: cu ascends, and whatever it holds the answer is in [0, n + 1].  first: cu[min(lane, n)], which
+// is all there is to look at up to 63 sequences.
+__device__ __forceinline__ int offsets_up_to(const int64_t* cu, int n, int64_t t, int lane, int64_t first) {
     int64_t lo = 0, hi = static_cast<int64_t>(n) + 1;
+    if (hi <= ARROL_WAVE) return __popcll(__ballot(lane < hi && first <= t));
     while (hi - lo > ARROL_WAVE) {
         const int64_t step = (hi - lo + ARROL_WAVE - 1) / ARROL_WAVE, i = lo + lane * step;
         const int below = __popcll(__ballot(i < hi && cu[i < hi ? i : lo] <= t));
@@ -63,12 +73,15 @@ __device__ __forceinline__ int offsets_up_to(const int64_t* cu, int n, int64_t t
 template <int VEC, bool INTERLEAVED, bool POOL>
 __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
     typedef typename Elements<VEC>::type vec;
+    constexpr int kInFlight = kUnits<POOL>;
     __shared__ float2 turns[kWaves][kMaxHalf];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
     const int64_t t = item / a.groups;
     const int group = static_cast<int>(item - t * a.groups);
     if (t >= a.T) return;
+    int64_t offset = 0;
+    if (POOL && a.cu) offset = a.cu[lane < a.n_seq ? lane : a.n_seq];
 
     const int n_turned = INTERLEAVED ? 0 : a.half / VEC;      // units of two halves; interleaved ones see for themselves
     const uint16_t *q = a.q + t * a.q_stride, *k = a.k + t * a.k_stride;
@@ -76,6 +89,9 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
     const int total = (a.heads + a.kv_heads) * a.units;
     const int stride = ARROL_WAVE * a.groups, d_head = stride / a.units, d_unit = stride - d_head * a.units;
     int u = group * ARROL_WAVE + lane, head = u / a.units, unit = u - head * a.units;
+    // where a unit's two parts lie in their head; the last unit of the rest may lack its second
+    auto first_of = [&](int unit) { return INTERLEAVED ? 2 * VEC * unit : unit < n_turned ? VEC * unit : 2 * a.half + 2 * VEC * (unit - n_turned); };
+    auto second_of = [&](int unit) { return INTERLEAVED || unit >= n_turned ? first_of(unit) + VEC : a.half + VEC * unit; };
 
     vec x[kInFlight], y[kInFlight];
     int of_head[kInFlight], of_unit[kInFlight];
@@ -86,9 +102,9 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
             of_unit[i] = unit;
             if (u < total) {
                 const uint16_t* row = head < a.heads ? q + head * a.hd : k + (head - a.heads) * a.hd;
-                const bool turned = unit < n_turned;
-                x[i] = *reinterpret_cast<const vec*>(row + (unit + (turned || INTERLEAVED ? 0 : n_turned)) * VEC);
-                if (!INTERLEAVED && turned) y[i] = *reinterpret_cast<const vec*>(row + a.half + unit * VEC);
+                const int second = second_of(unit);
+                x[i] = __builtin_nontemporal_load(reinterpret_cast<const vec*>(row + first_of(unit)));
+                if (second < a.hd) y[i] = __builtin_nontemporal_load(reinterpret_cast<const vec*>(row + second));
             }
             u += stride;
             head += d_head;
@@ -97,6 +113,14 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
         }
     };
     load();
+    u32x4 v[kInFlight];
+    const int n_v = a.kv_heads * a.hd / 8, v0 = group * ARROL_WAVE + lane;
+    const uint16_t* values = POOL ? a.v + t * a.v_stride : nullptr;
+    if (POOL) {
+#pragma unroll
+        for (int i = 0; i < kInFlight; ++i)
+            if (v0 + i * stride < n_v) v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(values + (v0 + i * stride) * 8));
+    }
 
     // where the token goes, and its position
     int64_t slot = 0, to = -1;            // to: token of the pool
@@ -105,22 +129,26 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
         int s = static_cast<int>(t);
         int64_t j = 0;
         if (a.cu) {
-            s = offsets_up_to(a.cu, a.n_seq, t, lane) - 1;
+            s = offsets_up_to(a.cu, a.n_seq, t, lane, offset) - 1;
             known = s >= 0 && s < a.n_seq;
-            if (known) j = t - (a.cu[s] > 0 ? a.cu[s] : 0);
         }
+        s = __builtin_amdgcn_readfirstlane(s);
         if (known) {
-            slot = a.start[s] + j;
+            if (a.cu) {
+                const int64_t begin = fetch(a.cu + s);
+                j = t - (begin > 0 ? begin : 0);
+            }
+            slot = fetch(a.start + s) + j;
             const int64_t p = slot / a.page;
             if (slot >= 0 && p < a.width) {
-                const int32_t id = a.table[static_cast<int64_t>(s) * a.width + p];
+                const int32_t id = fetch(a.table + static_cast<int64_t>(s) * a.width + p);
                 if (id >= 0 && id < a.n_pages) to = static_cast<int64_t>(id) * a.page + (slot - p * a.page);
             }
         }
     }
     const int half = known ? a.half : 0;
     if (half > 0) {
-        const double p = a.position ? static_cast<double>(a.position[t]) : static_cast<double>(slot);
+        const double p = a.position ? static_cast<double>(fetch(a.position + t)) : static_cast<double>(slot);
         for (int i = lane; i < half; i += ARROL_WAVE) {
             const double full = p * (a.inv_freq[i] * 0.15915494309189533577);     // 1 / 2 pi
             float s, c;
@@ -135,31 +163,28 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
 #pragma unroll
         for (int i = 0; i < kInFlight; ++i) {
             if (of_head[i] < 0) continue;
-            const bool turned = of_unit[i] < n_turned;
-            const int first = (of_unit[i] + (turned || INTERLEAVED ? 0 : n_turned)) * VEC;
+            const int first = first_of(of_unit[i]), second = second_of(of_unit[i]);
+            auto turn = [&](int pair, auto get, auto set) {
+                const float2 cs = turns[wave][pair];
+                const float p = widen(get(0)), r = widen(get(1));
+                set(0, narrow(p * cs.x - r * cs.y));
+                set(1, narrow(p * cs.y + r * cs.x));
+            };
             if (INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < VEC / 2; ++e) {
-                    const int pair = of_unit[i] * (VEC / 2) + e;
-                    if (pair < half) {
-                        const float2 cs = turns[wave][pair];
-                        const float p = widen(at<VEC>(x[i], 2 * e)), r = widen(at<VEC>(x[i], 2 * e + 1));
-                        put<VEC>(x[i], 2 * e, narrow(p * cs.x - r * cs.y));
-                        put<VEC>(x[i], 2 * e + 1, narrow(p * cs.y + r * cs.x));
-                    }
+                for (int e = 0; e < VEC; ++e) {       // pairs of x, then of y
+                    vec& z = e < VEC / 2 ? x[i] : y[i];
+                    const int at0 = 2 * (e % (VEC / 2)), pair = of_unit[i] * VEC + e;
+                    if (pair < half) turn(pair, [&](int w) { return at<VEC>(z, at0 + w); }, [&](int w, uint16_t b) { put<VEC>(z, at0 + w, b); });
                 }
-            } else if (turned && half > 0) {
+            } else if (of_unit[i] < n_turned && half > 0) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float2 cs = turns[wave][of_unit[i] * VEC + e];
-                    const float p = widen(at<VEC>(x[i], e)), r = widen(at<VEC>(y[i], e));
-                    put<VEC>(x[i], e, narrow(p * cs.x - r * cs.y));
-                    put<VEC>(y[i], e, narrow(p * cs.y + r * cs.x));
-                }
+                for (int e = 0; e < VEC; ++e)
+                    turn(of_unit[i] * VEC + e, [&](int w) { return at<VEC>(w ? y[i] : x[i], e); }, [&](int w, uint16_t b) { put<VEC>(w ? y[i] : x[i], e, b); });
             }
             auto store = [&](uint16_t* row) {
                 *reinterpret_cast<vec*>(row + first) = x[i];
-                if (!INTERLEAVED && turned) *reinterpret_cast<vec*>(row + a.half + first) = y[i];
+                if (second < a.hd) *reinterpret_cast<vec*>(row + second) = y[i];
             };
             const int kv_head = of_head[i] - a.heads;
             if (kv_head < 0) {
@@ -174,20 +199,21 @@ __global__ __launch_bounds__(kWaves * ARROL_WAVE) void rotary_kernel(Turn a) {
     }
 
     if (POOL && to >= 0) {
-        const int n = a.kv_heads * a.hd / 8;
-        const uint16_t* v = a.v + t * a.v_stride;
         uint16_t* pool_v = a.pool_v + to * a.kv_heads * a.hd;
-        for (int i = group * ARROL_WAVE + lane; i < n; i += stride)
-            *reinterpret_cast<u32x4*>(pool_v + i * 8) = *reinterpret_cast<const u32x4*>(v + i * 8);
+#pragma unroll
+        for (int i = 0; i < kInFlight; ++i)
+            if (v0 + i * stride < n_v) *reinterpret_cast<u32x4*>(pool_v + (v0 + i * stride) * 8) = v[i];
+        for (int i = v0 + kInFlight * stride; i < n_v; i += stride)
+            *reinterpret_cast<u32x4*>(pool_v + i * 8) = *reinterpret_cast<const u32x4*>(values + i * 8);
     }
 }
 
 template <bool POOL>
 int turn(Turn& a, bool interleaved, hipStream_t st) {
     const int vec = interleaved || a.half % 8 == 0 ? 8 : a.half % 4 == 0 ? 4 : a.half % 2 == 0 ? 2 : 1;
-    a.units = interleaved ? a.hd / 8 : (a.hd - a.half) / vec;
+    a.units = interleaved ? (a.hd + 15) / 16 : a.half / vec + (a.hd - 2 * a.half + 2 * vec - 1) / (2 * vec);
     const int64_t most = (static_cast<int64_t>(a.heads + a.kv_heads) * a.units + ARROL_WAVE - 1) / ARROL_WAVE;
-    const int64_t want = 8192 / a.T;
+    const int64_t want = kWavefronts<POOL> / a.T;
     a.groups = static_cast<int>(want < 1 ? 1 : want < most ? want : most);
     const dim3 grid(static_cast<unsigned>((a.T * a.groups + kWaves - 1) / kWaves)), block(kWaves * ARROL_WAVE);
     if (interleaved) arrol_launch(rotary_kernel<8, true, POOL>, grid, block, 0, st, a);

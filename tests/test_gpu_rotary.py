@@ -77,9 +77,9 @@ def test_rotary(A, H, KV, hd, rot, interleaved, T):
     assert none is None and torch.equal(only, A.arrol_rotary(q, k, position, f, interleaved=interleaved)[0])
 
 
-@pytest.mark.parametrize("T", [2048, 8191, 8193, 20011])
+@pytest.mark.parametrize("T", [2048, 8191, 8193, 20011, 65537])
 def test_rotary_of_many_tokens(A, T):
-    """A wavefront takes a part of a token's heads up to 8,192 tokens, whole tokens beyond."""
+    """A wavefront takes a part of a token's heads where tokens are few, whole tokens beyond 65,536."""
     print("[case] rotary T=%d" % T, flush=True)
     x, f = rand(T, 6, 64, seed=T), frequencies(A, 64)
     position = torch.arange(T, dtype=torch.int32, device=DEV) * 131
