@@ -11,7 +11,8 @@
 //   dz         256 x 256 tiles of W h, dz in the epilogue, stored token-major through the LDS in whole lines
 //   products   tiles of dL/dh (dz as it lies, W read in place down its rows) and of dL/dW (dz and the hidden states both read down their rows), in one launch, so that
 //              the long walks of the first and the many short ones of the second fill the chip together
-//   join       the slabs of dL/dh, where there are several, added in order
+//   join       where K extents of the products are cut into parts, whose sums go to slabs: the slabs added in order
+// Up to kFoundTokens tokens (and middle-sized tiles) there is no launch for the first step: every workgroup of the second finds the tokens by itself, and each copies some.
 // No atomics: sums have a fixed order.
 #include "common.h"
 #include "mid_nt.h"
@@ -26,6 +27,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kXcds = 8, kRound = 256;
 constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
+constexpr int kFoundTokens = 1024;
 
 // The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
 typedef ring_nt::RingTile<256, 256, 2, 4> Ring;
@@ -58,6 +60,9 @@ struct Grad {
     float* sum;                     // fp32 sums, read and / or written
     uint16_t* grad_w;
     int read_sum, write_sum;
+    float* slabs_w;                 // [parts][piece's rows][d], NULL: no parts
+    int64_t slab_w_stride;
+    int k64_per_part;
 };
 
 // Place in a work order in which every round of 256 workgroups gives each XCD (workgroup ids congruent mod 8) 32 that follow each other.  -1: none.
@@ -78,7 +83,8 @@ __device__ __forceinline__ void patch(int pos, int rows, int cols, int most, int
 
 __device__ __forceinline__ bool takes_part(float g, int32_t target, int V) { return g != 0.f && target >= 0 && target < V; }      // NaN does
 
-// Tokens that take part, packed.  A workgroup has ROWS tokens, a wavefront ROWS / 4 of them, and counts those before them itself.
+// Tokens that take part, packed.  A workgroup has kGatherRows tokens, a wavefront a quarter of them, and counts those before them itself.
+constexpr int kGatherRows = 16;
 struct Gather {
     const uint16_t* hidden;
     const int32_t* targets;
@@ -88,9 +94,8 @@ struct Gather {
     int32_t *target, *row, *n_active;
     int T, V, d;
 };
-template <int ROWS>
 __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
-    constexpr int kInFlight = 8;
+    constexpr int kInFlight = 8, ROWS = kGatherRows;
     __shared__ int before[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), t0 = blockIdx.x * ROWS;
     const bool in = lane < ROWS && t0 + lane < a.T;
@@ -163,19 +168,62 @@ struct Lane {
     __device__ __forceinline__ int place(int i) const { return 16 * (i + (lq & 1)) + 4 * (lq & 2); }      // of exchange()'s values
 };
 
+// The tokens that take part, found by a workgroup of 256 by itself, up to kFoundTokens of them: their numbers in `list`, the others' bits in `masks` clear; how many.
+struct Found {
+    uint64_t masks[kFoundTokens / ARROL_WAVE];
+    int list[kFoundTokens];
+};
+__device__ __forceinline__ int find_tokens(const Gather& a, Found& found) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rounds = (a.T + 255) / 256;
+    float g[kFoundTokens / 256];
+    int32_t y[kFoundTokens / 256];
+#pragma unroll
+    for (int i = 0; i < kFoundTokens / 256; ++i) {
+        const int t = i * 256 + tid;
+        g[i] = t < a.T ? a.grad_logp[t] : 0.f;
+        y[i] = t < a.T ? a.targets[t] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kFoundTokens / 256; ++i) {
+        const uint64_t active = __ballot(takes_part(g[i], y[i], a.V));
+        if (lane == 0) found.masks[i * 4 + wave] = active;
+    }
+    __syncthreads();
+    int n = 0;
+    for (int i = 0; i < rounds; ++i) {
+        int before = n;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int count = __popcll(found.masks[i * 4 + w]);
+            before += w < wave ? count : 0;
+            n += count;
+        }
+        const uint64_t mine = found.masks[i * 4 + wave];
+        if ((mine >> lane) & 1) found.list[before + __popcll(mine & ((uint64_t{1} << lane) - 1))] = i * 256 + tid;
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(n);
+}
+__device__ __forceinline__ void copy_row(const uint16_t* from, uint16_t* to, int vecs) {      // by a workgroup of 256; from NULL: zeros
+    for (int c = threadIdx.x; c < vecs; c += 256)
+        *reinterpret_cast<u32x4*>(to + c * 8) = from ? *reinterpret_cast<const u32x4*>(from + c * 8) : u32x4{0, 0, 0, 0};
+}
+
 // What the lane's tokens bring with them: of token 16 j + lane % 16 of the wavefront's part.  Fetched before the walk.
 template <class C>
 struct Tokens {
     float g[C::TJ], at[C::TJ];      // at: -lse log2 e
     int target[C::TJ];              // -1: none
-    __device__ __forceinline__ Tokens(const Grad& a, const Lane& me, int tb, int n_active) {
+    template <class RowOf>
+    __device__ __forceinline__ Tokens(const float* gs, const float* lse, const int32_t* targets, const Lane& me, int tb, int n_active, RowOf row_of) {
 #pragma unroll
         for (int j = 0; j < C::TJ; ++j) {
             const int t = tb * C::BN + me.wave % C::WN * (C::BN / C::WN) + j * 16 + me.l15;
             const bool live = t < n_active;
-            g[j] = live ? a.g[t] : 0.f;
-            at[j] = live ? -a.lse[t] * kLog2e : 0.f;
-            target[j] = live ? a.target[t] : -1;
+            const int r = live ? row_of(t) : 0;
+            g[j] = live ? gs[r] : 0.f;
+            at[j] = live ? -lse[r] * kLog2e : 0.f;
+            target[j] = live ? targets[r] : -1;
         }
     }
 };
@@ -249,9 +297,40 @@ __global__ __launch_bounds__(C::NT) void dz_kernel(Grad a) {
     int vt, tb;
     tiles.at(pos, vt, tb);
     const Lane me;
-    const Tokens<C> tokens(a, me, tb, n_active);
+    const Tokens<C> tokens(a.g, a.lse, a.target, me, tb, n_active, mid_nt::InOrder());
     f32x4 acc[C::TI][C::TJ];
     multiply<C, false, false>(tiles.walk(vt, tb), lds, acc, (a.d & 63) ? (a.d & 63) / 8 : 8);
+    store_dz<C>(a, me, tokens, acc, vt, tb, n_active);
+}
+
+// The same where the tokens are found here.  Which they are is left behind for the products, and their hidden states, packed, if `g.H` is given.
+template <class C>
+__global__ __launch_bounds__(C::NT) void dz_found_kernel(Grad a, Gather g) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    Found& found = *reinterpret_cast<Found*>(lds + C::LDS_BYTES);
+    const int n_active = find_tokens(g, found), vecs = a.d / 8;
+    if (blockIdx.x == 0) {
+        for (int r = threadIdx.x; r < n_active; r += 256) g.row[r] = found.list[r];
+        if (threadIdx.x == 0) *g.n_active = n_active;
+    }
+    if (g.grad_hidden && n_active < g.T)
+        for (int t = blockIdx.x; t < g.T; t += gridDim.x)
+            if (!((found.masks[t >> 6] >> (t & 63)) & 1)) copy_row(nullptr, g.grad_hidden + static_cast<int64_t>(t) * a.d, vecs);
+    const DzTiles<C> tiles(a, n_active);
+    const int pos = place(blockIdx.x, tiles.total());
+    if (pos < 0) return;
+    int vt, tb;
+    tiles.at(pos, vt, tb);
+    const int t0 = tb * C::BN;
+    if (g.H)        // the tile's tokens, shared out over the vocabulary's tiles
+        for (int t = t0 + vt; t < t0 + C::BN && t < n_active; t += tiles.n_vt)
+            copy_row(g.hidden + static_cast<int64_t>(found.list[t]) * a.d, g.H + static_cast<int64_t>(t) * a.d, vecs);
+    const Lane me;
+    const Tokens<C> tokens(g.grad_logp, g.lse, g.targets, me, tb, n_active, [&](int t) { return found.list[t]; });
+    f32x4 acc[C::TI][C::TJ];
+    ring_nt::Walk w = tiles.walk(vt, tb);
+    w.b_base = reinterpret_cast<const char*>(g.hidden);
+    mid_nt::walk<C, false, false>(w, lds, acc, (a.d & 63) ? (a.d & 63) / 8 : 8, [&](int r) { return found.list[t0 + r]; });
     store_dz<C>(a, me, tokens, acc, vt, tb, n_active);
 }
 
@@ -317,31 +396,37 @@ struct HiddenTiles {
     }
 };
 
-// dL/dW: columns of the hidden states times the piece's rows, both read down the tokens.  Tile (vt, db).
+// dL/dW: columns of the hidden states times the piece's rows, both read down the tokens or a part of them.  Tile (s, vt, db).
 template <class C>
 struct HeadTiles {
     const Grad& a;
-    const int n_active, n_vt, n_db;
-    __device__ __forceinline__ HeadTiles(const Grad& a, int n) : a(a), n_active(n), n_vt((a.n_v + C::BN - 1) / C::BN), n_db((a.d + C::BM - 1) / C::BM) {}
-    __device__ __forceinline__ int total() const { return n_vt * n_db; }
-    __device__ __forceinline__ void at(int pos, int& vt, int& db) const { patch(pos, n_db, n_vt, 8, db, vt); }
-    __device__ __forceinline__ ring_nt::Walk walk(int vt, int db) const {
+    const int n_active, n_vt, n_db, n_k64, n_parts;
+    __device__ __forceinline__ HeadTiles(const Grad& a, int n)
+        : a(a), n_active(n), n_vt((a.n_v + C::BN - 1) / C::BN), n_db((a.d + C::BM - 1) / C::BM), n_k64((n + 63) / 64), n_parts(a.slabs_w ? (n_k64 + a.k64_per_part - 1) / a.k64_per_part : 1) {}
+    __device__ __forceinline__ int total() const { return n_vt * n_db * n_parts; }
+    __device__ __forceinline__ void at(int pos, int& s, int& vt, int& db) const {
+        s = __builtin_amdgcn_readfirstlane(pos / (n_vt * n_db));
+        patch(pos - s * n_vt * n_db, n_db, n_vt, 8, db, vt);
+    }
+    __device__ __forceinline__ ring_nt::Walk walk(int s, int vt, int db) const {
         ring_nt::Walk w = {};
         const int64_t row = static_cast<int64_t>(a.d) * 2;
-        w.a_base = reinterpret_cast<const char*>(a.H) + db * C::BM * 2;
+        const int k_lo = a.slabs_w ? s * a.k64_per_part : 0, k_hi = a.slabs_w && k_lo + a.k64_per_part < n_k64 ? k_lo + a.k64_per_part : n_k64;
+        w.a_base = reinterpret_cast<const char*>(a.H) + static_cast<int64_t>(k_lo) * 64 * row + db * C::BM * 2;
         w.a_stride = static_cast<unsigned>(row);
         w.a_rows = a.d - db * C::BM;
-        w.a_k_rows = n_active;
-        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(vt) * C::BN);
+        w.a_k_rows = n_active - k_lo * 64;
+        w.b_base = reinterpret_cast<const char*>(a.dz + static_cast<int64_t>(k_lo) * 64 * a.v_stride + static_cast<int64_t>(vt) * C::BN);
         w.b_stride = static_cast<unsigned>(a.v_stride) * 2;
         w.b_rows = C::BN;                                // v_stride is a multiple of 256, and zeros follow the piece's last row up to a multiple of 64
-        w.n_k64 = (n_active + 63) / 64;
+        w.n_k64 = k_hi - k_lo;
         w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
         return w;
     }
-    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int vt, int db) const {
-        store_rows<C>(me, acc, vt * C::BN + me.wave % C::WN * (C::BN / C::WN), a.n_v, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.sum, a.read_sum, a.write_sum,
-                      a.grad_w, [](int r) { return r; });
+    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
+        const int r0 = vt * C::BN + me.wave % C::WN * (C::BN / C::WN), c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM);
+        const bool parts = a.slabs_w != nullptr;
+        store_rows<C>(me, acc, r0, a.n_v, c0, a.d, parts ? a.slabs_w + s * a.slab_w_stride : a.sum, !parts && a.read_sum, parts || a.write_sum, a.grad_w, [](int r) { return r; });
     }
 };
 
@@ -363,32 +448,45 @@ __global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
     const HeadTiles<CW> tiles(a, n_active);
     const int pos = place(blockIdx.x - a.grid_h, tiles.total());
     if (pos < 0) return;
-    int vt, db;
-    tiles.at(pos, vt, db);
+    int s, vt, db;
+    tiles.at(pos, s, vt, db);
     f32x4 acc[CW::TI][CW::TJ];
-    multiply<CW, true, true>(tiles.walk(vt, db), lds, acc);
-    tiles.store(Lane(), acc, vt, db);
+    multiply<CW, true, true>(tiles.walk(s, vt, db), lds, acc);
+    tiles.store(Lane(), acc, s, vt, db);
 }
 
-// Slabs of dL/dh added in order, rounded, to the tokens' own rows.
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ slabs, int64_t slab_stride, int n_slabs, const int32_t* __restrict__ row, const int32_t* __restrict__ n_active,
-                                                   int d, uint16_t* __restrict__ grad_hidden) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+// Slabs added in order: of dL/dh to the tokens' own rows (blocks up to blocks_h), of dL/dW to what its tiles would have written.
+__device__ __forceinline__ f32x4 slab_sum(const float* slabs, int64_t stride, int n) {
     constexpr int kInFlight = 8;
-    const int vecs = d / 4;
-    const int64_t total = static_cast<int64_t>(*n_active) * vecs;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<int64_t>(t) * vecs) * 4;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int s0 = 0; s0 < n_slabs; s0 += kInFlight) {
-            f32x4 y[kInFlight];
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < n; s0 += kInFlight) {
+        f32x4 y[kInFlight];
 #pragma unroll
-            for (int s = 0; s < kInFlight; ++s) y[s] = *reinterpret_cast<const f32x4*>(slabs + (s0 + s < n_slabs ? s0 + s : s0) * slab_stride + i * 4);
+        for (int s = 0; s < kInFlight; ++s) y[s] = *reinterpret_cast<const f32x4*>(slabs + (s0 + s < n ? s0 + s : s0) * stride);
 #pragma unroll
-            for (int s = 0; s < kInFlight; ++s)
-                if (s0 + s < n_slabs) x += y[s];
+        for (int s = 0; s < kInFlight; ++s)
+            if (s0 + s < n) x += y[s];
+    }
+    return x;
+}
+__global__ __launch_bounds__(256) void join_kernel(Grad a, int n_slabs, int blocks_h) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const int vecs = a.d / 4, n_active = *a.n_active;
+    if (static_cast<int>(blockIdx.x) < blocks_h) {
+        const int64_t total = static_cast<int64_t>(n_active) * vecs;
+        for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(blocks_h) * 256) {
+            const int t = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<int64_t>(t) * vecs) * 4;
+            *reinterpret_cast<bf16x4*>(a.grad_hidden + static_cast<int64_t>(a.row[t]) * a.d + c) = __builtin_convertvector(slab_sum(a.slabs + i * 4, a.slab_stride, n_slabs), bf16x4);
         }
-        *reinterpret_cast<bf16x4*>(grad_hidden + static_cast<int64_t>(row[t]) * d + c) = __builtin_convertvector(x, bf16x4);
+        return;
+    }
+    const int parts = ((n_active + 63) / 64 + a.k64_per_part - 1) / a.k64_per_part, first = blockIdx.x - blocks_h, blocks = gridDim.x - blocks_h;
+    const int64_t total = static_cast<int64_t>(a.n_v) * vecs;
+    for (int64_t i = static_cast<int64_t>(first) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(blocks) * 256) {
+        f32x4 x = slab_sum(a.slabs_w + i * 4, a.slab_w_stride, parts);
+        if (a.read_sum) x += *reinterpret_cast<const f32x4*>(a.sum + i * 4);
+        if (a.write_sum) *reinterpret_cast<f32x4*>(a.sum + i * 4) = x;
+        else *reinterpret_cast<bf16x4*>(a.grad_w + i * 4) = __builtin_convertvector(x, bf16x4);
     }
 }
 
@@ -413,13 +511,15 @@ constexpr Size kSize[kForms] = {{256, 256, 256, 256, 1, 8.7, 1.45, 1.1, 10.0, 1.
                                 {128, 64, 128, 128, 2, 1.7, 0.66, 0.33, 4.2, 0.95, 0.53}, {64, 64, 64, 64, 3, 1.4, 0.57, 0.2, 2.0, 0.6, 0.2}};
 
 constexpr int kMaxSlabs = 32, kSlabTiles = 512;     // of 256 x 256
-constexpr double kJoin = 2.5, kJoinBytes = 3e6;      // microseconds; bytes a microsecond
+constexpr int64_t kSlabFloats = kSlabTiles * int64_t{65536};
+constexpr double kJoin = 3.5, kJoinBytes = 3e6;      // microseconds; bytes a microsecond
 
 struct Pieces {
     int64_t rows, n_rows;           // tokens of a piece, pieces
     int64_t v, n_v;                 // vocabulary rows of a piece (a multiple of 256), pieces: as many as kPieceElements allow
     Form dz, products;
     int slabs, k64_per_slab;        // parts of the vocabulary piece that dL/dh's K extent is cut into, and their steps
+    int parts;                      // of the tokens that dL/dW's is
 };
 int64_t tiles_of(int64_t n, int64_t m, int bn, int bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); }
 
@@ -429,9 +529,9 @@ double dz_time(const Size& f, int64_t rows, int64_t v, int64_t d) {
     const double up = static_cast<double>(static_cast<int64_t>(r + 0.999));
     return (up < r + 0.5 ? up : r + 0.5) * (f.tile + steps * f.step);       // of many rounds the last one's workgroups start early
 }
-double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, int slabs) {
-    const double n_h = static_cast<double>(tiles_of(rows, d, f.bn, f.bm) * slabs), n_w = static_cast<double>(tiles_of(v, d, f.bn_w, f.bm_w));
-    const double k_h = static_cast<double>((v / 64 + slabs - 1) / slabs), k_w = static_cast<double>((rows + 63) / 64), places = 256.0 * f.per_unit;
+double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, int slabs, int parts) {
+    const double n_h = static_cast<double>(tiles_of(rows, d, f.bn, f.bm) * slabs), n_w = static_cast<double>(tiles_of(v, d, f.bn_w, f.bm_w) * parts);
+    const double k_h = static_cast<double>((v / 64 + slabs - 1) / slabs), k_w = static_cast<double>(((rows + 63) / 64 + parts - 1) / parts), places = 256.0 * f.per_unit;
     const double all = (n_h * (f.tile + k_h * f.step) + n_w * (f.tile_w + k_w * f.step_w)) / places;
     const double lone_h = f.tile + k_h * f.lone, lone_w = f.tile_w + k_w * f.lone_w, longest = lone_h > lone_w ? lone_h : lone_w;
     return n_h + n_w <= places ? (all > longest ? all : longest) : all + longest / 2;
@@ -442,12 +542,22 @@ void choose_forms(Pieces& p, int64_t d) {
         const Size& size = kSize[f];
         const double dz = f == kRing && d % 64 ? 1e30 : dz_time(size, p.rows, p.v, d);
         if (dz < best_dz) best_dz = dz, p.dz = static_cast<Form>(f);
+        // parts of dL/dW's K extent where that is long and its tiles are few: as many as fill the chip, of 8 steps at least
+        const int64_t tiles_w = tiles_of(p.v, d, size.bn_w, size.bm_w), k_w = (p.rows + 63) / 64;
+        int64_t parts = f != kRing && k_w >= 32 && tiles_w < 256 ? 512 / tiles_w : 1;
+        parts = parts < k_w / 8 ? parts : k_w / 8;
+        parts = parts < kMaxSlabs ? parts : kMaxSlabs;
+        if (parts * p.v * d > kSlabFloats) parts = kSlabFloats / (p.v * d);
         const int64_t tile = static_cast<int64_t>(size.bm) * size.bn, tiles = tiles_of(p.rows, d, size.bn, size.bm), k64 = p.v / 64;
-        for (int s = 1; s <= kMaxSlabs; s += s < 4 ? 1 : s / 4) {
-            if (s > 1 && (s > k64 / 2 || s * tiles * tile > kSlabTiles * int64_t{65536})) break;
-            const double join = s > 1 || p.n_v > 1 ? kJoin + 4.0 * s * p.rows * d / kJoinBytes : 0.0;
-            const double t = products_time(size, p.rows, p.v, d, s) + join;
-            if (t < best) best = t, p.products = static_cast<Form>(f), p.slabs = s;
+        for (int with = 0; with < (parts > 1 ? 2 : 1); ++with) {
+            const int n = with ? static_cast<int>(parts) : 1;
+            for (int s = 1; s <= kMaxSlabs; s += s < 4 ? 1 : s / 4) {
+                if (s > 1 && (s > k64 / 2 || s * tiles * tile > kSlabFloats)) break;
+                const bool join_h = s > 1 || p.n_v > 1;
+                const double join = join_h || with ? kJoin + ((join_h ? 4.0 * s * p.rows * d : 0.0) + (with ? 4.0 * n * p.v * d : 0.0)) / kJoinBytes : 0.0;
+                const double t = products_time(size, p.rows, p.v, d, s, n) + join;
+                if (t < best) best = t, p.products = static_cast<Form>(f), p.slabs = s, p.parts = n;
+            }
         }
     }
 }
@@ -467,13 +577,14 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
 }
 
 struct Workspace {
-    size_t H, g, lse, target, row, n_active, dz, slabs, sum, bytes;
+    size_t H, g, lse, target, row, n_active, dz, slabs, slabs_w, sum, bytes;
 };
 // Sizes that no smaller batch exceeds.
 Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     Workspace w;
     const int64_t rows = T < kPieceRows ? T : kPieceRows, all = up256(rows) * up256(V);
-    const int64_t one = rows * d, many = kMaxSlabs * one < kSlabTiles * 65536 ? kMaxSlabs * one : kSlabTiles * int64_t{65536};      // one slab, or kSlabTiles tiles at most
+    const int64_t one = rows * d, many = kMaxSlabs * one < kSlabFloats ? kMaxSlabs * one : kSlabFloats;      // one slab, or kSlabTiles tiles at most
+    const int64_t head = up256(V) * d;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes); return was; };
     w.n_active = take(4);
@@ -481,6 +592,7 @@ Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     w.H = take(up256(rows) * d * 2);
     w.dz = take((all < kPieceElements ? all : kPieceElements) * 2);
     w.slabs = take((one > many ? one : many) * 4);
+    w.slabs_w = take(T > 256 && 2 * head <= kSlabFloats ? (kMaxSlabs * head < kSlabFloats ? kMaxSlabs * head : kSlabFloats) * 4 : 0);
     w.sum = take(lm_head && T > kPieceRows ? V * d * 4 : 0);
     w.bytes = at;
     return w;
@@ -504,6 +616,17 @@ bool start_products(unsigned grid, const Grad& a, hipStream_t st) {
 }
 bool launch_dz(Form f, unsigned grid, const Grad& a, hipStream_t st) {
     return f == kRing ? start_dz<Ring>(grid, a, st) : f == kMid128 ? start_dz<Mid128>(grid, a, st) : f == kMidFew ? start_dz<MidFew>(grid, a, st) : start_dz<Mid64>(grid, a, st);
+}
+template <class C>
+bool start_found(unsigned grid, const Grad& a, const Gather& g, hipStream_t st) {
+    static arrol_device_flags ok;
+    constexpr int kBytes = C::LDS_BYTES + sizeof(Found);
+    if (!arrol_allow_lds(&dz_found_kernel<C>, kBytes, ok)) return false;
+    arrol_launch(dz_found_kernel<C>, dim3(grid), dim3(C::NT), kBytes, st, a, g);
+    return true;
+}
+bool launch_found(Form f, unsigned grid, const Grad& a, const Gather& g, hipStream_t st) {
+    return f == kMid128 ? start_found<Mid128>(grid, a, g, st) : f == kMidFew ? start_found<MidFew>(grid, a, g, st) : start_found<Mid64>(grid, a, g, st);
 }
 bool launch_products(Form f, const Grad& a, hipStream_t st) {
     const unsigned grid = static_cast<unsigned>(a.grid_h + a.grid_w);
@@ -556,8 +679,9 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
         g.H = const_cast<uint16_t*>(a.H), g.grad_hidden = grad_hidden ? static_cast<uint16_t*>(grad_hidden) + t0 * d : nullptr;
         g.g = const_cast<float*>(a.g), g.lse_out = const_cast<float*>(a.lse), g.target = const_cast<int32_t*>(a.target), g.row = const_cast<int32_t*>(a.row);
         g.n_active = const_cast<int32_t*>(a.n_active), g.T = static_cast<int>(rows), g.V = V, g.d = d;
-        if (rows <= 1024) arrol_launch(gather_kernel<4>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, g);
-        else arrol_launch(gather_kernel<16>, dim3(static_cast<unsigned>((rows + 15) / 16)), dim3(256), 0, st, g);
+        const bool found = p.dz != kRing && rows <= kFoundTokens && p.n_v == 1, want_head = grad_lm_head || lm_head_sum;
+        if (!found) arrol_launch(gather_kernel, dim3(static_cast<unsigned>((rows + kGatherRows - 1) / kGatherRows)), dim3(256), 0, st, g);
+        if (!want_head) g.H = nullptr;
         const bool direct = p.slabs == 1 && p.n_v == 1;
         a.slab_stride = rows * d;
         a.slabs = direct ? nullptr : reinterpret_cast<float*>(base + ws.slabs);
@@ -565,22 +689,24 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
         for (int64_t q = 0; q < p.n_v; ++q) {
             const int64_t v0 = q * p.v, n_v = V - v0 < p.v ? V - v0 : p.v;
             a.W = static_cast<const uint16_t*>(lm_head) + v0 * d, a.v0 = static_cast<int>(v0), a.n_v = static_cast<int>(n_v), a.v_stride = static_cast<int>(p.v);
-            if (!launch_dz(p.dz, rounded(tiles_of(rows, n_v, kSize[p.dz].bn, kSize[p.dz].bm)), a, st)) return refused();
+            const unsigned grid = rounded(tiles_of(rows, n_v, kSize[p.dz].bn, kSize[p.dz].bm));
+            if (!(found ? launch_found(p.dz, grid, a, g, st) : launch_dz(p.dz, grid, a, st))) return refused();
             a.k64_per_slab = p.k64_per_slab, a.add = q > 0;
             a.grid_h = grad_hidden ? static_cast<int>(rounded(tiles_of(rows, d, size.bn, size.bm) * p.slabs)) : 0;
             a.grid_w = 0;
-            if (grad_lm_head || lm_head_sum) {
-                a.grid_w = static_cast<int>(rounded(tiles_of(n_v, d, size.bn_w, size.bm_w)));
+            if (want_head) {
+                a.grid_w = static_cast<int>(rounded(tiles_of(n_v, d, size.bn_w, size.bm_w) * p.parts));
+                a.slabs_w = p.parts > 1 ? reinterpret_cast<float*>(base + ws.slabs_w) : nullptr;
+                a.slab_w_stride = n_v * d, a.k64_per_part = static_cast<int>(((rows + 63) / 64 + p.parts - 1) / p.parts);
                 a.sum = (lm_head_sum ? lm_head_sum : reinterpret_cast<float*>(base + ws.sum)) + v0 * d;
                 a.grad_w = grad_lm_head ? static_cast<uint16_t*>(grad_lm_head) + v0 * d : nullptr;
                 a.read_sum = lm_head_sum || piece > 0, a.write_sum = lm_head_sum || piece + 1 < p.n_rows;
             }
             if (!launch_products(p.products, a, st)) return refused();
-        }
-        if (grad_hidden && !direct) {
-            const int64_t blocks = (rows * (d / 4) + 255) / 256;
-            arrol_launch(join_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a.slabs, a.slab_stride, p.slabs, a.row, a.n_active,
-                         d, a.grad_hidden);
+            const bool join_h = grad_hidden && !direct && q + 1 == p.n_v, join_w = want_head && p.parts > 1;
+            const int64_t blocks_h = join_h ? (rows * (d / 4) + 255) / 256 : 0, blocks_w = join_w ? (n_v * (d / 4) + 255) / 256 : 0;
+            const unsigned of_h = static_cast<unsigned>(blocks_h < 4096 ? blocks_h : 4096), of_w = static_cast<unsigned>(blocks_w < 4096 ? blocks_w : 4096);
+            if (join_h || join_w) arrol_launch(join_kernel, dim3(of_h + of_w), dim3(256), 0, st, a, p.slabs, static_cast<int>(of_h));
         }
     }
     return arrol_launch_status();

@@ -47,7 +47,8 @@ struct Stream {
     const char* base;
     unsigned voff[N], stride;
     int k[N], left;          // K-major: row of the step, and rows that exist from it on
-    __device__ __forceinline__ void start(const char* b, unsigned s, int rows, int k_rows, int wave, int lane) {
+    template <class RowOf>
+    __device__ __forceinline__ void start(const char* b, unsigned s, int rows, int k_rows, int wave, int lane, RowOf row_of) {
         base = b;
         stride = s;
         left = k_rows;
@@ -61,7 +62,7 @@ struct Stream {
             } else {
                 const int r = 8 * u + (lane >> 3);
                 k[q] = 0;
-                voff[q] = static_cast<unsigned>(r < rows ? r : rows - 1) * stride + ((lane & 7) ^ (r & 6)) * 16;
+                voff[q] = static_cast<unsigned>(row_of(r < rows ? r : rows - 1)) * stride + ((lane & 7) ^ (r & 6)) * 16;
             }
         }
     }
@@ -79,10 +80,14 @@ struct Stream {
     }
 };
 
+struct InOrder {
+    __device__ __forceinline__ int operator()(int r) const { return r; }
+};
+
 // As ring_nt::walk, but the accumulators belong to C's tile; the LDS is not to be touched afterwards without a barrier.  tail: 16-byte chunks of a row that
-// exist in the last step, 1 .. 8 (K-major operands: 8).
-template <class C, bool B_KMAJOR = false, bool A_KMAJOR = false>
-__device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8) {
+// exist in the last step, 1 .. 8 (K-major operands: 8).  b_row: where row r of a B that is given row by row lies (rows of b_base, their bytes below 2^32).
+template <class C, bool B_KMAJOR = false, bool A_KMAJOR = false, class RowOf = InOrder>
+__device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int tail = 8, RowOf b_row = RowOf()) {
     constexpr int BM = C::BM, BN = C::BN, TI = C::TI, TJ = C::TJ, NS = C::NS;
     constexpr bool kTail = !A_KMAJOR && !B_KMAJOR;
     typedef __attribute__((address_space(3))) void* lds_ptr_t;
@@ -98,8 +103,8 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
     if (steps <= 0) return;
     Stream<BM, C::LA, A_KMAJOR> a;
     Stream<BN, C::LB, B_KMAJOR> b;
-    a.start(w.a_base, w.a_stride, w.a_rows, w.a_k_rows, wave, lane);
-    b.start(w.b_base, w.b_stride, w.b_rows, w.b_k_rows, wave, lane);
+    a.start(w.a_base, w.a_stride, w.a_rows, w.a_k_rows, wave, lane, InOrder());
+    b.start(w.b_base, w.b_stride, w.b_rows, w.b_k_rows, wave, lane, b_row);
     const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((lds_ptr_t)lds));
     unsigned dst = lds0;
     int issued = 0;
