@@ -1,13 +1,15 @@
 """Generation and update of pruned rollouts on one paged pool, as an engine around the library would run them.
 
-A toy transformer (attention layers with a residual, random weights) goes through one step of the method:
+A toy transformer (attention layers with rotated positions and a residual, random weights) goes through one step of the method:
 
-  prompts    arrol_attention over the packed prompts, their keys and values into pages that all rollouts of a prompt share
-  decode     arrol_decode_attention, one token a rollout, the prompt read once for its group; weights gathered over layers and tokens
+  prompts    arrol_append: keys and values into pages that all rollouts of a prompt share, keys and queries turned by their positions; arrol_attention over the
+             packed prompts
+  decode     arrol_append and arrol_decode_attention, one token a rollout, the prompt read once for its group; weights gathered over layers and tokens
   prune      arrol_score on the hidden states, arrol_select, arrol_compact_inplace on rollouts and prompts together
   evict      arrol_evict: the survivors' own caches cut to a budget by the gathered weights
-  decode     the survivors go on, on what is left of their caches
-  update     arrol_attention on the survivors' packed rows, arrol_logprob, and arrol_attention_grad
+  decode     the survivors go on, on what is left of their caches, their positions counted on
+  update     on the survivors' packed rows arrol_rotary, arrol_attention, arrol_logprob and the GRPO objective, and back: arrol_logprob_grad, arrol_attention_grad and
+             arrol_rotary's inverse, to the gradients of LM head and projection
 
   python examples/rollout_attention.py
 """
@@ -33,6 +35,8 @@ class Toy:
         self.qkv = [rand(cfg.d, (n_heads + 2 * cfg.n_kv_heads) * cfg.head_dim) for _ in range(cfg.n_layers)]
         self.out = [rand(n_heads * cfg.head_dim, cfg.d) for _ in range(cfg.n_layers)]
         self.embed = W.randn_bf16((cfg.vocab, cfg.d), g, dev)
+        self.head = W.randn_bf16((cfg.vocab, cfg.d), g, dev, std=cfg.d ** -0.5)
+        self.inv_freq = A.arrol_rotary_frequencies(cfg.head_dim, device=dev)
 
     def project(self, layer, x):
         """Queries, keys and values as slices of one projection."""
@@ -61,22 +65,16 @@ def run(cfg=None, n_heads=4, steps=20, budget=12, dev="cuda:0", seed=3):
     table[N:, :prompt_pages] = pages[N * own_pages:].view(B, prompt_pages)
     kv = torch.zeros(cfg.n_layers, 2, pages.numel(), page, toy.KV, toy.hd, dtype=torch.bfloat16, device=dev)
 
-    def put(layer, rows, at, k, v):
-        """Keys and values of token at[i] of table row rows[i]."""
-        ids, slot = table[rows, at // page].long(), at % page
-        kv[layer, 0, ids, slot], kv[layer, 1, ids, slot] = k, v
-
     # prompts, packed
     prompt_len = torch.randint(1, cfg.ckpt_len + 1, (B,), generator=g, device=dev, dtype=torch.int32)
     cu = offsets(prompt_len, dev)
     T = int(cu[-1])
-    seq = torch.searchsorted(cu, torch.arange(T, device=dev), right=True) - 1
     tokens = torch.randint(0, cfg.vocab, (T,), generator=g, device=dev)
     x = toy.embed[tokens]
     for layer in range(cfg.n_layers):
         q, k, v = toy.project(layer, x)
-        put(layer, N + seq, torch.arange(T, device=dev) - cu[seq], k, v)
-        x = toy.add(layer, x, A.arrol_attention(q, k, v, cu)[0])
+        new = A.arrol_append(k, v, kv, layer, table[N:], torch.zeros(B, dtype=torch.int32, device=dev), cu, q=q, inv_freq=toy.inv_freq, want_k=True)
+        x = toy.add(layer, x, A.arrol_attention(new["q"], new["k"], v, cu)[0])
 
     seq_len = torch.zeros(N, dtype=torch.int32, device=dev)
     group = torch.arange(B + 1, device=dev, dtype=torch.int64) * cfg.G
@@ -89,12 +87,13 @@ def run(cfg=None, n_heads=4, steps=20, budget=12, dev="cuda:0", seed=3):
         n = seq_len.numel()
         new = torch.randint(0, cfg.vocab, (n,), generator=g, device=dev)
         history.append(new)
-        rows, at, x = torch.arange(n, device=dev), seq_len.long(), toy.embed[new]
+        at, x = seq_len.clone(), toy.embed[new]
+        position = prompt_len.repeat_interleave(n // B) + len(history) - 1      # what has been evicted counts
         seq_len.add_(1)
         for layer in range(cfg.n_layers):
             q, k, v = toy.project(layer, x)
-            put(layer, rows, at, k, v)
-            got = A.arrol_decode_attention(q.contiguous(), kv, layer, table[:n], seq_len, table[n:], prompt_len, group, want_weight=True, weight=weight, out_weight=weight)
+            q = A.arrol_append(k, v, kv, layer, table[:n], at, q=q, position=position, inv_freq=toy.inv_freq)["q"]
+            got = A.arrol_decode_attention(q, kv, layer, table[:n], seq_len, table[n:], prompt_len, group, want_weight=True, weight=weight, out_weight=weight)
             x = toy.add(layer, x, got["out"])
         return x, dict(q=q, k=k, v=v, layer=layer, **got)
 
@@ -127,14 +126,29 @@ def run(cfg=None, n_heads=4, steps=20, budget=12, dev="cuda:0", seed=3):
     cu_s = offsets(lengths, dev)
     packed = torch.cat([torch.cat([tokens[cu[b]:cu[b + 1]], response[r]]) for r, b in ((r, r // cfg.K) for r in range(n))])
     x = toy.embed[packed]
+    within = torch.arange(packed.numel(), device=dev) - cu_s[:-1].repeat_interleave(lengths)
+    position = within.to(torch.int32)
     q, k, v = toy.project(0, x)
+    q, k = A.arrol_rotary(q, k, position, toy.inv_freq)
     out, lse = A.arrol_attention(q, k, v, cu_s)
     y = toy.add(0, x, out)
-    logprob = A.arrol_logprob(y.contiguous(), toy.embed, torch.roll(packed, -1).to(torch.int32))
-    # d(sum of log-probs)/d(attention's output) by way of a stand-in for the rest of the backward pass
-    grad = A.arrol_attention_grad(q, k, v, out, lse, (y @ toy.out[0].t()).view(out.shape).contiguous(), cu_s)
+    targets = torch.roll(packed, -1).to(torch.int32)
+    logprob, lse_v = A.arrol_logprob(y, toy.head, targets, want_lse=True)
+    reward = torch.randint(0, 2, (n,), generator=g, device=dev).float()
+    advantage, share = A.arrol_grpo_advantage(reward, group)
+    old = logprob + 0.1 * torch.randn(logprob.shape, generator=g, device=dev)
+    objective, grad_logp, _ = A.arrol_grpo_objective(logprob, old, cu_s, advantage, share)
+    # the tokens that were generated, not the prompts' nor what would follow the last one
+    trained = (within + 1 >= prompt_len.repeat_interleave(cfg.K).repeat_interleave(lengths)) & (within + 1 < lengths.repeat_interleave(lengths))
+    grad_logp = torch.where(trained, grad_logp, torch.zeros_like(grad_logp))
+    d_logits = A.arrol_logprob_grad(y, toy.head, targets, lse_v, grad_logp)
+    grad = A.arrol_attention_grad(q, k, v, out, lse, (d_logits["grad_hidden"] @ toy.out[0].t()).view(out.shape), cu_s)
+    grad["grad_q"], grad["grad_k"] = A.arrol_rotary(grad["grad_q"], grad["grad_k"], position, toy.inv_freq, inverse=True)
+    grad["projection"] = x.t() @ torch.cat([grad["grad_q"], grad["grad_k"], grad["grad_v"]], 1).flatten(1)
+    grad.update(d_logits)
     torch.cuda.synchronize()
-    return dict(checkpoint=checkpoint, kept=kept, moved=moved, evicted=evicted, last=last, hidden=hidden, toy=toy, logprob=logprob, grad=grad, cfg=cfg)
+    update = dict(x=x, cu=cu_s, position=position, targets=targets, grad_logp=grad_logp, objective=objective)
+    return dict(checkpoint=checkpoint, kept=kept, moved=moved, evicted=evicted, last=last, hidden=hidden, toy=toy, logprob=logprob, grad=grad, update=update, cfg=cfg)
 
 
 if __name__ == "__main__":

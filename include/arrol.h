@@ -249,6 +249,16 @@ size_t arrol_logprob_grad_workspace_bytes(int64_t T, int32_t V, int32_t d, int32
 int arrol_logprob_grad(const void* hidden, const void* lm_head, const int32_t* targets, const float* lse, const float* grad_logp,
                        int64_t T, int32_t V, int32_t d, void* grad_hidden, void* grad_lm_head, float* lm_head_sum,
                        void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Test and measurement aid, a host computation: what arrol_logprob_grad takes for a call, so that a test can say what it reaches.
+ * *logit_rows, *logit_tokens        vocabulary rows and tokens of a workgroup's tile of dz
+ * *product_columns, *product_tokens columns and tokens of one of dL/dh (its tiles of dL/dW: 256 x 256, 64 x 64 with 64 x 64, otherwise 128 x 128)
+ * *slabs, *parts                    parts that the vocabulary is cut into for dL/dh, and the tokens for dL/dW
+ * *pieces                           pieces of tokens times pieces of the vocabulary
+ * *found                            1 where the workgroups of dz find the tokens that take part by themselves, 0 where a launch before them does
+ */
+int arrol_logprob_grad_kernels(int64_t T, int32_t V, int32_t d, int32_t* logit_rows, int32_t* logit_tokens, int32_t* product_columns,
+                               int32_t* product_tokens, int32_t* slabs, int32_t* parts, int32_t* pieces, int32_t* found);
 
 /*
  * Stage 5 -- rank-weighted vote (Sec. 4.4: candidates are sorted by head score and their

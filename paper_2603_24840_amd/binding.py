@@ -78,6 +78,7 @@ _SIGNATURES = {
     "arrol_logprob": (ctypes.c_int, [_vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _i32, _vp, _sz, _vp]),
     "arrol_logprob_grad_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "arrol_logprob_grad": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "arrol_logprob_grad_kernels": (ctypes.c_int, [_i64, _i32, _i32] + [_vp] * 8),
     "arrol_logprob_kernel": (ctypes.c_int, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
     "arrol_logprob_streamed": (ctypes.c_int, [_i64, _i32, _i32, _i32, _vp]),
     "arrol_token_confidence_workspace_bytes": (_sz, [_i32, _i32]),

@@ -576,6 +576,8 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
     return p;
 }
 
+bool found_by_dz(const Pieces& p, int64_t rows) { return p.dz != kRing && rows <= kFoundTokens && p.n_v == 1; }
+
 struct Workspace {
     size_t H, g, lse, target, row, n_active, dz, slabs, slabs_w, sum, bytes;
 };
@@ -647,6 +649,15 @@ extern "C" size_t arrol_logprob_grad_workspace_bytes(int64_t T, int32_t V, int32
     return sizes_ok(T, V, d) && T > 0 ? workspace(T, V, d, want_lm_head != 0).bytes : 0;
 }
 
+extern "C" int arrol_logprob_grad_kernels(int64_t T, int32_t V, int32_t d, int32_t* logit_rows, int32_t* logit_tokens, int32_t* product_columns, int32_t* product_tokens,
+                                          int32_t* slabs, int32_t* parts, int32_t* n_pieces, int32_t* found) {
+    if (!sizes_ok(T, V, d) || T < 1 || !logit_rows || !logit_tokens || !product_columns || !product_tokens || !slabs || !parts || !n_pieces || !found) return ARROL_EINVAL;
+    const Pieces p = pieces(T, V, d);
+    *logit_rows = kSize[p.dz].bm, *logit_tokens = kSize[p.dz].bn, *product_columns = kSize[p.products].bm, *product_tokens = kSize[p.products].bn;
+    *slabs = p.slabs, *parts = p.parts, *n_pieces = static_cast<int32_t>(p.n_rows * p.n_v < 0x7fffffff ? p.n_rows * p.n_v : 0x7fffffff), *found = found_by_dz(p, p.rows);
+    return ARROL_OK;
+}
+
 extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const int32_t* targets, const float* lse, const float* grad_logp, int64_t T, int32_t V,
                                   int32_t d, void* grad_hidden, void* grad_lm_head, float* lm_head_sum, void* workspace_, size_t workspace_bytes, void* stream) {
     if (!sizes_ok(T, V, d) || (!grad_hidden && !grad_lm_head && !lm_head_sum && T > 0) || (grad_lm_head && lm_head_sum)) return ARROL_EINVAL;
@@ -679,7 +690,7 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
         g.H = const_cast<uint16_t*>(a.H), g.grad_hidden = grad_hidden ? static_cast<uint16_t*>(grad_hidden) + t0 * d : nullptr;
         g.g = const_cast<float*>(a.g), g.lse_out = const_cast<float*>(a.lse), g.target = const_cast<int32_t*>(a.target), g.row = const_cast<int32_t*>(a.row);
         g.n_active = const_cast<int32_t*>(a.n_active), g.T = static_cast<int>(rows), g.V = V, g.d = d;
-        const bool found = p.dz != kRing && rows <= kFoundTokens && p.n_v == 1, want_head = grad_lm_head || lm_head_sum;
+        const bool found = found_by_dz(p, rows), want_head = grad_lm_head || lm_head_sum;
         if (!found) arrol_launch(gather_kernel, dim3(static_cast<unsigned>((rows + kGatherRows - 1) / kGatherRows)), dim3(256), 0, st, g);
         if (!want_head) g.H = nullptr;
         const bool direct = p.slabs == 1 && p.n_v == 1;

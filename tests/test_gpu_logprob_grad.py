@@ -81,6 +81,39 @@ def test_gradient(A, T, V, d):
     check(A, *make(T, V, d, seed=T + V))
 
 
+KERNELS = [(1211, 46, 8), (2044, 41, 8), (19579, 39, 8), (3047, 516, 8), (5, 538, 5376), (3, 7073, 408), (811, 43, 4944), (215, 5014, 1216), (984, 1231, 3960), (202, 3792, 2816),
+           (1022, 2639, 368), (225, 15340, 664), (467, 9258, 568), (394, 14224, 448), (1152, 11261, 536), (4392, 3092, 192), (4025, 2946, 576), (2579, 3172, 1728), (724, 17984, 384),
+           (15386, 6011, 192), (1046, 3757, 8)]
+
+
+def kernels(A, T, V, d):
+    """What the call takes, as the header numbers it."""
+    import ctypes
+    out = [ctypes.c_int32() for _ in range(8)]
+    assert A.lib().arrol_logprob_grad_kernels(T, V, d, *[ctypes.byref(x) for x in out]) == 0
+    names = ("logit_rows", "logit_tokens", "product_columns", "product_tokens", "slabs", "parts", "pieces", "found")
+    return dict(zip(names, [x.value for x in out]))
+
+
+@pytest.mark.parametrize("T,V,d", KERNELS)
+def test_gradient_in_every_form(A, T, V, d):
+    print("[case] logprob_grad T=%d V=%d d=%d %s" % (T, V, d, kernels(A, T, V, d)), flush=True)
+    h, w, y, lse, g = make(T, V, d, seed=T + d)
+    check(A, h, w, y, lse, g)
+    total = torch.full((V, d), -1.0, device=DEV)
+    A.arrol_logprob_grad(h, w, y, lse, g, want_hidden=False, lm_head_sum=total)
+    dW, tW = reference(h, w, y, lse, g)[2:]
+    agree("lm_head_sum", total, dW - 1, tW + 8 * E * (1 + dW.abs()), norm=False)
+
+
+def test_every_form_is_reached(A):
+    got = [kernels(A, *x) for x in KERNELS]
+    tiles = {(256, 256), (128, 128), (128, 64), (64, 64)}
+    assert {(k["logit_rows"], k["logit_tokens"]) for k in got} == tiles and {(k["product_columns"], k["product_tokens"]) for k in got} == tiles
+    assert {(k["logit_rows"], k["logit_tokens"]) for k in got if k["found"]} == tiles - {(256, 256)} and {(k["logit_rows"], k["logit_tokens"]) for k in got if not k["found"]} == tiles
+    assert {(k["slabs"] > 1, k["parts"] > 1) for k in got} == {(a, b) for a in (False, True) for b in (False, True)} and any(k["pieces"] > 1 and k["parts"] > 1 for k in got)
+
+
 @pytest.mark.parametrize("T,V,d", [(16385, 300, 64), (16384, 20000, 64), (33000, 17000, 72)])
 def test_gradient_in_pieces(A, T, V, d):
     """More than 16,384 tokens, and more than 2^28 values of dz."""

@@ -53,3 +53,16 @@ def test_binding_refuses(A):
                      ((h, w, y, f, f), dict(lm_head_sum=torch.zeros(9, 64))), ((h, w, y, f, f), dict(want_hidden=False, want_lm_head=False)), ((h[0], w, y, f, f), {})):
         with pytest.raises((TypeError, ValueError)):
             A.arrol_logprob_grad(*args, **kw)
+
+
+def test_kernel_query(A):
+    out = [ctypes.c_int32(-7) for _ in range(8)]
+    ask = lambda T, V, d, n=8: A.lib().arrol_logprob_grad_kernels(T, V, d, *[ctypes.byref(x) for x in out[:n]], *[None] * (8 - n))
+    for bad in ((0, 10, 64), (-1, 10, 64), (10, 0, 64), (10, 10, 60), (10, 10, 16392)):
+        assert ask(*bad) == -1 and all(x.value == -7 for x in out)
+    assert ask(10, 10, 64, 7) == -1
+    for T, V, d in ((1, 1, 8), (16384, 151936, 4096), (10 ** 9, 2 ** 24, 16384), (40000, 300, 64), (1024, 5000, 1000)):
+        assert ask(T, V, d) == 0
+        rows, tokens, columns, product_tokens, slabs, parts, pieces, found = (x.value for x in out)
+        assert rows in (64, 128, 256) and columns in (64, 128, 256) and tokens in (64, 128, 256) and product_tokens in (64, 128, 256)
+        assert (rows != 256 or d % 64 == 0) and 1 <= slabs <= 32 and 1 <= parts <= 32 and pieces >= 1 and (not found or (T <= 1024 and rows < 256))
