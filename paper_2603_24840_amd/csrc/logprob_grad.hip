@@ -28,6 +28,9 @@ constexpr int kXcds = 8, kRound = 256;
 constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
 constexpr int kFoundTokens = 1024;
+// An LM head of more elements than these is more than the 256 MiB cache holds, and so is its gradient: that goes past the caches, where its lines would have to be written back
+// while the next call reads (16 x 151,936 x 2048, calls one after the other: dz 191 us, so 132; the call 532 and 491.  128 tokens: 608 and 551).
+constexpr int64_t kCachedElements = int64_t{1} << 27;
 
 // The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
 typedef ring_nt::RingTile<256, 256, 2, 4> Ring;
@@ -57,6 +60,7 @@ struct Grad {
     uint16_t* grad_hidden;
     int grid_h, grid_w;             // workgroups of dL/dh and of dL/dW, 0 where not wanted
     // dL/dW of the piece
+    bool stream;                    // W and its gradient do not fit the caches: stored past them
     float* sum;                     // fp32 sums, read and / or written
     uint16_t* grad_w;
     int read_sum, write_sum;
@@ -335,7 +339,7 @@ __global__ __launch_bounds__(C::NT) void dz_found_kernel(Grad a, Gather g) {
 }
 
 // The epilogue of both products: acc[i][j][v] belongs to column c0 + 16 i + 4 lq + v of row r0 + 16 j + l15.  sum: fp32, read and / or written; else bf16.
-template <class C, class RowOf>
+template <class C, bool PAST = false, class RowOf>
 __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int r0, int rows, int c0, int d, float* sum, bool read, bool write, uint16_t* out, RowOf row_of) {
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
@@ -357,7 +361,10 @@ __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C:
             } else {
                 const u32x4 packed = exchange(x, y);      // by all lanes
                 const int c = c0 + me.place(i);
-                if (live && c < d) *reinterpret_cast<u32x4*>(to + c) = packed;
+                if (live && c < d) {
+                    if constexpr (PAST) __builtin_nontemporal_store(packed, reinterpret_cast<u32x4*>(to + c));
+                    else *reinterpret_cast<u32x4*>(to + c) = packed;
+                }
             }
         }
     }
@@ -426,7 +433,9 @@ struct HeadTiles {
     __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
         const int r0 = vt * C::BN + me.wave % C::WN * (C::BN / C::WN), c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM);
         const bool parts = a.slabs_w != nullptr;
-        store_rows<C>(me, acc, r0, a.n_v, c0, a.d, parts ? a.slabs_w + s * a.slab_w_stride : a.sum, !parts && a.read_sum, parts || a.write_sum, a.grad_w, [](int r) { return r; });
+        const auto same = [](int r) { return r; };
+        if (a.stream && !a.write_sum) store_rows<C, true>(me, acc, r0, a.n_v, c0, a.d, a.sum, a.read_sum, false, a.grad_w, same);      // of such a size there are no parts
+        else store_rows<C>(me, acc, r0, a.n_v, c0, a.d, parts ? a.slabs_w + s * a.slab_w_stride : a.sum, !parts && a.read_sum, parts || a.write_sum, a.grad_w, same);
     }
 };
 
@@ -681,7 +690,7 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
     a.g = reinterpret_cast<float*>(base + ws.g), a.lse = reinterpret_cast<float*>(base + ws.lse);
     a.target = reinterpret_cast<int32_t*>(base + ws.target), a.row = reinterpret_cast<int32_t*>(base + ws.row);
     a.n_active = reinterpret_cast<int32_t*>(base + ws.n_active);
-    a.d = d;
+    a.d = d, a.stream = static_cast<int64_t>(V) * d > kCachedElements;
     const Size& size = kSize[p.products];
     for (int64_t piece = 0; piece < p.n_rows; ++piece) {
         const int64_t t0 = piece * p.rows, rows = T - t0 < p.rows ? T - t0 : p.rows;
