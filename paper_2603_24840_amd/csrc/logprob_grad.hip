@@ -15,7 +15,7 @@
 // Up to kFoundTokens tokens (and middle-sized tiles) there is no launch for the first step: every workgroup of the second finds the tokens by itself, and each copies some.
 // No atomics: sums have a fixed order.
 //
-// What bounds it.  Large batches: the matrix cores under the card's power limit.  4,873 tokens (4,721 that take part) x 128,256 x 2048 6.6 to 6.8 ms, 1.16 to 1.19 PFLOP/s, on cards
+// What bounds it.  Large batches: the matrix cores under the card's power limit.  5,130 tokens (4,970 that take part) x 128,256 x 2048 6.6 to 6.8 ms, 1.16 to 1.19 PFLOP/s, on cards
 // where torch's 16,384 x 16,384 x 8,192 product reaches 1.29 and its products of these three shapes 1.18, 0.59 and 0.98; 6,278 x 151,936 x 4096 18.0 to 18.7 ms, 1.21 to 1.26.
 // Of the dz launches 13 % is the epilogue (2,253 us, 1,961 without, 2,145 without its stores, 2,229 without exponentials).  Few tokens: reading W twice and writing its
 // gradient, 16 x 151,936 x 2048 478 us (1.87 GB: 3.9 TB/s).  Small calls: three or four launches of 3 to 8 us.
