@@ -253,7 +253,7 @@ int arrol_logprob_grad(const void* hidden, const void* lm_head, const int32_t* t
  * Test and measurement aid, a host computation: what arrol_logprob_grad takes for a call, so that a test can say what it reaches.
  * *logit_rows, *logit_tokens        vocabulary rows and tokens of a workgroup's tile of dz
  * *product_columns, *product_tokens columns and tokens of one of dL/dh (its tiles of dL/dW: 256 x 256, 64 x 64 with 64 x 64, otherwise 128 x 128)
- * *slabs, *parts                    parts that the vocabulary is cut into for dL/dh, and the tokens for dL/dW
+ * *slabs, *parts                    parts that the vocabulary is cut into for dL/dh, and the tokens for dL/dW; *parts 0: dL/dW with the hidden states in registers
  * *pieces                           pieces of tokens times pieces of the vocabulary
  * *found                            1 where the workgroups of dz find the tokens that take part by themselves, 0 where a launch before them does
  */

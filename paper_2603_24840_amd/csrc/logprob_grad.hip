@@ -10,7 +10,8 @@
 //   per piece of the vocabulary:
 //   dz         256 x 256 tiles of W h, dz in the epilogue, stored token-major through the LDS in whole lines
 //   products   tiles of dL/dh (dz as it lies, W read in place down its rows) and of dL/dW (dz and the hidden states both read down their rows), in one launch, so that
-//              the long walks of the first and the many short ones of the second fill the chip together
+//              the long walks of the first and the many short ones of the second fill the chip together.  Up to kResidentTokens tokens of a large vocabulary dL/dW keeps the hidden
+//              states in registers instead
 //   join       where K extents of the products are cut into parts, whose sums go to slabs: the slabs added in order
 // Up to kFoundTokens tokens (and middle-sized tiles) there is no launch for the first step: every workgroup of the second finds the tokens by itself, and each copies some.
 // No atomics: sums have a fixed order.
@@ -18,8 +19,10 @@
 // What bounds it.  Large batches: the matrix cores under the card's power limit.  5,130 tokens (4,970 that take part) x 128,256 x 2048 6.6 to 6.8 ms, 1.16 to 1.19 PFLOP/s, on cards
 // where torch's 16,384 x 16,384 x 8,192 product reaches 1.29 and its products of these three shapes 1.18, 0.59 and 0.98; 6,278 x 151,936 x 4096 18.0 to 18.7 ms, 1.21 to 1.26.
 // Of the dz launches 13 % is the epilogue (2,253 us, 1,961 without, 2,145 without its stores, 2,229 without exponentials).  Few tokens: reading W twice and writing its
-// gradient, 16 x 151,936 x 2048 478 us (1.87 GB: 3.9 TB/s).  Small calls: three or four launches of 3 to 8 us.
-// Not kept: 256 workgroups that walk over tiles, the next tile's loads under way during an epilogue (dz 1.4 % faster, products 3.5 % slower); the K-major offsets of the ring
+// gradient, 16 x 151,936 x 2048 397 us (1.87 GB: 4.7 TB/s).  Between them, 311 x 151,936 x 2048 711 us: the LDS, into which tiles of 128 x 160 bring 36 KB and out of which they read
+// 72 KB a step of 640 cycles of products (matrix cores busy 38 % in dz and dL/dh).  Small calls: three or four launches of 3 to 8 us.
+// Not kept: in 128 x 160 tiles the next but one step's loads before the products, with a second barrier (even), the last step peeled off (dz 258 to 363: registers), tiles of 128 x 320 and
+// 256 x 320 for dz (even, and 8 % faster at 151,936 but 37 % slower at 32,000); 256 workgroups that walk over tiles, the next tile's loads under way during an epilogue (dz 1.4 % faster, products 3.5 % slower); the K-major offsets of the ring
 // formed ahead (products 4.5 % slower); dL/dh with the operands' roles exchanged, bands of 4, pieces of 2^27 to 2^30 values (even).
 #include "common.h"
 #include "mid_nt.h"
@@ -43,6 +46,7 @@ constexpr int64_t kCachedElements = int64_t{1} << 27;
 typedef ring_nt::RingTile<256, 256, 2, 4> Ring;
 template <int BM, int BN, int NS> using Mid = mid_nt::Tile<BM, BN, 2, 2, NS>;
 typedef Mid<128, 128, 2> Mid128;
+typedef Mid<128, 160, 2> Mid160;
 typedef Mid<128, 64, 3> MidFew;
 typedef Mid<64, 64, 3> Mid64;
 template <class C, bool B_KMAJOR, bool A_KMAJOR>
@@ -74,6 +78,7 @@ struct Grad {
     float* slabs_w;                 // [parts][piece's rows][d], NULL: no parts
     int64_t slab_w_stride;
     int k64_per_part;
+    int blocks;                     // of 64 of the piece's rows that a workgroup of ResidentTiles walks over
 };
 
 // Place in a work order in which every round of 256 workgroups gives each XCD (workgroup ids congruent mod 8) 32 that follow each other.  -1: none.
@@ -240,13 +245,15 @@ struct Tokens {
 };
 
 // acc[i][j][v] = z of vocabulary row 16 i + 4 (lane / 16) + v and token 16 j + lane % 16 of the wavefront's part of the tile.  dz of rows past the vocabulary and of
-// tokens past the last are zeros: the products' K extents are whole steps of 64.
+// tokens past the last, up to a multiple of 64, are zeros: the products' K extents are whole steps of 64.
 template <class C>
 __device__ __forceinline__ void store_dz(const Grad& a, const Lane& me, const Tokens<C>& tokens, const f32x4 (&acc)[C::TI][C::TJ], int vt, int tb, int n_active) {
     const int v_first = vt * C::BM + me.wave / C::WN * (C::BM / C::WM), t_first = tb * C::BN + me.wave % C::WN * (C::BN / C::WN);
+    const int rows = (n_active + 63) / 64 * 64;
     const bool edge = v_first + C::BM / C::WM > a.n_v || t_first + C::BN / C::WN > n_active;
 #pragma unroll
     for (int j = 0; j < C::TJ; ++j) {
+        if (t_first + j * 16 >= rows) break;
         const int t = t_first + j * 16 + me.l15;
         const float g = tokens.g[j], at = tokens.at[j];
         const int y = tokens.target[j] - a.v0 - v_first - 4 * me.lq;        // of this lane's rows: 16 i + v
@@ -274,6 +281,13 @@ __device__ __forceinline__ void store_dz(const Grad& a, const Lane& me, const To
 #pragma unroll
             for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(to + me.place(i)) = exchange(plain(i), plain(i + 1));
         }
+    }
+    if constexpr (C::BN % 64 != 0) {        // the zeros of a multiple of 64 that ends behind the last tile, 32 tokens at most
+        static_assert(C::BN % 64 == 32 && C::WN == 2, "tokens behind the tile");
+        const int t = (tb + 1) * C::BN + me.wave % 2 * 16 + me.l15;
+        if ((tb + 1) * C::BN >= n_active && t < rows)
+#pragma unroll
+            for (int i = 0; i < C::TI; i += 2) *reinterpret_cast<u32x4*>(a.dz + static_cast<int64_t>(t) * a.v_stride + v_first + me.place(i)) = u32x4{0, 0, 0, 0};
     }
 }
 
@@ -446,6 +460,176 @@ struct HeadTiles {
     }
 };
 
+// dL/dW of up to kResidentTokens tokens.  A wavefront keeps 64 columns of the hidden states of all tokens in registers (160 of its 254) and walks down the vocabulary, 64 rows
+// of dz at a time, which its workgroup of 256 columns shares: one barrier for the products of all tokens, and the next rows' loads and the last ones' stores under way meanwhile.
+// The accesses of a wavefront complete in the order of their issue, so a wait for the loads counts the eight stores behind them, which come on no branch where a block is whole.
+// 151,936 x 2048, this launch's dL/dW alone: 64 tokens 130 us (4.8 TB/s, bound by the stores), 192 177, 311 205 (622 MB at 3.0 TB/s and 0.94 PFLOP/s; matrix cores busy 41 %); tiles of 128 x 128
+// take 190 at 64 tokens and 332 at 311.  Stores of whole lines of 128 bytes instead of halves: 64 tokens 185 to 130, 311 214 to 205.  Blocks to a workgroup, 311 tokens, both products: 4 736, 8 717, 16 722.
+constexpr int kResidentSteps = 5, kResidentTokens = kResidentSteps * 64;
+struct ResidentTiles {
+    static constexpr int kStage = kResidentSteps * 8192, LDS_BYTES = 2 * kStage;
+    struct Part {                   // for store_rows
+        static constexpr int TI = 4, TJ = 2;
+    };
+    typedef __attribute__((address_space(3))) void* lds_ptr_t;
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
+
+    const Grad& a;
+    const int n_active, n_db, n_vb;
+    __device__ __forceinline__ ResidentTiles(const Grad& a, int n) : a(a), n_active(n), n_db((a.d + 255) / 256), n_vb((a.n_v + 63) / 64) {}
+    __device__ __forceinline__ int total() const { return (n_vb + a.blocks - 1) / a.blocks * n_db; }
+
+    static __device__ __forceinline__ void load(const char* base, unsigned off, unsigned dst) {
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory");
+    }
+    // Eight consecutive rows 8 (lane / 16) .. of column lane % 16 of block i, from a step of 64 rows of 128 bytes (off as in mid_nt::walk).
+    static __device__ __forceinline__ bf16x8 down(const unsigned char* at, const int (&off)[2], int i) {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + (off[0] ^ (i << 5))));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + (off[1] ^ (i << 5))));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+
+    template <bool PAST>
+    __device__ __forceinline__ void run(const Lane& me, unsigned char* lds, int pos) const {
+        const Grad& a = this->a;
+        const int db = __builtin_amdgcn_readfirstlane(pos % n_db), b0 = __builtin_amdgcn_readfirstlane(pos / n_db * a.blocks), b1 = b0 + a.blocks < n_vb ? b0 + a.blocks : n_vb;
+        const int steps = (n_active + 63) / 64, c0 = db * 256 + me.wave * 64;
+        const bool idle = c0 >= a.d;
+        const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((lds_ptr_t)lds));
+        int off[2];
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+            const int e = me.l15 >> 2, q = me.l15 & 3, k = 8 * me.lq + 4 * h2 + e;
+            off[h2] = k * 128 + (((q >> 1) ^ mid_nt::k_swizzle<64>(k)) << 4) + (q & 1) * 8;
+        }
+        const int row = me.lane >> 3;       // of 8 that a load fetches
+
+        // the hidden states, two steps at a time through the wavefront's own quarter of the LDS
+        bf16x8 h[kResidentSteps][2][4];
+        const int valid = a.d - c0 < 64 ? (a.d - c0) / 8 : 8;
+        const unsigned own = lds0 + me.wave * (LDS_BYTES / 4);
+        const char* const h_base = reinterpret_cast<const char*>(a.H) + c0 * 2;
+#pragma unroll
+        for (int k0 = 0; k0 < kResidentSteps; k0 += 2) {
+            if (idle || k0 >= steps) break;
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                if (k0 + u / 8 >= kResidentSteps || k0 + u / 8 >= steps) break;
+                const int r = 8 * u + row, t = k0 * 64 + r, c = (me.lane & 7) ^ mid_nt::k_swizzle<64>(r & 63);
+                load(h_base, static_cast<unsigned>(t < n_active ? t : n_active - 1) * (a.d * 2u) + (c < valid ? c : valid - 1) * 16, own + u * 1024);
+            }
+            mid_nt::wait_vmcnt<0>();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int k = k0; k < k0 + 2 && k < kResidentSteps; ++k)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[k][half][i] = down(lds + me.wave * (LDS_BYTES / 4) + (k - k0) * 8192 + half * 4096, off, i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        __syncthreads();
+
+        const char* base = reinterpret_cast<const char*>(a.dz) + static_cast<int64_t>(b0) * 128;
+        const unsigned stride = static_cast<unsigned>(a.v_stride) * 2;
+        unsigned voff[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = (me.wave * 2 + u) * 8 + row;
+            voff[u] = r * stride + ((me.lane & 7) ^ mid_nt::k_swizzle<64>(r)) * 16;
+        }
+        auto issue = [&](int stage) {
+            const char* from = base;
+            for (int k = 0; k < steps; ++k) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) load(from, voff[u], lds0 + stage * kStage + k * 8192 + (me.wave * 2 + u) * 1024);
+                from += static_cast<int64_t>(stride) * 64;
+            }
+            base += 128;
+        };
+        if (b0 < b1) issue(0);
+        const bool rows_out = !a.write_sum && !a.read_sum && c0 + 64 <= a.d;
+        bool counted = false;               // the wavefront's last eight accesses are the stores of the block before
+        for (int b = b0; b < b1; ++b) {
+            if (counted) mid_nt::wait_vmcnt<8>();
+            else mid_nt::wait_vmcnt<0>();
+            __syncthreads();
+            const int stage = (b - b0) & 1;
+            if (b + 1 < b1) issue(stage ^ 1);
+            if (idle) continue;
+            const unsigned char* st = lds + stage * kStage;
+            counted = rows_out && b * 64 + 64 <= a.n_v;
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                f32x4 acc[4][2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < kResidentSteps; ++k) {
+                    if (k >= steps) break;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const unsigned char* at = st + k * 8192 + half * 4096;
+                        const bf16x8 f0 = down(at, off, j), f1 = down(at, off, j + 1);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            acc[i][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[k][half][i], f0, acc[i][0], 0, 0, 0);
+                            acc[i][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[k][half][i], f1, acc[i][1], 0, 0, 0);
+                        }
+                    }
+                }
+                const int r0 = b * 64 + j * 16;
+                if (counted) {
+#pragma unroll
+                    for (int jj = 0; jj < 2; ++jj) {
+                        // whole lines: lanes of rows r and r + 8 exchange halves, so that a store is 128 bytes of eight rows
+                        const bool low = me.l15 < 8;
+                        uint16_t* to = a.grad_w + static_cast<int64_t>(r0 + jj * 16 + (me.l15 & 7)) * a.d + c0 + me.place(low ? 0 : 2);
+                        const u32x4 x = exchange(acc[0][jj], acc[1][jj]), y = exchange(acc[2][jj], acc[3][jj]);
+                        u32x4 first, second;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const unsigned other = __builtin_amdgcn_update_dpp(0, low ? y[v] : x[v], 0x128, 0xf, 0xf, false);      // of lane l15 ^ 8
+                            first[v] = low ? x[v] : other;
+                            second[v] = low ? other : y[v];
+                        }
+                        if constexpr (PAST) {
+                            __builtin_nontemporal_store(first, reinterpret_cast<u32x4*>(to));
+                            __builtin_nontemporal_store(second, reinterpret_cast<u32x4*>(to + 8 * static_cast<int64_t>(a.d)));
+                        } else {
+                            *reinterpret_cast<u32x4*>(to) = first;
+                            *reinterpret_cast<u32x4*>(to + 8 * static_cast<int64_t>(a.d)) = second;
+                        }
+                    }
+                } else store_rows<Part>(me, acc, r0, a.n_v, c0, a.d, a.sum, a.read_sum, a.write_sum, a.grad_w, [](int r) { return r; });
+            }
+        }
+    }
+};
+
+template <class CH>
+__global__ __launch_bounds__(CH::NT, 2) void products_resident_kernel(Grad a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int n_active = __builtin_amdgcn_readfirstlane(*a.n_active);
+    if (static_cast<int>(blockIdx.x) < a.grid_h) {
+        const HiddenTiles<CH> tiles(a, n_active);
+        const int pos = place(blockIdx.x, tiles.total());
+        if (pos < 0) return;
+        int s, tb, db;
+        tiles.at(pos, s, tb, db);
+        f32x4 acc[CH::TI][CH::TJ];
+        multiply<CH, false, true>(tiles.walk(s, tb, db), lds, acc);
+        tiles.store(Lane(), acc, s, tb, db);
+        return;
+    }
+    const ResidentTiles tiles(a, n_active);
+    const int pos = place(blockIdx.x - a.grid_h, tiles.total());
+    if (pos < 0) return;
+    if (a.stream && !a.write_sum) tiles.run<true>(Lane(), lds, pos);
+    else tiles.run<false>(Lane(), lds, pos);
+}
+
 template <class CH, class CW>
 __global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -515,19 +699,23 @@ int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
 // Which forms a piece takes, of dz and of the products: those whose estimated times are the smallest.  Measured, microseconds: what a tile costs beside its K64
 // steps, a step where the chip is full (of every one of the `per_unit` workgroups that a compute unit has at a time) and a step where it is not.  1,024 x 32,000 x 2048:
-// dz 114 / 138 / 179 / 206, products 250 / 242 / 286 / 407; 318 x 4,096 x 256: 14.5 / 9.1 / 6.5 / 6.9 and 17.6 / 8.7 / 7.8 / 7.7; 16 x 151,936 x 2048 (LM head from memory, and
-// its gradient to it): 249 / 221 / 189 / 177 and 306 / 328 / 331 / 330.
-enum Form { kRing, kMid128, kMidFew, kMid64, kForms };
+// dz 111 / 154 / 148 / 197 / 220, products 245 / 249 / 246 / 293 / 446; 640 tokens of it: 103 / 91 / 107 / 122 / 137 and 175 / 158 / 166 / 193 / 276; 318 x 4,096 x 256:
+// 14.9 / 11.4 / 9.7 / 7.9 / 7.4 and 19.4 / 10.0 / 9.3 / 9.2 / 6.8; 16 x 151,936 x 2048 (LM head from memory, and its gradient to it): 249 / 150 / 221 / 133 / 135 of dz.
+enum Form { kRing, kMid160, kMid128, kMidFew, kMid64, kForms };
 struct Size {
     int bm, bn, bm_w, bn_w;         // of dz and dL/dh, and of dL/dW
     int per_unit;
     double tile, step, lone, tile_w, step_w, lone_w;
 };
-constexpr Size kSize[kForms] = {{256, 256, 256, 256, 1, 8.7, 1.45, 1.1, 10.0, 1.55, 1.1}, {128, 128, 128, 128, 2, 4.8, 0.95, 0.53, 4.2, 0.95, 0.53},
+constexpr Size kSize[kForms] = {{256, 256, 256, 256, 1, 8.7, 1.45, 1.1, 10.0, 1.55, 1.1}, {128, 160, 128, 128, 2, 5.5, 1.07, 0.6, 4.2, 0.95, 0.53}, {128, 128, 128, 128, 2, 4.8, 0.95, 0.53, 4.2, 0.95, 0.53},
                                 {128, 64, 128, 128, 2, 1.7, 0.66, 0.33, 4.2, 0.95, 0.53}, {64, 64, 64, 64, 3, 1.4, 0.57, 0.2, 2.0, 0.6, 0.2}};
 
 constexpr int kMaxSlabs = 32, kSlabTiles = 512;     // of 256 x 256
 constexpr int64_t kSlabFloats = kSlabTiles * int64_t{65536};
+// From so many blocks of 64 x 256 on, seven to a compute unit, the hidden states' way into the registers is worth it.  The launch of the products, resident and in tiles: 311 x 151,936 x 2048
+// (19,000 blocks) 457 us and 600, 16 tokens 260 and 335, 110 x 79,125 x 3264 228 and 272, 300 x 32,000 x 1024 (2,000) 54 and 61; 250 x 20,000 x 1000 (1,252) 38.4 and 34.8, 320 x 16,384 x 512
+// (512) 22.7 and 19.8.
+constexpr int kResidentBlocks = 1792;
 constexpr double kJoin = 3.5, kJoinBytes = 3e6;      // microseconds; bytes a microsecond
 
 struct Pieces {
@@ -536,6 +724,7 @@ struct Pieces {
     Form dz, products;
     int slabs, k64_per_slab;        // parts of the vocabulary piece that dL/dh's K extent is cut into, and their steps
     int parts;                      // of the tokens that dL/dW's is
+    int blocks;                     // of 64 vocabulary rows to a workgroup of the resident form of dL/dW, 0: the tiles of `products`
 };
 int64_t tiles_of(int64_t n, int64_t m, int bn, int bm) { return ((n + bn - 1) / bn) * ((m + bm - 1) / bm); }
 
@@ -545,11 +734,14 @@ double dz_time(const Size& f, int64_t rows, int64_t v, int64_t d) {
     const double up = static_cast<double>(static_cast<int64_t>(r + 0.999));
     return (up < r + 0.5 ? up : r + 0.5) * (f.tile + steps * f.step);       // of many rounds the last one's workgroups start early
 }
-double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, int slabs, int parts) {
-    const double n_h = static_cast<double>(tiles_of(rows, d, f.bn, f.bm) * slabs), n_w = static_cast<double>(tiles_of(v, d, f.bn_w, f.bm_w) * parts);
-    const double k_h = static_cast<double>((v / 64 + slabs - 1) / slabs), k_w = static_cast<double>(((rows + 63) / 64 + parts - 1) / parts), places = 256.0 * f.per_unit;
-    const double all = (n_h * (f.tile + k_h * f.step) + n_w * (f.tile_w + k_w * f.step_w)) / places;
-    const double lone_h = f.tile + k_h * f.lone, lone_w = f.tile_w + k_w * f.lone_w, longest = lone_h > lone_w ? lone_h : lone_w;
+// blocks: of the resident form of dL/dW, 0: tiles.  The resident form, two workgroups to a compute unit: 3.0 + 2.0 for every 64 tokens to fetch the hidden states, 3.0 + 0.5 a block; alone on
+// it 2.0 + 1.0 and 1.2 + 0.2.
+double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, int slabs, int parts, int blocks) {
+    const double n_h = static_cast<double>(tiles_of(rows, d, f.bn, f.bm) * slabs), n_w = static_cast<double>(blocks ? tiles_of(v, d, 64 * blocks, 256) : tiles_of(v, d, f.bn_w, f.bm_w) * parts);
+    const double k_h = static_cast<double>((v / 64 + slabs - 1) / slabs), k_w = static_cast<double>(((rows + 63) / 64 + parts - 1) / parts), places = 256.0 * (blocks ? 2 : f.per_unit);
+    const double each_w = blocks ? 3.0 + 2.0 * k_w + blocks * (3.0 + 0.5 * k_w) : f.tile_w + k_w * f.step_w;
+    const double lone_h = f.tile + k_h * f.lone, lone_w = blocks ? 2.0 + k_w + blocks * (1.2 + 0.2 * k_w) : f.tile_w + k_w * f.lone_w, longest = lone_h > lone_w ? lone_h : lone_w;
+    const double all = (n_h * (f.tile + k_h * f.step) + n_w * each_w) / places;
     return n_h + n_w <= places ? (all > longest ? all : longest) : all + longest / 2;
 }
 void choose_forms(Pieces& p, int64_t d) {
@@ -565,14 +757,16 @@ void choose_forms(Pieces& p, int64_t d) {
         parts = parts < kMaxSlabs ? parts : kMaxSlabs;
         if (parts * p.v * d > kSlabFloats) parts = kSlabFloats / (p.v * d);
         const int64_t tile = static_cast<int64_t>(size.bm) * size.bn, tiles = tiles_of(p.rows, d, size.bn, size.bm), k64 = p.v / 64;
-        for (int with = 0; with < (parts > 1 ? 2 : 1); ++with) {
-            const int n = with ? static_cast<int>(parts) : 1;
+        const bool resident = f != kRing && p.rows <= kResidentTokens && tiles_of(p.v, d, 64, 256) >= kResidentBlocks;
+        for (int with = 0; with < 5; ++with) {          // 0: one part, 1: those parts, 2 ..: resident hidden states and 4, 8 or 16 blocks
+            if ((with == 1 && parts < 2) || (with > 1 && !resident)) continue;
+            const int n = with == 1 ? static_cast<int>(parts) : 1, blocks = with > 1 ? 1 << with : 0;
             for (int s = 1; s <= kMaxSlabs; s += s < 4 ? 1 : s / 4) {
                 if (s > 1 && (s > k64 / 2 || s * tiles * tile > kSlabFloats)) break;
                 const bool join_h = s > 1 || p.n_v > 1;
-                const double join = join_h || with ? kJoin + ((join_h ? 4.0 * s * p.rows * d : 0.0) + (with ? 4.0 * n * p.v * d : 0.0)) / kJoinBytes : 0.0;
-                const double t = products_time(size, p.rows, p.v, d, s, n) + join;
-                if (t < best) best = t, p.products = static_cast<Form>(f), p.slabs = s, p.parts = n;
+                const double join = join_h || with == 1 ? kJoin + ((join_h ? 4.0 * s * p.rows * d : 0.0) + (with == 1 ? 4.0 * n * p.v * d : 0.0)) / kJoinBytes : 0.0;
+                const double t = products_time(size, p.rows, p.v, d, s, n, blocks) + join;
+                if (t < best) best = t, p.products = static_cast<Form>(f), p.slabs = s, p.parts = n, p.blocks = blocks;
             }
         }
     }
@@ -633,7 +827,7 @@ bool start_products(unsigned grid, const Grad& a, hipStream_t st) {
     return start<products_kernel<CH, CW>, CH::NT, (CH::LDS_BYTES > CW::LDS_BYTES ? CH::LDS_BYTES : CW::LDS_BYTES)>(grid, a, st);
 }
 bool launch_dz(Form f, unsigned grid, const Grad& a, hipStream_t st) {
-    return f == kRing ? start_dz<Ring>(grid, a, st) : f == kMid128 ? start_dz<Mid128>(grid, a, st) : f == kMidFew ? start_dz<MidFew>(grid, a, st) : start_dz<Mid64>(grid, a, st);
+    return f == kRing ? start_dz<Ring>(grid, a, st) : f == kMid160 ? start_dz<Mid160>(grid, a, st) : f == kMid128 ? start_dz<Mid128>(grid, a, st) : f == kMidFew ? start_dz<MidFew>(grid, a, st) : start_dz<Mid64>(grid, a, st);
 }
 template <class C>
 bool start_found(unsigned grid, const Grad& a, const Gather& g, hipStream_t st) {
@@ -644,11 +838,18 @@ bool start_found(unsigned grid, const Grad& a, const Gather& g, hipStream_t st) 
     return true;
 }
 bool launch_found(Form f, unsigned grid, const Grad& a, const Gather& g, hipStream_t st) {
-    return f == kMid128 ? start_found<Mid128>(grid, a, g, st) : f == kMidFew ? start_found<MidFew>(grid, a, g, st) : start_found<Mid64>(grid, a, g, st);
+    return f == kMid160 ? start_found<Mid160>(grid, a, g, st) : f == kMid128 ? start_found<Mid128>(grid, a, g, st) : f == kMidFew ? start_found<MidFew>(grid, a, g, st) : start_found<Mid64>(grid, a, g, st);
+}
+template <class CH>
+bool start_resident(unsigned grid, const Grad& a, hipStream_t st) {
+    return start<products_resident_kernel<CH>, CH::NT, (CH::LDS_BYTES > ResidentTiles::LDS_BYTES ? CH::LDS_BYTES : ResidentTiles::LDS_BYTES)>(grid, a, st);
 }
 bool launch_products(Form f, const Grad& a, hipStream_t st) {
     const unsigned grid = static_cast<unsigned>(a.grid_h + a.grid_w);
-    return f == kRing ? start_products<Ring, Ring>(grid, a, st) : f == kMid128 ? start_products<Mid128, Mid128>(grid, a, st)
+    if (a.blocks)
+        return f == kMid160 ? start_resident<Mid160>(grid, a, st) : f == kMid128 ? start_resident<Mid128>(grid, a, st)
+             : f == kMidFew ? start_resident<MidFew>(grid, a, st) : start_resident<Mid64>(grid, a, st);
+    return f == kRing ? start_products<Ring, Ring>(grid, a, st) : f == kMid160 ? start_products<Mid160, Mid128>(grid, a, st) : f == kMid128 ? start_products<Mid128, Mid128>(grid, a, st)
          : f == kMidFew ? start_products<MidFew, Mid128>(grid, a, st) : start_products<Mid64, Mid64>(grid, a, st);
 }
 
@@ -670,7 +871,7 @@ extern "C" int arrol_logprob_grad_kernels(int64_t T, int32_t V, int32_t d, int32
     if (!sizes_ok(T, V, d) || T < 1 || !logit_rows || !logit_tokens || !product_columns || !product_tokens || !slabs || !parts || !n_pieces || !found) return ARROL_EINVAL;
     const Pieces p = pieces(T, V, d);
     *logit_rows = kSize[p.dz].bm, *logit_tokens = kSize[p.dz].bn, *product_columns = kSize[p.products].bm, *product_tokens = kSize[p.products].bn;
-    *slabs = p.slabs, *parts = p.parts, *n_pieces = static_cast<int32_t>(p.n_rows * p.n_v < 0x7fffffff ? p.n_rows * p.n_v : 0x7fffffff), *found = found_by_dz(p, p.rows);
+    *slabs = p.slabs, *parts = p.blocks ? 0 : p.parts, *n_pieces = static_cast<int32_t>(p.n_rows * p.n_v < 0x7fffffff ? p.n_rows * p.n_v : 0x7fffffff), *found = found_by_dz(p, p.rows);
     return ARROL_OK;
 }
 
@@ -722,7 +923,8 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
             a.grid_h = grad_hidden ? static_cast<int>(rounded(tiles_of(rows, d, size.bn, size.bm) * p.slabs)) : 0;
             a.grid_w = 0;
             if (want_head) {
-                a.grid_w = static_cast<int>(rounded(tiles_of(n_v, d, size.bn_w, size.bm_w) * p.parts));
+                a.grid_w = static_cast<int>(rounded(p.blocks ? tiles_of(n_v, d, 64 * p.blocks, 256) : tiles_of(n_v, d, size.bn_w, size.bm_w) * p.parts));
+                a.blocks = p.blocks;
                 a.slabs_w = p.parts > 1 ? reinterpret_cast<float*>(base + ws.slabs_w) : nullptr;
                 a.slab_w_stride = n_v * d, a.k64_per_part = static_cast<int>(((rows + 63) / 64 + p.parts - 1) / p.parts);
                 a.sum = (lm_head_sum ? lm_head_sum : reinterpret_cast<float*>(base + ws.sum)) + v0 * d;

@@ -11,8 +11,8 @@
 // Rows, chunks and K rows past the end repeat the last ones: loads stay inside the operands.  Of K rows past the end one operand holds zeros; of the chunks past
 // the end of a row (the last step of a K extent that is no multiple of 64, both operands row by row) the fragments are cleared.
 //
-// Bound by the LDS where the chip is full (128 x 128: 64 KB of fragments and 32 KB of loads a K64 step at 128 bytes a cycle are half as long again as the products; two workgroups
-// to a compute unit, 0.95 us a step for both), and by each step's chain of barrier, fragments and products where it is not (64 x 64: 0.2 to 0.3 us a step, however many stages the loads are ahead).
+// Bound by the LDS where the chip is full (a K64 step of 128 x 160: 72 KB of fragments at 128 bytes a cycle and 36 KB of loads at 64 are 1,150 cycles, the products 640; two workgroups
+// to a compute unit), and by each step's chain of barrier, fragments and products where it is not (64 x 64: 0.2 to 0.3 us a step, however many stages the loads are ahead).
 #pragma once
 #include "common.h"
 #include "ring_nt.h"
@@ -29,7 +29,7 @@ struct Tile {
     static constexpr int TI = BM / WM / 16, TJ = BN / WN / 16;
     static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB;      // loads of a wavefront and step, 1 KiB each
     static constexpr int STAGE_BYTES = (BM + BN) * 128, LDS_BYTES = NS * STAGE_BYTES;
-    static_assert((BM == 64 || BM == 128) && (BN == 64 || BN == 128) && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NS >= 2, "tile");
+    static_assert((BM == 64 || BM == 128) && BN % 32 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && NS >= 2, "tile");
     static_assert((NS - 2) * LOADS < 64, "loads that may be in flight behind a wait");
 };
 
@@ -103,6 +103,7 @@ __device__ __forceinline__ void walk(const Walk& w, unsigned char* lds, f32x4 (&
     for (int i = 0; i < TI; ++i)
 #pragma unroll
         for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    static_assert(!B_KMAJOR || BN == 64 || BN == 128, "swizzle");
     if (steps <= 0) return;
     Stream<BM, C::LA, A_KMAJOR> a;
     Stream<BN, C::LB, B_KMAJOR> b;

@@ -83,7 +83,8 @@ def test_gradient(A, T, V, d):
 
 KERNELS = [(1211, 46, 8), (2044, 41, 8), (19579, 39, 8), (3047, 516, 8), (5, 538, 5376), (3, 7073, 408), (811, 43, 4944), (215, 5014, 1216), (984, 1231, 3960), (202, 3792, 2816),
            (1022, 2639, 368), (225, 15340, 664), (467, 9258, 568), (394, 14224, 448), (1152, 11261, 536), (4392, 3092, 192), (4025, 2946, 576), (2579, 3172, 1728), (724, 17984, 384),
-           (15386, 6011, 192), (1046, 3757, 8)]
+           (15386, 6011, 192), (1046, 3757, 8), (131, 51545, 8), (1948, 4612, 8), (146, 6790, 1016), (155, 60441, 280), (74, 58503, 264), (311, 60001, 264), (1, 60000, 264),
+           (239, 8272, 3792), (53, 7924, 3992), (9, 140000, 960)]
 
 
 def kernels(A, T, V, d):
@@ -108,10 +109,36 @@ def test_gradient_in_every_form(A, T, V, d):
 
 def test_every_form_is_reached(A):
     got = [kernels(A, *x) for x in KERNELS]
-    tiles = {(256, 256), (128, 128), (128, 64), (64, 64)}
+    tiles = {(256, 256), (128, 160), (128, 128), (128, 64), (64, 64)}
     assert {(k["logit_rows"], k["logit_tokens"]) for k in got} == tiles and {(k["product_columns"], k["product_tokens"]) for k in got} == tiles
     assert {(k["logit_rows"], k["logit_tokens"]) for k in got if k["found"]} == tiles - {(256, 256)} and {(k["logit_rows"], k["logit_tokens"]) for k in got if not k["found"]} == tiles
     assert {(k["slabs"] > 1, k["parts"] > 1) for k in got} == {(a, b) for a in (False, True) for b in (False, True)} and any(k["pieces"] > 1 and k["parts"] > 1 for k in got)
+    assert {(k["product_columns"], k["product_tokens"]) for k in got if k["parts"] == 0} == tiles - {(256, 256)}
+
+
+@pytest.mark.parametrize("T,V,d", [(320, 60001, 264), (65, 30016, 1000)])
+def test_few_tokens_of_a_large_vocabulary(A, T, V, d):
+    """The hidden states of all tokens in registers: as many tokens as fit, as few as none, a workspace of NaN, NaN of one that takes part."""
+    print("[case] logprob_grad resident T=%d V=%d d=%d" % (T, V, d), flush=True)
+    assert kernels(A, T, V, d)["parts"] == 0
+    h, w, y, lse, g = make(T, V, d, seed=11, idle=0)
+    ws = torch.full((A.lib().arrol_logprob_grad_workspace_bytes(T, V, d, 1),), 255, dtype=torch.uint8, device=DEV)
+    want = check(A, h, w, y, lse, g)
+    got = A.arrol_logprob_grad(h, w, y, lse, g, workspace=ws)
+    assert all(torch.equal(want[x], got[x]) for x in want)
+    assert torch.equal(A.arrol_logprob_grad(h, w, y, lse, g, want_hidden=False)["grad_lm_head"], want["grad_lm_head"])
+    one = torch.zeros_like(g)
+    one[T - 1] = g[T - 1]
+    check(A, h, w, y, lse, one)
+    total = torch.full((V, d), 2.0, device=DEV)
+    got = A.arrol_logprob_grad(h, w, y, lse, torch.zeros_like(g), workspace=ws)
+    A.arrol_logprob_grad(h, w, y, lse, torch.zeros_like(g), lm_head_sum=total)
+    assert not got["grad_hidden"].any() and not got["grad_lm_head"].any() and bool((total == 2).all())
+    x = h.clone()
+    x[T // 2, 5] = float("nan")
+    got = A.arrol_logprob_grad(x, w, y, lse, g)
+    others = torch.arange(T, device=DEV) != T // 2
+    assert torch.equal(got["grad_hidden"][others], want["grad_hidden"][others]) and bool(torch.isnan(got["grad_lm_head"]).all())
 
 
 @pytest.mark.parametrize("T,V,d", [(16385, 300, 64), (16384, 20000, 64), (33000, 17000, 72)])
