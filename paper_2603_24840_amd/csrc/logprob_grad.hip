@@ -184,6 +184,18 @@ struct Lane {
     __device__ __forceinline__ int place(int i) const { return 16 * (i + (lq & 1)) + 4 * (lq & 2); }      // of exchange()'s values
 };
 
+// x, y: exchange()'s of 64 consecutive columns of the lane's row.  Lanes of rows r and r + 8 exchange halves: `first` belongs to row lane % 8 of the 16, `second` to the row
+// 8 on, both at place(0), or place(2) for the upper lanes, so that a store is whole lines of eight rows.
+__device__ __forceinline__ void whole_lines(const Lane& me, u32x4 x, u32x4 y, u32x4& first, u32x4& second) {
+    const bool low = me.l15 < 8;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const unsigned other = __builtin_amdgcn_update_dpp(0, low ? y[v] : x[v], 0x128, 0xf, 0xf, false);      // of lane l15 ^ 8
+        first[v] = low ? x[v] : other;
+        second[v] = low ? other : y[v];
+    }
+}
+
 // The tokens that take part, found by a workgroup of 256 by itself, up to kFoundTokens of them: their numbers in `list`, the others' bits in `masks` clear; how many.
 struct Found {
     uint64_t masks[kFoundTokens / ARROL_WAVE];
@@ -372,6 +384,17 @@ __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C:
             const int c = c0 + 16 * i + 4 * me.lq;
             return read && live && c < d ? *reinterpret_cast<const f32x4*>(sum + line + c) + acc[i][j] : acc[i][j];
         };
+        if constexpr (PAST && C::TI % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < C::TI; i += 4) {
+                u32x4 first, second;
+                whole_lines(me, exchange(value(i), value(i + 1)), exchange(value(i + 2), value(i + 3)), first, second);
+                const int row = r0 + j * 16 + (me.l15 & 7), c = c0 + me.place(i + (me.l15 < 8 ? 0 : 2));
+                if (row < rows && c < d) __builtin_nontemporal_store(first, reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row_of(row)) * d + c));
+                if (row + 8 < rows && c < d) __builtin_nontemporal_store(second, reinterpret_cast<u32x4*>(out + static_cast<int64_t>(row_of(row + 8)) * d + c));
+            }
+            continue;
+        }
 #pragma unroll
         for (int i = 0; i < C::TI; i += 2) {
             const f32x4 x = value(i), y = value(i + 1);
@@ -583,17 +606,9 @@ struct ResidentTiles {
                 if (counted) {
 #pragma unroll
                     for (int jj = 0; jj < 2; ++jj) {
-                        // whole lines: lanes of rows r and r + 8 exchange halves, so that a store is 128 bytes of eight rows
-                        const bool low = me.l15 < 8;
-                        uint16_t* to = a.grad_w + static_cast<int64_t>(r0 + jj * 16 + (me.l15 & 7)) * a.d + c0 + me.place(low ? 0 : 2);
-                        const u32x4 x = exchange(acc[0][jj], acc[1][jj]), y = exchange(acc[2][jj], acc[3][jj]);
+                        uint16_t* to = a.grad_w + static_cast<int64_t>(r0 + jj * 16 + (me.l15 & 7)) * a.d + c0 + me.place(me.l15 < 8 ? 0 : 2);
                         u32x4 first, second;
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const unsigned other = __builtin_amdgcn_update_dpp(0, low ? y[v] : x[v], 0x128, 0xf, 0xf, false);      // of lane l15 ^ 8
-                            first[v] = low ? x[v] : other;
-                            second[v] = low ? other : y[v];
-                        }
+                        whole_lines(me, exchange(acc[0][jj], acc[1][jj]), exchange(acc[2][jj], acc[3][jj]), first, second);
                         if constexpr (PAST) {
                             __builtin_nontemporal_store(first, reinterpret_cast<u32x4*>(to));
                             __builtin_nontemporal_store(second, reinterpret_cast<u32x4*>(to + 8 * static_cast<int64_t>(a.d)));
