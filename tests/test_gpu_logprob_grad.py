@@ -141,6 +141,14 @@ def test_few_tokens_of_a_large_vocabulary(A, T, V, d):
     assert torch.equal(got["grad_hidden"][others], want["grad_hidden"][others]) and bool(torch.isnan(got["grad_lm_head"]).all())
 
 
+@pytest.mark.parametrize("T,V,d", [(330, 140001, 968), (900, 69999, 1984), (330, 1200001, 120), (300, 600001, 264)])
+def test_gradient_larger_than_the_caches(A, T, V, d):
+    """An LM head's gradient that is stored past the caches, of odd sizes and in several forms."""
+    print("[case] logprob_grad past the caches T=%d V=%d d=%d %s" % (T, V, d, kernels(A, T, V, d)), flush=True)
+    assert V * d > 2 ** 27
+    check(A, *make(T, V, d, seed=5))
+
+
 @pytest.mark.parametrize("T,V,d", [(16385, 300, 64), (16384, 20000, 64), (33000, 17000, 72)])
 def test_gradient_in_pieces(A, T, V, d):
     """More than 16,384 tokens, and more than 2^28 values of dz."""
