@@ -62,6 +62,7 @@ struct Grad {
     const float *g, *lse;           // gathered
     const int32_t *target, *row;
     const int32_t* n_active;
+    float* rest;                    // of dz at a token's target: what its rounding to bf16 left
     int d, v0, n_v;                 // first row of the piece, and how many
     int v_stride;                   // of dz, a multiple of 256
     // dL/dh
@@ -281,7 +282,11 @@ __device__ __forceinline__ void store_dz(const Grad& a, const Lane& me, const To
             f32x4 x = plain(i);
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                if (mine && y == 16 * i + v) x[v] += g;
+                if (mine && y == 16 * i + v) {
+                    x[v] += g;
+                    const float rest = x[v] - static_cast<float>(static_cast<__bf16>(x[v]));
+                    a.rest[t] = fabsf(rest) < 3e38f ? rest : 0.f;       // infinities and NaN are in dz itself
+                }
                 if (t >= n_active || v_first + 16 * i + 4 * me.lq + v >= a.n_v) x[v] = 0.f;
             }
             return x;
@@ -347,7 +352,10 @@ __global__ __launch_bounds__(C::NT) void dz_found_kernel(Grad a, Gather g) {
     Found& found = *reinterpret_cast<Found*>(lds + C::LDS_BYTES);
     const int n_active = find_tokens(g, found), vecs = a.d / 8;
     if (blockIdx.x == 0) {
-        for (int r = threadIdx.x; r < n_active; r += 256) g.row[r] = found.list[r];
+        for (int r = threadIdx.x; r < n_active; r += 256) {
+            g.row[r] = found.list[r];
+            g.target[r] = g.targets[found.list[r]];
+        }
         if (threadIdx.x == 0) *g.n_active = n_active;
     }
     if (g.grad_hidden && n_active < g.T)
@@ -414,6 +422,19 @@ __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C:
     }
 }
 
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void add_times(f32x4& x, float f, bf16x4 four) {
+    const f32x4 y = __builtin_convertvector(four, f32x4);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) x[v] = fmaf(f, y[v], x[v]);
+}
+
+// dz is largest at a token's target by far, so of few tokens a gradient is as far off as that one rounding, 2^-8 at most, beside its own, and does not average out.  What dz lost there is
+// added in fp32: to dL/dh_t one row of W, up to kRestTokens tokens, to dL/dW a hidden state for every token whose target the row is, up to kResidentTokens.  The resident form of dL/dW has it
+// for nothing; its tiles need a barrier and a look at the tokens each (500 x 18,920 x 3128: products 132 us, with it 152; 64 x 4,096 x 1024 9.2 and 10.1).  What an
+// epilogue needs is asked for before its walk.
+constexpr int kRestTokens = 1024, kResidentSteps = 5, kResidentTokens = kResidentSteps * 64;
+
 // dL/dh: columns of W, which is read down its rows, times tokens' rows of dz; K = the vocabulary piece or a part of it.  Tile (s, at, db): part, tokens, columns.
 template <class C>
 struct HiddenTiles {
@@ -440,8 +461,36 @@ struct HiddenTiles {
         w.n_k64 = k_hi - k_lo;
         return w;
     }
-    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int s, int tb, int db) const {
+    // The rests of the piece's targets and where their rows of W are, for the first part; 0 and -1 otherwise.
+    struct Rests {
+        int y[C::TJ];
+        float rest[C::TJ];
+    };
+    __device__ __forceinline__ Rests rests(const Lane& me, int s, int tb) const {
+        Rests r;
+        const int t_first = tb * C::BN + me.wave % C::WN * (C::BN / C::WN) + me.l15;
+#pragma unroll
+        for (int j = 0; j < C::TJ; ++j) {
+            const int t = t_first + 16 * j;
+            const bool on = s == 0 && n_active <= kRestTokens && t < n_active;
+            r.y[j] = on ? a.target[t] - a.v0 : -1;
+            r.rest[j] = on ? a.rest[t] : 0.f;
+        }
+        return r;
+    }
+    __device__ __forceinline__ void store(const Lane& me, const Rests& rests, f32x4 (&acc)[C::TI][C::TJ], int s, int tb, int db) const {
         const Grad& a = this->a;
+        if (s == 0 && n_active <= kRestTokens) {
+            const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq;
+#pragma unroll
+            for (int j = 0; j < C::TJ; ++j) {
+                if (rests.y[j] < 0 || rests.y[j] >= a.n_v) continue;
+                const uint16_t* w = a.W + static_cast<int64_t>(rests.y[j]) * a.d + c0;
+#pragma unroll
+                for (int i = 0; i < C::TI; ++i)
+                    if (c0 + 16 * i < a.d) add_times(acc[i][j], rests.rest[j], *reinterpret_cast<const bf16x4*>(w + 16 * i));
+            }
+        }
         store_rows<C>(me, acc, tb * C::BN + me.wave % C::WN * (C::BN / C::WN), n_active, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.slabs + s * a.slab_stride, a.add,
                       a.slabs != nullptr, a.grad_hidden, [&](int t) { return a.row[t]; });
     }
@@ -474,7 +523,76 @@ struct HeadTiles {
         w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
         return w;
     }
-    __device__ __forceinline__ void store(const Lane& me, const f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
+    // The rows of the tile that are targets, of token threadIdx.x and every NT-th from it on, for the first part.
+    static constexpr int kRounds = (kResidentTokens + C::NT - 1) / C::NT;
+    struct Rests {
+        int row[kRounds];
+    };
+    __device__ __forceinline__ Rests rests(int s, int vt) const {
+        Rests r;
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+            const int t = u * C::NT + threadIdx.x;
+            r.row[u] = s == 0 && n_active <= kResidentTokens && t < n_active ? a.target[t] - a.v0 - vt * C::BN : -1;
+        }
+        return r;
+    }
+    // Their rests times the hidden states, token by token.  Every wavefront column has its own.
+    __device__ __forceinline__ void add_rests(const Lane& me, const Rests& rests, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int vt, int db) const {
+        constexpr int kAtOnce = C::TI > 4 ? 2 : 4, kRows = C::BN / C::WN, kMasks = kRounds * C::NW;
+        uint64_t* masks = reinterpret_cast<uint64_t*>(lds);         // [WN][kMasks], a bit for every token
+        __syncthreads();                    // all have read the last step
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u)
+#pragma unroll
+            for (int w = 0; w < C::WN; ++w) {
+                const uint64_t mask = __ballot(rests.row[u] >= w * kRows && rests.row[u] < (w + 1) * kRows);
+                if (me.lane == 0) masks[w * kMasks + u * C::NW + me.wave] = mask;
+            }
+        __syncthreads();
+        const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq, first = vt * C::BN + me.wave % C::WN * kRows;
+        const uint64_t mine = me.lane < kMasks ? masks[me.wave % C::WN * kMasks + me.lane] : 0;
+        uint64_t some = __ballot(mine != 0), tokens = 0;
+        int at = 0;
+        for (;;) {
+            int t[kAtOnce], row[kAtOnce];
+            float rest[kAtOnce];
+            bf16x4 h[kAtOnce][C::TI];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (!tokens && some) {
+                    at = __builtin_ctzll(some);
+                    some &= some - 1;
+                    tokens = static_cast<uint64_t>(__builtin_amdgcn_readlane(static_cast<unsigned>(mine >> 32), at)) << 32 |
+                             static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<unsigned>(mine), at));
+                }
+                t[k] = tokens ? at * 64 + __builtin_ctzll(tokens) : -1;
+                tokens &= tokens - 1;
+            }
+            if (t[0] < 0) break;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int from = t[k] < 0 ? 0 : t[k];
+                row[k] = a.target[from];
+                rest[k] = a.rest[from];
+#pragma unroll
+                for (int i = 0; i < C::TI; ++i) h[k][i] = *reinterpret_cast<const bf16x4*>(a.H + static_cast<int64_t>(from) * a.d + (c0 + 16 * i < a.d ? c0 + 16 * i : 0));
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (t[k] < 0) break;
+                const int r = __builtin_amdgcn_readfirstlane(row[k]) - a.v0 - first;
+#pragma unroll
+                for (int j = 0; j < C::TJ; ++j) {
+                    if (r >> 4 != j || (r & 15) != me.l15) continue;
+#pragma unroll
+                    for (int i = 0; i < C::TI; ++i) add_times(acc[i][j], rest[k], h[k][i]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const Lane& me, const Rests& rests, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
+        if (s == 0 && n_active <= kResidentTokens) add_rests(me, rests, lds, acc, vt, db);
         const int r0 = vt * C::BN + me.wave % C::WN * (C::BN / C::WN), c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM);
         const bool parts = a.slabs_w != nullptr;
         const auto same = [](int r) { return r; };
@@ -488,7 +606,6 @@ struct HeadTiles {
 // The accesses of a wavefront complete in the order of their issue, so a wait for the loads counts the eight stores behind them, which come on no branch where a block is whole.
 // 151,936 x 2048, this launch's dL/dW alone: 64 tokens 130 us (4.8 TB/s, bound by the stores), 192 177, 311 205 (622 MB at 3.0 TB/s and 0.94 PFLOP/s; matrix cores busy 41 %); tiles of 128 x 128
 // take 190 at 64 tokens and 332 at 311.  Stores of whole lines of 128 bytes instead of halves: 64 tokens 185 to 130, 311 214 to 205.  Blocks to a workgroup, 311 tokens, both products: 4 736, 8 717, 16 722.
-constexpr int kResidentSteps = 5, kResidentTokens = kResidentSteps * 64;
 struct ResidentTiles {
     static constexpr int kStage = kResidentSteps * 8192, LDS_BYTES = 2 * kStage;
     struct Part {                   // for store_rows
@@ -513,6 +630,24 @@ struct ResidentTiles {
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
+    // The rests of the tokens whose targets are among the 32 rows from `first` on times their hidden states, token by token.  target: of token 64 k + lane.
+    __device__ __forceinline__ void add_rests(const Lane& me, const int (&target)[kResidentSteps], f32x4 (&acc)[4][2], int first, int c0) const {
+#pragma unroll
+        for (int k = 0; k < kResidentSteps; ++k)
+            for (uint64_t tokens = __ballot(target[k] >= first && target[k] < first + 32); tokens; tokens &= tokens - 1) {
+                const int at = __builtin_ctzll(tokens), row = __builtin_amdgcn_readlane(target[k], at) - first;
+                const float rest = a.rest[k * 64 + at];
+                const uint16_t* h = a.H + static_cast<int64_t>(k * 64 + at) * a.d + c0 + 4 * me.lq;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (row >> 4 != j || (row & 15) != me.l15) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c0 + 4 * me.lq + 16 * i < a.d) add_times(acc[i][j], rest, *reinterpret_cast<const bf16x4*>(h + 16 * i));
+                }
+            }
+        mid_nt::wait_vmcnt<0>();        // or the compiler would wait for loads of this branch, and so for the stores, wherever it is left
+    }
     template <bool PAST>
     __device__ __forceinline__ void run(const Lane& me, unsigned char* lds, int pos) const {
         const Grad& a = this->a;
@@ -552,6 +687,17 @@ struct ResidentTiles {
                     for (int i = 0; i < 4; ++i) h[k][half][i] = down(lds + me.wave * (LDS_BYTES / 4) + (k - k0) * 8192 + half * 4096, off, i);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
+        int target[kResidentSteps];         // rows of the workgroup's
+        unsigned targets = 0;               // blocks that hold one
+#pragma unroll
+        for (int k = 0; k < kResidentSteps; ++k) {
+            const int t = k * 64 + me.lane;
+            target[k] = t < n_active ? a.target[t] - a.v0 - b0 * 64 : -1;
+            if (target[k] >= 0 && target[k] < (b1 - b0) * 64) targets |= 1u << (target[k] / 64);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o /= 2) targets |= __shfl_xor(targets, o);
+        targets = __builtin_amdgcn_readfirstlane(targets);
         __syncthreads();
 
         const char* base = reinterpret_cast<const char*>(a.dz) + static_cast<int64_t>(b0) * 128;
@@ -603,6 +749,7 @@ struct ResidentTiles {
                     }
                 }
                 const int r0 = b * 64 + j * 16;
+                if ((targets >> (b - b0)) & 1) add_rests(me, target, acc, r0 - b0 * 64, c0);
                 if (counted) {
 #pragma unroll
                     for (int jj = 0; jj < 2; ++jj) {
@@ -633,9 +780,10 @@ __global__ __launch_bounds__(CH::NT, 2) void products_resident_kernel(Grad a) {
         if (pos < 0) return;
         int s, tb, db;
         tiles.at(pos, s, tb, db);
+        const auto rests = tiles.rests(Lane(), s, tb);
         f32x4 acc[CH::TI][CH::TJ];
         multiply<CH, false, true>(tiles.walk(s, tb, db), lds, acc);
-        tiles.store(Lane(), acc, s, tb, db);
+        tiles.store(Lane(), rests, acc, s, tb, db);
         return;
     }
     const ResidentTiles tiles(a, n_active);
@@ -655,9 +803,10 @@ __global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
         if (pos < 0) return;
         int s, tb, db;
         tiles.at(pos, s, tb, db);
+        const auto rests = tiles.rests(Lane(), s, tb);
         f32x4 acc[CH::TI][CH::TJ];
         multiply<CH, false, true>(tiles.walk(s, tb, db), lds, acc);
-        tiles.store(Lane(), acc, s, tb, db);
+        tiles.store(Lane(), rests, acc, s, tb, db);
         return;
     }
     const HeadTiles<CW> tiles(a, n_active);
@@ -665,9 +814,10 @@ __global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
     if (pos < 0) return;
     int s, vt, db;
     tiles.at(pos, s, vt, db);
+    const auto rests = tiles.rests(s, vt);
     f32x4 acc[CW::TI][CW::TJ];
     multiply<CW, true, true>(tiles.walk(s, vt, db), lds, acc);
-    tiles.store(Lane(), acc, s, vt, db);
+    tiles.store(Lane(), rests, lds, acc, s, vt, db);
 }
 
 // Slabs added in order: of dL/dh to the tokens' own rows (blocks up to blocks_h), of dL/dW to what its tiles would have written.
@@ -804,7 +954,7 @@ Pieces pieces(int64_t T, int64_t V, int64_t d) {
 bool found_by_dz(const Pieces& p, int64_t rows) { return p.dz != kRing && rows <= kFoundTokens && p.n_v == 1; }
 
 struct Workspace {
-    size_t H, g, lse, target, row, n_active, dz, slabs, slabs_w, sum, bytes;
+    size_t H, g, lse, target, row, rest, n_active, dz, slabs, slabs_w, sum, bytes;
 };
 // Sizes that no smaller batch exceeds.
 Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
@@ -815,7 +965,7 @@ Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes); return was; };
     w.n_active = take(4);
-    w.g = take(rows * 4), w.lse = take(rows * 4), w.target = take(rows * 4), w.row = take(rows * 4);
+    w.g = take(rows * 4), w.lse = take(rows * 4), w.target = take(rows * 4), w.row = take(rows * 4), w.rest = take(rows * 4);
     w.H = take(up256(rows) * d * 2);
     w.dz = take((all < kPieceElements ? all : kPieceElements) * 2);
     w.slabs = take((one > many ? one : many) * 4);
@@ -911,7 +1061,7 @@ extern "C" int arrol_logprob_grad(const void* hidden, const void* lm_head, const
     Grad a = {};
     a.H = reinterpret_cast<uint16_t*>(base + ws.H), a.dz = reinterpret_cast<uint16_t*>(base + ws.dz);
     a.g = reinterpret_cast<float*>(base + ws.g), a.lse = reinterpret_cast<float*>(base + ws.lse);
-    a.target = reinterpret_cast<int32_t*>(base + ws.target), a.row = reinterpret_cast<int32_t*>(base + ws.row);
+    a.target = reinterpret_cast<int32_t*>(base + ws.target), a.row = reinterpret_cast<int32_t*>(base + ws.row), a.rest = reinterpret_cast<float*>(base + ws.rest);
     a.n_active = reinterpret_cast<int32_t*>(base + ws.n_active);
     a.d = d, a.stream = static_cast<int64_t>(V) * d > kCachedElements;
     const Size& size = kSize[p.products];
