@@ -482,13 +482,23 @@ struct HiddenTiles {
         const Grad& a = this->a;
         if (s == 0 && n_active <= kRestTokens) {
             const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq;
+            constexpr int kAtOnce = C::TI > 4 ? 1 : C::TJ % 2 ? C::TJ : 2;
 #pragma unroll
-            for (int j = 0; j < C::TJ; ++j) {
-                if (rests.y[j] < 0 || rests.y[j] >= a.n_v) continue;
-                const uint16_t* w = a.W + static_cast<int64_t>(rests.y[j]) * a.d + c0;
+            for (int j0 = 0; j0 < C::TJ; j0 += kAtOnce) {
+                bf16x4 w[kAtOnce][C::TI];
 #pragma unroll
-                for (int i = 0; i < C::TI; ++i)
-                    if (c0 + 16 * i < a.d) add_times(acc[i][j], rests.rest[j], *reinterpret_cast<const bf16x4*>(w + 16 * i));
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const int y = rests.y[j0 + k];
+                    const uint16_t* row = a.W + static_cast<int64_t>(y >= 0 && y < a.n_v ? y : 0) * a.d;
+#pragma unroll
+                    for (int i = 0; i < C::TI; ++i) w[k][i] = *reinterpret_cast<const bf16x4*>(row + (c0 + 16 * i < a.d ? c0 + 16 * i : 0));
+                }
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (rests.y[j0 + k] < 0 || rests.y[j0 + k] >= a.n_v) continue;
+#pragma unroll
+                    for (int i = 0; i < C::TI; ++i) add_times(acc[i][j0 + k], rests.rest[j0 + k], w[k][i]);
+                }
             }
         }
         store_rows<C>(me, acc, tb * C::BN + me.wave % C::WN * (C::BN / C::WN), n_active, db * C::BM + me.wave / C::WN * (C::BM / C::WM), a.d, a.slabs + s * a.slab_stride, a.add,
@@ -637,13 +647,17 @@ struct ResidentTiles {
             for (uint64_t tokens = __ballot(target[k] >= first && target[k] < first + 32); tokens; tokens &= tokens - 1) {
                 const int at = __builtin_ctzll(tokens), row = __builtin_amdgcn_readlane(target[k], at) - first;
                 const float rest = a.rest[k * 64 + at];
-                const uint16_t* h = a.H + static_cast<int64_t>(k * 64 + at) * a.d + c0 + 4 * me.lq;
+                bf16x4 h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = c0 + 4 * me.lq + 16 * i;
+                    h[i] = *reinterpret_cast<const bf16x4*>(a.H + static_cast<int64_t>(k * 64 + at) * a.d + (c < a.d ? c : 0));
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     if (row >> 4 != j || (row & 15) != me.l15) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (c0 + 4 * me.lq + 16 * i < a.d) add_times(acc[i][j], rest, *reinterpret_cast<const bf16x4*>(h + 16 * i));
+                    for (int i = 0; i < 4; ++i) add_times(acc[i][j], rest, h[i]);
                 }
             }
         mid_nt::wait_vmcnt<0>();        // or the compiler would wait for loads of this branch, and so for the stores, wherever it is left
