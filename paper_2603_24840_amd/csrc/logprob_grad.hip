@@ -8,7 +8,7 @@
 //   gather     tokens that take part (g_t != 0 and a target inside the vocabulary) are counted and their hidden states put next to each other; the others' gradients are
 //              zeros.  Whatever such a token's hidden state holds takes no part, and no product is spent on it
 //   per piece of the vocabulary:
-//   dz         256 x 256 tiles of W h, dz in the epilogue, stored token-major through the LDS in whole lines
+//   dz         tiles of W h, dz in the epilogue, stored token-major; what rounding it took at the tokens' targets is kept for few tokens' products
 //   products   tiles of dL/dh (dz as it lies, W read in place down its rows) and of dL/dW (dz and the hidden states both read down their rows), in one launch, so that
 //              the long walks of the first and the many short ones of the second fill the chip together.  Up to kResidentTokens tokens of a large vocabulary dL/dW keeps the hidden
 //              states in registers instead
@@ -20,10 +20,10 @@
 // where torch's 16,384 x 16,384 x 8,192 product reaches 1.29 and its products of these three shapes 1.18, 0.59 and 0.98; 6,278 x 151,936 x 4096 18.0 to 18.7 ms, 1.21 to 1.26.
 // Of the dz launches 13 % is the epilogue (2,253 us, 1,961 without, 2,145 without its stores, 2,229 without exponentials).  Few tokens: reading W twice and writing its
 // gradient, 16 x 151,936 x 2048 397 us (1.87 GB: 4.7 TB/s).  Between them, 311 x 151,936 x 2048 711 us: the LDS, into which tiles of 128 x 160 bring 36 KB and out of which they read
-// 72 KB a step of 640 cycles of products (matrix cores busy 38 % in dz and dL/dh).  Small calls: three or four launches of 3 to 8 us.
+// 72 KB a step of 640 cycles of products (matrix cores busy 38 % in dz and dL/dh).  Small calls: three launches of 2 to 8 us.
 // Not kept: in 128 x 160 tiles the next but one step's loads before the products, with a second barrier (even), the last step peeled off (dz 258 to 363: registers), tiles of 128 x 320 and
-// 256 x 320 for dz (even, and 8 % faster at 151,936 but 37 % slower at 32,000); 256 workgroups that walk over tiles, the next tile's loads under way during an epilogue (dz 1.4 % faster, products 3.5 % slower); the K-major offsets of the ring
-// formed ahead (products 4.5 % slower); dL/dh with the operands' roles exchanged, bands of 4, pieces of 2^27 to 2^30 values (even).
+// 256 x 320 for dz (even, and 8 % faster at 151,936 but 37 % slower at 32,000); 256 workgroups that walk over tiles, the next tile's loads under way during an epilogue (dz 1.4 % faster,
+// products 3.5 % slower); the K-major offsets of the ring formed ahead (products 4.5 % slower); dL/dh with the operands' roles exchanged, bands of 4, pieces of 2^27 to 2^30 values (even).
 #include "common.h"
 #include "mid_nt.h"
 #include "ring_nt.h"
@@ -879,7 +879,7 @@ int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 // Which forms a piece takes, of dz and of the products: those whose estimated times are the smallest.  Measured, microseconds: what a tile costs beside its K64
 // steps, a step where the chip is full (of every one of the `per_unit` workgroups that a compute unit has at a time) and a step where it is not.  1,024 x 32,000 x 2048:
 // dz 111 / 154 / 148 / 197 / 220, products 245 / 249 / 246 / 293 / 446; 640 tokens of it: 103 / 91 / 107 / 122 / 137 and 175 / 158 / 166 / 193 / 276; 318 x 4,096 x 256:
-// 14.9 / 11.4 / 9.7 / 7.9 / 7.4 and 19.4 / 10.0 / 9.3 / 9.2 / 6.8; 16 x 151,936 x 2048 (LM head from memory, and its gradient to it): 249 / 150 / 221 / 133 / 135 of dz.
+// 14.9 / 11.4 / 9.7 / 7.9 / 7.4 and 19.4 / 10.0 / 9.3 / 9.2 / 6.8; 16 x 151,936 x 2048 (LM head from memory, and its gradient to it): dz in 128 x 160 150, 128 x 64 132, 64 x 64 135.
 enum Form { kRing, kMid160, kMid128, kMidFew, kMid64, kForms };
 struct Size {
     int bm, bn, bm_w, bn_w;         // of dz and dL/dh, and of dL/dW
