@@ -495,7 +495,7 @@ struct HiddenTiles {
                 }
 #pragma unroll
                 for (int k = 0; k < kAtOnce; ++k) {
-                    if (rests.y[j0 + k] < 0 || rests.y[j0 + k] >= a.n_v) continue;
+                    if (rests.y[j0 + k] < 0 || rests.y[j0 + k] >= a.n_v || rests.rest[j0 + k] == 0.f) continue;      // 0 times infinity
 #pragma unroll
                     for (int i = 0; i < C::TI; ++i) add_times(acc[i][j0 + k], rests.rest[j0 + k], w[k][i]);
                 }
@@ -594,7 +594,7 @@ struct HeadTiles {
                 const int r = __builtin_amdgcn_readfirstlane(row[k]) - a.v0 - first;
 #pragma unroll
                 for (int j = 0; j < C::TJ; ++j) {
-                    if (r >> 4 != j || (r & 15) != me.l15) continue;
+                    if (r >> 4 != j || (r & 15) != me.l15 || rest[k] == 0.f) continue;
 #pragma unroll
                     for (int i = 0; i < C::TI; ++i) add_times(acc[i][j], rest[k], h[k][i]);
                 }
@@ -655,7 +655,7 @@ struct ResidentTiles {
                 }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    if (row >> 4 != j || (row & 15) != me.l15) continue;
+                    if (row >> 4 != j || (row & 15) != me.l15 || rest == 0.f) continue;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) add_times(acc[i][j], rest, h[i]);
                 }

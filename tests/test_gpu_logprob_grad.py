@@ -285,10 +285,11 @@ def test_against_differences(A, of):
             assert float(want) > 4 * float(tol)         # moved along the gradient, L rises by far more than that
 
 
-def test_on_a_stream_and_in_graphs(A):
+@pytest.mark.parametrize("T,V,d", [(300, 700, 128), (100, 60001, 264)])
+def test_on_a_stream_and_in_graphs(A, T, V, d):
     """Two graphs that share a workspace, replayed in turn with eager calls between them, on data that changes."""
-    print("[case] logprob_grad in graphs", flush=True)
-    data = [make(300, 700, 128, seed=s) for s in range(4)]
+    print("[case] logprob_grad in graphs T=%d V=%d d=%d" % (T, V, d), flush=True)
+    data = [make(T, V, d, seed=s) for s in range(4)]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     got = A.arrol_logprob_grad(*data[0], stream=side)
@@ -296,8 +297,8 @@ def test_on_a_stream_and_in_graphs(A):
     want = [A.arrol_logprob_grad(*x) for x in data]
     assert all(torch.equal(got[x], want[0][x]) for x in got)
     buffers = [x.clone() for x in data[0]]
-    ws = torch.empty(A.lib().arrol_logprob_grad_workspace_bytes(300, 700, 128, 1), dtype=torch.uint8, device=DEV)
-    total = torch.zeros(700, 128, device=DEV)
+    ws = torch.empty(A.lib().arrol_logprob_grad_workspace_bytes(T, V, d, 1), dtype=torch.uint8, device=DEV)
+    total = torch.zeros(V, d, device=DEV)
     graphs = []
     for kw in (dict(), dict(lm_head_sum=total)):
         graph = torch.cuda.CUDAGraph()
