@@ -18,7 +18,8 @@ namespace {
 constexpr int kWaves = 4;                 // of a workgroup
 // Units of a lane in flight, and wavefronts that a launch is cut into where tokens are fewer.  11,136 tokens, 32 + 8 heads of 128, from and to memory: 2 and 65,536 45.3 us
 // (5.0 TB/s), 4 and 8,192 46.8, loads through the caches 50.4; stores past the caches too: 41.2, but the attention behind it 8 longer.  Into the pool, where every wavefront looks
-// for its token's page: 6,426 tokens of 24 + 8 heads of 80, 3 and 8,192 23.8 us, 2 and 65,536 28.3, 4 and 65,536 35.6.
+// for its token's page: 6,426 tokens of 24 + 8 heads of 80, 3 and 8,192 23.8 us, 2 and 65,536 28.3, 4 and 65,536 35.6; accesses of 16 bytes at
+// multiples of 8 where the second half begins there, with a short last unit, 29.5.
 template <bool POOL> constexpr int kUnits = POOL ? 3 : 2;
 template <bool POOL> constexpr int kWavefronts = POOL ? 8192 : 65536;
 constexpr int kMaxHalf = 128;
