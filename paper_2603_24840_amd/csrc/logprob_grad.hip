@@ -431,7 +431,7 @@ __device__ __forceinline__ void add_times(f32x4& x, float f, bf16x4 four) {
 
 // dz is largest at a token's target by far, so of few tokens a gradient is as far off as that one rounding, 2^-8 at most, beside its own, and does not average out.  What dz lost there is
 // added in fp32: to dL/dh_t one row of W, up to kRestTokens tokens, to dL/dW a hidden state for every token whose target the row is, up to kResidentTokens.  The resident form of dL/dW has it
-// for nothing; its tiles need a barrier and a look at the tokens each (500 x 18,920 x 3128: products 132 us, with it 152; 64 x 4,096 x 1024 9.2 and 10.1).  What an
+// for nothing; tiles have to fetch their tokens' one after the other (up to 512 tokens: products of 500 x 18,920 x 3128 152 us, without it 133; of 510 x 391 x 128 19.8 and 6.1).  What an
 // epilogue needs is asked for before its walk.
 constexpr int kRestTokens = 1024, kResidentSteps = 5, kResidentTokens = kResidentSteps * 64;
 
@@ -533,35 +533,30 @@ struct HeadTiles {
         w.b_k_rows = w.n_k64 * 64;                       // rows of zeros behind n_active
         return w;
     }
-    // The rows of the tile that are targets, of token threadIdx.x and every NT-th from it on, for the first part.
-    static constexpr int kRounds = (kResidentTokens + C::NT - 1) / C::NT;
+    // The wavefront's rows that are targets, of token lane and every 64th from it on, for the first part.
     struct Rests {
-        int row[kRounds];
+        int row[kResidentTokens / ARROL_WAVE];
     };
-    __device__ __forceinline__ Rests rests(int s, int vt) const {
+    __device__ __forceinline__ int first_row(const Lane& me, int vt) const { return vt * C::BN + me.wave % C::WN * (C::BN / C::WN); }
+    __device__ __forceinline__ Rests rests(const Lane& me, int s, int vt) const {
         Rests r;
 #pragma unroll
-        for (int u = 0; u < kRounds; ++u) {
-            const int t = u * C::NT + threadIdx.x;
-            r.row[u] = s == 0 && n_active <= kResidentTokens && t < n_active ? a.target[t] - a.v0 - vt * C::BN : -1;
+        for (int u = 0; u < kResidentTokens / ARROL_WAVE; ++u) {
+            const int t = u * ARROL_WAVE + me.lane;
+            r.row[u] = s == 0 && n_active <= kResidentTokens && t < n_active ? a.target[t] - a.v0 - first_row(me, vt) : -1;
         }
         return r;
     }
-    // Their rests times the hidden states, token by token.  Every wavefront column has its own.
-    __device__ __forceinline__ void add_rests(const Lane& me, const Rests& rests, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int vt, int db) const {
-        constexpr int kAtOnce = C::TI > 4 ? 2 : 4, kRows = C::BN / C::WN, kMasks = kRounds * C::NW;
-        uint64_t* masks = reinterpret_cast<uint64_t*>(lds);         // [WN][kMasks], a bit for every token
-        __syncthreads();                    // all have read the last step
+    // Their rests times the hidden states, token by token.
+    __device__ __forceinline__ void add_rests(const Lane& me, const Rests& rests, f32x4 (&acc)[C::TI][C::TJ], int vt, int db) const {
+        constexpr int kAtOnce = C::TI > 4 ? 2 : 4, kRows = C::BN / C::WN;
+        uint64_t mine = 0;                  // of 64 tokens, lane by lane
 #pragma unroll
-        for (int u = 0; u < kRounds; ++u)
-#pragma unroll
-            for (int w = 0; w < C::WN; ++w) {
-                const uint64_t mask = __ballot(rests.row[u] >= w * kRows && rests.row[u] < (w + 1) * kRows);
-                if (me.lane == 0) masks[w * kMasks + u * C::NW + me.wave] = mask;
-            }
-        __syncthreads();
-        const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq, first = vt * C::BN + me.wave % C::WN * kRows;
-        const uint64_t mine = me.lane < kMasks ? masks[me.wave % C::WN * kMasks + me.lane] : 0;
+        for (int u = 0; u < kResidentTokens / ARROL_WAVE; ++u) {
+            const uint64_t mask = __ballot(rests.row[u] >= 0 && rests.row[u] < kRows);
+            mine = me.lane == u ? mask : mine;
+        }
+        const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq, first = first_row(me, vt);
         uint64_t some = __ballot(mine != 0), tokens = 0;
         int at = 0;
         for (;;) {
@@ -601,8 +596,8 @@ struct HeadTiles {
             }
         }
     }
-    __device__ __forceinline__ void store(const Lane& me, const Rests& rests, unsigned char* lds, f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
-        if (s == 0 && n_active <= kResidentTokens) add_rests(me, rests, lds, acc, vt, db);
+    __device__ __forceinline__ void store(const Lane& me, const Rests& rests, f32x4 (&acc)[C::TI][C::TJ], int s, int vt, int db) const {
+        if (s == 0 && n_active <= kResidentTokens) add_rests(me, rests, acc, vt, db);
         const int r0 = vt * C::BN + me.wave % C::WN * (C::BN / C::WN), c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM);
         const bool parts = a.slabs_w != nullptr;
         const auto same = [](int r) { return r; };
@@ -828,10 +823,10 @@ __global__ __launch_bounds__(CH::NT) void products_kernel(Grad a) {
     if (pos < 0) return;
     int s, vt, db;
     tiles.at(pos, s, vt, db);
-    const auto rests = tiles.rests(s, vt);
+    const auto rests = tiles.rests(Lane(), s, vt);
     f32x4 acc[CW::TI][CW::TJ];
     multiply<CW, true, true>(tiles.walk(s, vt, db), lds, acc);
-    tiles.store(Lane(), rests, lds, acc, s, vt, db);
+    tiles.store(Lane(), rests, acc, s, vt, db);
 }
 
 // Slabs added in order: of dL/dh to the tokens' own rows (blocks up to blocks_h), of dL/dW to what its tiles would have written.
