@@ -37,9 +37,6 @@ using ring_nt::f32x4;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kXcds = 8, kRound = 256;
-// An LM head of more elements than these is more than the 256 MiB cache holds, and so is its gradient: that goes past the caches, where its lines would have to be written back
-// while the next call reads (16 x 151,936 x 2048, calls one after the other: dz 191 us, so 132; the call 532 and 491.  128 tokens: 608 and 551).
-constexpr int64_t kCachedElements = int64_t{1} << 27;
 
 // The forms that the contractions come in.  BM: of the dimension that lies contiguous in the result (vocabulary of dz, columns of the gradients), BN: of its rows.
 typedef ring_nt::RingTile<256, 256, 2, 4> Ring;
@@ -600,7 +597,7 @@ struct HeadTiles {
         const int r0 = vt * C::BN + me.wave % C::WN * (C::BN / C::WN), c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM);
         const bool parts = a.slabs_w != nullptr;
         const auto same = [](int r) { return r; };
-        if (a.stream && !a.write_sum) store_rows<C, true>(me, acc, r0, a.n_v, c0, a.d, a.sum, a.read_sum, false, a.grad_w, same);      // of such a size there are no parts
+        if (a.stream && !a.write_sum) store_rows<C, true>(me, acc, r0, a.n_v, c0, a.d, a.sum, a.read_sum, false, a.grad_w, same);      // of such a size there are no parts: part_floats()
         else store_rows<C>(me, acc, r0, a.n_v, c0, a.d, parts ? a.slabs_w + s * a.slab_w_stride : a.sum, !parts && a.read_sum, parts || a.write_sum, a.grad_w, same);
     }
 };

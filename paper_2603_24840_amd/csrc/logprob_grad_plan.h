@@ -9,6 +9,9 @@ namespace logprob_grad {
 constexpr int64_t kPieceRows = 16384;              // tokens of a piece
 constexpr int64_t kPieceElements = int64_t{1} << 28;     // of dz
 constexpr int kFoundTokens = 1024;                 // of a piece, that the workgroups of the first product look through by themselves
+// An LM head of more elements than these is more than the 256 MiB cache holds, and so is its gradient: that goes past the caches, where its lines would have to be written back
+// while the next call reads (16 x 151,936 x 2048, calls one after the other: dz 191 us, so 132; the call 532 and 491.  128 tokens: 608 and 551).
+constexpr int64_t kCachedElements = int64_t{1} << 27;
 constexpr int kResidentSteps = 5, kResidentTokens = kResidentSteps * 64;
 
 inline size_t up(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -29,6 +32,7 @@ constexpr Size kSize[kForms] = {{256, 256, 256, 256, 1, 8.7, 1.45, 1.1, 10.0, 1.
 
 constexpr int kMaxSlabs = 32, kSlabTiles = 512;     // of 256 x 256
 constexpr int64_t kSlabFloats = kSlabTiles * int64_t{65536};
+static_assert(kSlabFloats / 2 <= kCachedElements, "a gradient that goes past the caches has no parts");
 // From so many blocks of 64 x 256 on, seven to a compute unit, the hidden states' way into the registers is worth it.  The launch of the products, resident and in tiles: 311 x 151,936 x 2048
 // (19,000 blocks) 457 us and 600, 16 tokens 260 and 335, 110 x 79,125 x 3264 228 and 272, 300 x 32,000 x 1024 (2,000) 54 and 61; 250 x 20,000 x 1000 (1,252) 38.4 and 34.8, 320 x 16,384 x 512
 // (512) 22.7 and 19.8.
@@ -61,10 +65,17 @@ inline double products_time(const Size& f, int64_t rows, int64_t v, int64_t d, i
     const double all = (n_h * (f.tile + k_h * f.step) + n_w * each_w) / places;
     return n_h + n_w <= places ? (all > longest ? all : longest) : all + longest / 2;
 }
-inline void choose_forms(Pieces& p, int64_t d) {
+// fp32 values kept for the sums of dL/dW's parts: parts are taken only where there are some, so where two whole gradients fit, whatever the pieces and the estimates.
+inline int64_t part_floats(int64_t T, int64_t V, int64_t d) {
+    const int64_t head = up256(V) * d;
+    if (T <= 256 || 2 * head > kSlabFloats) return 0;
+    return kMaxSlabs * head < kSlabFloats ? kMaxSlabs * head : kSlabFloats;
+}
+inline void choose_forms(Pieces& p, int64_t T, int64_t V, int64_t d, const Size* sizes) {
     double best_dz = 1e30, best = 1e30;
+    const int64_t floats = part_floats(T, V, d);
     for (int f = 0; f < kForms; ++f) {
-        const Size& size = kSize[f];
+        const Size& size = sizes[f];
         const double dz = f == kRing && d % 64 ? 1e30 : dz_time(size, p.rows, p.v, d);
         if (dz < best_dz) best_dz = dz, p.dz = static_cast<Form>(f);
         // parts of dL/dW's K extent where that is long and its tiles are few: as many as fill the chip, of 8 steps at least
@@ -72,7 +83,7 @@ inline void choose_forms(Pieces& p, int64_t d) {
         int64_t parts = f != kRing && k_w >= 32 && tiles_w < 256 ? 512 / tiles_w : 1;
         parts = parts < k_w / 8 ? parts : k_w / 8;
         parts = parts < kMaxSlabs ? parts : kMaxSlabs;
-        if (parts * p.v * d > kSlabFloats) parts = kSlabFloats / (p.v * d);
+        if (parts * p.v * d > floats) parts = floats / (p.v * d);
         const int64_t tile = static_cast<int64_t>(size.bm) * size.bn, tiles = tiles_of(p.rows, d, size.bn, size.bm), k64 = p.v / 64;
         const bool resident = f != kRing && p.rows <= kResidentTokens && tiles_of(p.v, d, 64, 256) >= kResidentBlocks;
         for (int with = 0; with < 5; ++with) {          // 0: one part, 1: those parts, 2 ..: resident hidden states and 4, 8 or 16 blocks
@@ -88,7 +99,7 @@ inline void choose_forms(Pieces& p, int64_t d) {
         }
     }
 }
-inline Pieces pieces(int64_t T, int64_t V, int64_t d) {
+inline Pieces pieces(int64_t T, int64_t V, int64_t d, const Size* sizes = kSize) {
     Pieces p;
     p.n_rows = (T + kPieceRows - 1) / kPieceRows;
     p.rows = (T + p.n_rows - 1) / p.n_rows;
@@ -96,7 +107,7 @@ inline Pieces pieces(int64_t T, int64_t V, int64_t d) {
     p.n_v = (all + most - 1) / most;
     p.v = up256((all + p.n_v - 1) / p.n_v);
     p.n_v = (all + p.v - 1) / p.v;
-    choose_forms(p, d);
+    choose_forms(p, T, V, d, sizes);
     const int64_t k64 = ((V < p.v ? V : p.v) + 63) / 64;      // of the first piece, no part of which may be empty
     p.k64_per_slab = static_cast<int>((k64 + p.slabs - 1) / p.slabs);
     p.slabs = static_cast<int>((k64 + p.k64_per_slab - 1) / p.k64_per_slab);
@@ -113,7 +124,6 @@ inline Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     Workspace w;
     const int64_t rows = T < kPieceRows ? T : kPieceRows, all = up256(rows) * up256(V);
     const int64_t one = rows * d, many = kMaxSlabs * one < kSlabFloats ? kMaxSlabs * one : kSlabFloats;      // one slab, or kSlabTiles tiles at most
-    const int64_t head = up256(V) * d;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes); return was; };
     w.n_active = take(4);
@@ -121,7 +131,7 @@ inline Workspace workspace(int64_t T, int64_t V, int64_t d, bool lm_head) {
     w.H = take(up256(rows) * d * 2);
     w.dz = take((all < kPieceElements ? all : kPieceElements) * 2);
     w.slabs = take((one > many ? one : many) * 4);
-    w.slabs_w = take(T > 256 && 2 * head <= kSlabFloats ? (kMaxSlabs * head < kSlabFloats ? kMaxSlabs * head : kSlabFloats) * 4 : 0);
+    w.slabs_w = take(part_floats(T, V, d) * 4);
     w.sum = take(lm_head && T > kPieceRows ? V * d * 4 : 0);
     w.bytes = at;
     return w;
