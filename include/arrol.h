@@ -620,8 +620,9 @@ int arrol_rotary_frequencies(int32_t rotary_dim, double base, double factor, dou
  *   k' goes besides (the attention over packed rows reads it there).  inv_freq NULL: nothing is turned, and rotary_dim and position have no meaning.
  * start int32 [n_seq]; position int32 [T]; block_table int32 [n_seq, max_pages_per_seq].
  * Nothing else of the pool is touched, and the pool overlaps none of the other arrays.  A token whose slot is negative or past its table's row, or on a page id
- * outside [0, n_pages), is not written; of two tokens with one slot each head's key and value may be either's.  A row of no sequence is not written to the pool, and
- * its q_out and k_out rows are its q and k as they are.
+ * outside [0, n_pages), is not written.  Tokens of one call need slots of their own: where two have the same, each element of the key and the value there may be
+ * either's, so that a head may hold a mixture of both; the rest of the pool is as it would be.  A row of no sequence is not written to the pool, and its q_out and
+ * k_out rows are its q and k as they are.
  * Sizes as in arrol_rotary; n_pages * page_tokens below 2^31.  T == 0 is a no-op.
  */
 int arrol_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,

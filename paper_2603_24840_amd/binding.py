@@ -990,7 +990,7 @@ def arrol_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, p
     """New tokens into one layer of the paged pool (kv is modified in place): k, v bf16 [T, n_kv_heads, head_dim] (rows may be strided), block_table int32 [n, pages],
     start int32 [n] the slot of every row's first new token.  One token a row, or with cu_seqlens int64 [n+1] packed sequences.  With inv_freq fp64 [rotary_dim/2] keys and
     queries q bf16 [T, n_heads, head_dim] (None: none) are turned as by arrol_rotary, by position int32 [T] (None: the slots).  want_k: the turned keys
-    as packed rows too.  out_q and out_k (None: new) may be q and k.  -> dict(q, k), None where there is none."""
+    as packed rows too.  out_q and out_k (None: new) may be q and k.  Of tokens with one slot the pool may hold a mixture.  -> dict(q, k), None where there is none."""
     if stream is None:
         result = (_marshal or _load_marshal()).append(k, v, kv, layer, block_table, start, cu_seqlens, q, position, inv_freq, interleaved, magnitude, want_k, out_q, out_k)
         if result is not None:

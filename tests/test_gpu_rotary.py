@@ -254,6 +254,30 @@ def test_append_stays_in_bounds_for_any_offsets(A, cu):
     assert not bool(touched[1].any()) and not bool(touched[:, :, [0, 3, 6, 9, 10, 11]].any()) and bool(torch.isfinite(got["q"].float()).all())
 
 
+@pytest.mark.parametrize("KV,hd,rot,same", [(1, 8, 2, 3), (2, 64, 64, 40), (5, 80, 40, 2), (8, 128, 128, 17), (3, 40, 36, 2)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_of_tokens_with_one_slot(A, KV, hd, rot, same, interleaved):
+    """Every element of the slot is one of its tokens', and nothing else of the pool is touched."""
+    print("[case] append, %d tokens a slot, heads=%d hd=%d rot=%d interleaved=%d" % (same, KV, hd, rot, interleaved), flush=True)
+    n, f = 6, frequencies(A, rot)
+    x = rand(n * same, 1 + 2 * KV, hd, seed=hd)
+    k, v = x[:, 1:1 + KV], x[:, 1 + KV:]
+    table, start = torch.tensor([[4], [1], [7], [2], [0], [6]], dtype=torch.int32, device=DEV), torch.tensor([3, 15, 0, 8, 9, 1], dtype=torch.int32, device=DEV)
+    position = torch.arange(n * same, dtype=torch.int32, device=DEV) * 11
+    before = rand(1, 2, 9, 16, KV, hd, seed=4)
+    turned = A.arrol_rotary(k, None, position, f, interleaved=interleaved)[0]
+    for packed in (False, True):        # a token a row of the table, row s + n i being row s again, or sequences of one token
+        kv = before.clone()
+        cu = torch.arange(n * same + 1, dtype=torch.int64, device=DEV) if packed else None
+        got = A.arrol_append(k, v, kv, 0, table.repeat(same, 1), start.repeat(same), cu, q=x[:, :1], position=position, inv_freq=f, interleaved=interleaved, want_k=True)
+        assert torch.equal(got["k"], turned) and torch.equal(got["q"], A.arrol_rotary(x[:, :1], None, position, f, interleaved=interleaved)[0])
+        for rows, of in ((turned, 0), (v, 1)):
+            there = kv[0, of, table[:, 0].long(), start.long()]
+            assert bool((there == rows.view(same, n, KV, hd)).any(0).all())
+        kv[0, :, table[:, 0].long(), start.long()] = before[0, :, table[:, 0].long(), start.long()]
+        assert torch.equal(kv, before)
+
+
 def test_append_in_place_and_without_queries(A):
     print("[case] append in place", flush=True)
     x, f = rand(50, 8, 64), frequencies(A, 64)
