@@ -66,3 +66,20 @@ def test_kernel_query(A):
         rows, tokens, columns, product_tokens, slabs, parts, pieces, found = (x.value for x in out)
         assert rows in (64, 128, 256) and columns in (64, 128, 256) and tokens in (64, 128, 256) and product_tokens in (64, 128, 256)
         assert (rows != 256 or d % 64 == 0) and 1 <= slabs <= 32 and 1 <= parts <= 32 and pieces >= 1 and (not found or (T <= 1024 and rows < 256))
+
+
+def test_kernel_query_has_what_the_header_says(A):
+    """Every number of tiles and parts that the header names, and no other, over sizes that meet them all."""
+    out = [ctypes.c_int32() for _ in range(8)]
+    seen = [set() for _ in out]
+    for T, V, d in ((1, 1, 8), (16384, 151936, 4096), (10 ** 9, 2 ** 24, 16384), (40000, 300, 64), (1024, 5000, 1000), (311, 151936, 2048), (60, 60001, 264), (297, 878561, 72), (72, 79901, 264),
+                    (640, 32000, 2048), (2579, 3172, 1728), (330, 140001, 968), (346, 4096, 256), (2, 1268440, 144), (332, 515, 2848), (943, 2368, 2360)):
+        assert A.lib().arrol_logprob_grad_kernels(T, V, d, *[ctypes.byref(x) for x in out]) == 0
+        rows, tokens, columns, product_tokens, slabs, parts, pieces, found = values = [x.value for x in out]
+        tiles = {(256, 256), (128, 160), (128, 128), (128, 64), (64, 64)}
+        assert (rows, tokens) in tiles and (columns, product_tokens) in tiles and (rows != 256 or d % 64 == 0)
+        assert 1 <= slabs <= 32 and 0 <= parts <= 32 and (parts > 0 or (T <= 320 and columns < 256)) and pieces >= 1 and (not found or (T <= 1024 and rows < 256))
+        for have, x in zip(seen, values):
+            have.add(x)
+    assert seen[1] == seen[3] == {64, 128, 160, 256} and seen[0] == seen[2] == {64, 128, 256} and seen[7] == {0, 1}
+    assert max(seen[4]) > 1 and {0, 1} < seen[5] and max(seen[6]) > 1
