@@ -136,6 +136,27 @@ def test_few_tokens_are_off_by_the_result_s_rounding_alone(A, T, V, d, target):
         assert float((got[name].double() - want).norm()) <= bound, (name, float((got[name].double() - want).norm()) / float(want.norm()), bound / float(want.norm()))
 
 
+FEW = [(724, 17984, 384), (900, 69999, 1984), (330, 140001, 968), (843, 556, 1928), (332, 515, 2848), (934, 27627, 72), (330, 1200001, 120), (771, 270492, 80),           # dL/dh
+       (194, 3396, 2816), (202, 3517, 1856), (137, 1113, 2728), (258, 5487, 1064), (72, 79901, 264), (1, 317915, 104), (40, 103018, 296),                                           # both
+       (300, 600001, 264), (90, 1134480, 72), (297, 878561, 72), (8, 1065945, 16), (2, 1268440, 144)]                                                            # pieces of the vocabulary
+
+
+@pytest.mark.parametrize("target", ["any", "one", "near"])
+@pytest.mark.parametrize("T,V,d", FEW)
+def test_few_tokens_in_the_other_forms(A, T, V, d, target):
+    test_few_tokens_are_off_by_the_result_s_rounding_alone(A, T, V, d, target)
+
+
+def test_every_form_has_few_tokens(A):
+    """What the roundings at the targets are added in: dL/dh up to 1,024 tokens, dL/dW up to 320 in tiles of the same, of 128 x 128 for the middle ones, or resident."""
+    got = [(T, kernels(A, T, V, d)) for T, V, d in FEW]
+    tiles = {(256, 256), (128, 160), (128, 128), (128, 64), (64, 64)}
+    form = lambda k: (k["product_columns"], k["product_tokens"])
+    assert {form(k) for _, k in got} == tiles and {k["slabs"] > 1 for _, k in got} == {False, True} and all(T <= 1024 for T, _ in got)
+    assert {form(k) for T, k in got if T <= 320 and k["parts"] == 1} == tiles and {form(k) for T, k in got if k["parts"] == 0} == tiles - {(256, 256)}
+    assert {(T <= 320, k["parts"] == 0) for T, k in got if k["pieces"] > 1} == {(False, False), (True, False), (True, True)}
+
+
 @pytest.mark.parametrize("T,V,d", [(320, 60001, 264), (65, 30016, 1000)])
 def test_few_tokens_of_a_large_vocabulary(A, T, V, d):
     """The hidden states of all tokens in registers: as many tokens as fit, as few as none, a workspace of NaN, NaN of one that takes part."""
