@@ -235,7 +235,7 @@ int arrol_logprob_streamed(int64_t T, int32_t V, int32_t d, int32_t n_splits, in
  * grad_logp = dL/dlogprob fp32 [T] (arrol_grpo_objective's grad_logp, for instance; its sign is the caller's):
  *   dz_tv = grad_logp_t ([v = y_t] - exp(z_tv - lse_t)),  dL/dh_t = sum_v dz_tv W_v,  dL/dW_v = sum_t dz_tv h_t
  * The logits are formed again in pieces of the vocabulary and the tokens; of a piece only dz is kept, in bf16 (rounded by up to 2^-8 each); products accumulate in fp32.
- * What that rounding took at the tokens' targets is added back in fp32 where few tokens of a piece take part: up to 1,024 in grad_hidden, up to 320 in the LM head's gradient.
+ * What that rounding took at the tokens' targets is added back in fp32: in grad_hidden always, in the LM head's gradient where up to 320 tokens of a piece take part.
  * A token whose grad_logp is 0, or whose target lies outside [0, V), takes no part, whatever its hidden state, lse and grad_logp hold (NaN and infinities, too): its
  * grad_hidden is 0.  No products are spent on such tokens.
  * hidden, lm_head, targets as in arrol_logprob; d at most 16384, V at most 2^24, T below 2^40.

@@ -8,7 +8,7 @@
 //   gather     tokens that take part (g_t != 0 and a target inside the vocabulary) are counted and their hidden states put next to each other; the others' gradients are
 //              zeros.  Whatever such a token's hidden state holds takes no part, and no product is spent on it
 //   per piece of the vocabulary:
-//   dz         tiles of W h, dz in the epilogue, stored token-major; what rounding it took at the tokens' targets is kept for few tokens' products
+//   dz         tiles of W h, dz in the epilogue, stored token-major; what rounding it took at the tokens' targets is kept for the products
 //   products   tiles of dL/dh (dz as it lies, W read in place down its rows) and of dL/dW (dz and the hidden states both read down their rows), in one launch, so that
 //              the long walks of the first and the many short ones of the second fill the chip together.  Up to kResidentTokens tokens of a large vocabulary dL/dW keeps the hidden
 //              states in registers instead
@@ -425,11 +425,12 @@ __device__ __forceinline__ void add_times(f32x4& x, float f, bf16x4 four) {
     for (int v = 0; v < 4; ++v) x[v] = fmaf(f, y[v], x[v]);
 }
 
-// dz is largest at a token's target by far, so of few tokens a gradient is as far off as that one rounding, 2^-8 at most, beside its own, and does not average out.  What dz lost there is
-// added in fp32: to dL/dh_t one row of W, up to kRestTokens tokens, to dL/dW a hidden state for every token whose target the row is, up to kResidentTokens.  The resident form of dL/dW has it
-// for nothing; tiles have to fetch their tokens' one after the other (up to 512 tokens: products of 500 x 18,920 x 3128 152 us, without it 133; of 510 x 391 x 128 19.8 and 6.1).  What an
-// epilogue needs is asked for before its walk.
-constexpr int kRestTokens = 1024;
+// dz is largest at a token's target by far, and that one rounding, 2^-8 at most, counts beside a result's own: in dL/dh_t, where no other token averages it out, and in the row of dL/dW
+// that it is the target of, unless many tokens share it.  What dz lost there is added in fp32.  To dL/dh_t it is one row of W, a token's for itself: 5,130 x 128,256 x 2048 6,905 us and
+// without 6,965, 8,777 x 4,096 x 1024 317 and 315, at worst 4,000 x 300 x 1088 39.8 and 37.8.  To dL/dW it is a hidden state for every token whose target a row is.  The resident form has
+// that for nothing; tiles have to find their tokens and fetch them one after the other, so there it is up to kResidentTokens, where the forms meet, and beyond a gradient is 2.4e-3 off
+// in norm instead of 1.7e-3 (up to 1,024 tokens: 640 x 32,000 x 2048 292 us and without 267, 500 x 18,920 x 3128 275 and 256, 510 x 391 x 128 25.9 and 13.2).  What an epilogue
+// needs is asked for before its walk.
 
 // dL/dh: columns of W, which is read down its rows, times tokens' rows of dz; K = the vocabulary piece or a part of it.  Tile (s, at, db): part, tokens, columns.
 template <class C>
@@ -468,7 +469,7 @@ struct HiddenTiles {
 #pragma unroll
         for (int j = 0; j < C::TJ; ++j) {
             const int t = t_first + 16 * j;
-            const bool on = s == 0 && n_active <= kRestTokens && t < n_active;
+            const bool on = s == 0 && t < n_active;
             r.y[j] = on ? a.target[t] - a.v0 : -1;
             r.rest[j] = on ? a.rest[t] : 0.f;
         }
@@ -476,7 +477,7 @@ struct HiddenTiles {
     }
     __device__ __forceinline__ void store(const Lane& me, const Rests& rests, f32x4 (&acc)[C::TI][C::TJ], int s, int tb, int db) const {
         const Grad& a = this->a;
-        if (s == 0 && n_active <= kRestTokens) {
+        if (s == 0) {
             const int c0 = db * C::BM + me.wave / C::WN * (C::BM / C::WM) + 4 * me.lq;
             constexpr int kAtOnce = C::TI > 4 ? 1 : C::TJ % 2 ? C::TJ : 2;
 #pragma unroll

@@ -157,6 +157,13 @@ def test_every_form_has_few_tokens(A):
     assert {(T <= 320, k["parts"] == 0) for T, k in got if k["pieces"] > 1} == {(False, False), (True, False), (True, True)}
 
 
+@pytest.mark.parametrize("target", ["any", "one", "near"])
+@pytest.mark.parametrize("T,V,d", [(1100, 5000, 1088), (1153, 11261, 536), (2100, 700, 320), (4025, 2946, 576), (5130, 32000, 512), (16384, 20000, 64), (33000, 1700, 72)])
+def test_hidden_gradient_of_many_tokens_is_off_by_its_rounding_alone(A, T, V, d, target):
+    """No number of tokens averages out what dz loses at a token's target, which is a row of W of that token's alone."""
+    test_few_tokens_are_off_by_the_result_s_rounding_alone(A, T, V, d, target)
+
+
 @pytest.mark.parametrize("T,V,d", [(320, 60001, 264), (65, 30016, 1000)])
 def test_few_tokens_of_a_large_vocabulary(A, T, V, d):
     """The hidden states of all tokens in registers: as many tokens as fit, as few as none, a workspace of NaN, NaN of one that takes part."""
