@@ -432,6 +432,7 @@ def kv_layout_of(kv):
     if kv.dim() != 6 or kv.shape[1] != 2:
         raise ValueError("KV pool must be [layers, 2, pages, page_tokens, kv_heads, head_dim]")
     L, _, P, pt, H, hd = kv.shape
+    L, pt, H, hd = (_int32(x, "a side of the KV pool") for x in (L, pt, H, hd))
     return KVLayout(L, pt, H, hd, P)
 
 
@@ -968,6 +969,7 @@ def arrol_rotary(q, k, position, inv_freq, interleaved=False, inverse=False, mag
 
 @_on_stream
 def _py_rotary(q, k, position, inv_freq, interleaved=False, inverse=False, magnitude=1.0, out_q=None, out_k=None, stream=None):
+    rotary_dim = _int32(2 * inv_freq.numel(), "twice the number of frequencies")
     strides = _heads(q, "q"), (0 if k is None else _heads(k, "k"))
     if k is not None and (k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]):
         raise ValueError("k must have the rows and the head_dim of q")
@@ -978,7 +980,7 @@ def _py_rotary(q, k, position, inv_freq, interleaved=False, inverse=False, magni
     out_q, q_out_stride = _out_rows(out_q, q, "out_q")
     out_k, k_out_stride = (None, 0) if k is None else _out_rows(out_k, k, "out_k")
     rc = lib().arrol_rotary(q.data_ptr(), strides[0], None if k is None else k.data_ptr(), strides[1], _ptr(position, torch.int32, "position"),
-                            _ptr(inv_freq, torch.float64, "inv_freq"), q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], 2 * inv_freq.numel(),
+                            _ptr(inv_freq, torch.float64, "inv_freq"), q.shape[0], q.shape[1], 0 if k is None else k.shape[1], q.shape[2], rotary_dim,
                             int(bool(interleaved)), int(bool(inverse)), float(magnitude), out_q.data_ptr(), q_out_stride,
                             None if k is None else out_k.data_ptr(), k_out_stride, _stream(stream))
     _check("arrol_rotary", rc)
@@ -1002,15 +1004,18 @@ def arrol_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, p
 @_on_stream
 def _py_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, position=None, inv_freq=None, interleaved=False, magnitude=1.0, want_k=False,
                out_q=None, out_k=None, stream=None):
-    strides = _heads(k, "k"), _heads(v, "v"), (0 if q is None else _heads(q, "q"))
+    rotary_dim = 0 if inv_freq is None else _int32(2 * inv_freq.numel(), "twice the number of frequencies")
+    n = _int32(start.numel(), "the number of rows")
+    _int32(max(block_table.shape, default=0), "a side of block_table")
     lay, layer = kv_layout_of(kv), _int32(layer, "layer")
+    strides = _heads(k, "k"), _heads(v, "v"), (0 if q is None else _heads(q, "q"))
     if k.shape != v.shape or k.shape[1:] != (lay.n_kv_heads, lay.head_dim):
         raise ValueError("k and v must be [T, n_kv_heads, head_dim] with the pool's heads")
     if q is not None and (q.shape[0] != k.shape[0] or q.shape[2] != lay.head_dim):
         raise ValueError("q must have the rows and the head_dim of k")
     if (q is None and out_q is not None) or (not want_k and out_k is not None):
         raise ValueError("out_q is given without q, or out_k while turned keys are not wanted")
-    n, T = start.numel(), k.shape[0]
+    T = k.shape[0]
     if block_table.dim() != 2 or block_table.shape[0] != n or (n != T if cu_seqlens is None else cu_seqlens.numel() != n + 1):
         raise ValueError("block_table must be [n, pages], start [n], cu_seqlens [n+1]; without cu_seqlens there is a row of k for each")
     if position is not None and position.numel() != T:
@@ -1019,7 +1024,7 @@ def _py_append(k, v, kv, layer, block_table, start, cu_seqlens=None, q=None, pos
     out_k, k_out_stride = (None, 0) if not want_k else _out_rows(out_k, k, "out_k")
     rc = lib().arrol_append(k.data_ptr(), strides[0], v.data_ptr(), strides[1], None if q is None else q.data_ptr(), strides[2],
                             _ptr(cu_seqlens, torch.int64, "cu_seqlens"), _ptr(start, torch.int32, "start"), _ptr(position, torch.int32, "position"),
-                            _ptr(inv_freq, torch.float64, "inv_freq"), T, n, 0 if q is None else q.shape[1], 0 if inv_freq is None else 2 * inv_freq.numel(),
+                            _ptr(inv_freq, torch.float64, "inv_freq"), T, n, 0 if q is None else q.shape[1], rotary_dim,
                             int(bool(interleaved)), float(magnitude), _ptr(kv, torch.bfloat16, "kv"), lay, layer, _ptr(block_table, torch.int32, "block_table"),
                             block_table.shape[1], None if q is None else out_q.data_ptr(), q_out_stride, None if out_k is None else out_k.data_ptr(), k_out_stride,
                             _stream(stream))
@@ -1043,7 +1048,7 @@ def arrol_logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden=Tru
 def _py_logprob_grad(hidden, lm_head, targets, lse, grad_logp, want_hidden=True, want_lm_head=True, lm_head_sum=None, workspace=None, stream=None):
     if hidden.dim() != 2 or lm_head.dim() != 2 or hidden.shape[1] != lm_head.shape[1]:
         raise ValueError("hidden must be [T, d] and lm_head [V, d]")
-    (T, d), V, dev = hidden.shape, lm_head.shape[0], hidden.device
+    T, d, V, dev = hidden.shape[0], _int32(hidden.shape[1], "the columns of hidden"), _int32(lm_head.shape[0], "the rows of lm_head"), hidden.device
     if targets.numel() != T or lse.numel() != T or grad_logp.numel() != T:
         raise ValueError("targets, lse and grad_logp must be [T]")
     if lm_head_sum is not None and lm_head_sum.shape != lm_head.shape:

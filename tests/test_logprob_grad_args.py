@@ -55,6 +55,16 @@ def test_binding_refuses(A):
             A.arrol_logprob_grad(*args, **kw)
 
 
+def test_binding_refuses_sizes_past_32_bits(A):
+    """Of which the library would be handed the lower half: 2^32 + 10 rows as 10."""
+    meta = lambda *s, **kw: torch.empty(*s, device="meta", **kw)
+    y, f = meta(4, dtype=torch.int32), meta(4)
+    for V, d in ((2 ** 32 + 10, 64), (10, 2 ** 32 + 64)):
+        for kw in ({}, dict(want_lm_head=False), dict(want_hidden=False, lm_head_sum=meta(V, d))):
+            with pytest.raises(ValueError, match="32 bits"):
+                A.arrol_logprob_grad(meta(4, d, dtype=torch.bfloat16), meta(V, d, dtype=torch.bfloat16), y, f, f, **kw)
+
+
 def test_kernel_query(A):
     out = [ctypes.c_int32(-7) for _ in range(8)]
     ask = lambda T, V, d, n=8: A.lib().arrol_logprob_grad_kernels(T, V, d, *[ctypes.byref(x) for x in out[:n]], *[None] * (8 - n))

@@ -68,6 +68,20 @@ def test_binding_refuses(A):
         A.arrol_rotary(gpu_like, None, i32(4), f)
 
 
+def test_binding_refuses_sizes_past_32_bits(A):
+    """Of which the library would be handed the lower half: 2^32 + 64 as 64."""
+    meta = lambda *s, **kw: torch.empty(*s, device="meta", **kw)
+    x, i32 = meta(4, 2, 64, dtype=torch.bfloat16), meta(4, dtype=torch.int32)
+    many, f = meta(2 ** 31 + 32, dtype=torch.float64), meta(32, dtype=torch.float64)
+    kv = meta(1, 2, 4, 16, 2, 64, dtype=torch.bfloat16)
+    for call in (lambda: A.arrol_rotary(x, x, i32, many), lambda: A.arrol_append(x, x, kv, 0, meta(4, 1, dtype=torch.int32), i32, inv_freq=many),
+                 lambda: A.arrol_append(x, x, kv, 0, meta(2 ** 32 + 4, 1, dtype=torch.int32), meta(2 ** 32 + 4, dtype=torch.int32), inv_freq=f),
+                 lambda: A.arrol_append(x, x, kv, 0, meta(4, 2 ** 32 + 1, dtype=torch.int32), i32, inv_freq=f),
+                 lambda: A.arrol_append(x, x, meta(1, 2, 1, 2 ** 32 + 16, 2, 64, dtype=torch.bfloat16), 0, meta(4, 1, dtype=torch.int32), i32, inv_freq=f)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+
+
 def test_frequencies(A):
     """Against the definition: unscaled, all divided, and by parts, whose ends and middle are known."""
     plain = A.arrol_rotary_frequencies(64, 5e5, device="cpu")
