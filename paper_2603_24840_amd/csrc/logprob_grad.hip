@@ -17,10 +17,12 @@
 // No atomics: sums have a fixed order.
 //
 // What bounds it.  Large batches: the matrix cores under the card's power limit.  5,130 tokens (4,970 that take part) x 128,256 x 2048 6.6 to 6.8 ms, 1.16 to 1.19 PFLOP/s, on cards
-// where torch's 16,384 x 16,384 x 8,192 product reaches 1.29 and its products of these three shapes 1.18, 0.59 and 0.98; 6,278 x 151,936 x 4096 18.0 to 18.7 ms, 1.21 to 1.26.
+// where torch's 16,384 x 16,384 x 8,192 product reaches 1.28 to 1.32 and its products of these three shapes 1.22, 1.19 and 1.04; 6,278 x 151,936 x 4096 18.0 to 18.7 ms, 1.21 to 1.26.
 // Of the dz launches 13 % is the epilogue (2,253 us, 1,961 without, 2,145 without its stores, 2,229 without exponentials).  Few tokens: reading W twice and writing its
 // gradient, 16 x 151,936 x 2048 397 us (1.87 GB: 4.7 TB/s).  Between them, 311 x 151,936 x 2048 711 us: the LDS, into which tiles of 128 x 160 bring 36 KB and out of which they read
-// 72 KB a step of 640 cycles of products (matrix cores busy 38 % in dz and dL/dh).  Small calls: three launches of 2 to 8 us.
+// 72 KB a step of 640 cycles of products (matrix cores busy 40 % in the products' launch).  Small calls: three launches one after the other, 8.0, 7.5 and 2.4 us of 346 x 4,096 x 256; of its dz the
+// tile's four steps are 2.2 by their measured costs, the rest the launch and finding the tokens before the first load.  Sums (lm_head_sum): read in the epilogue with nothing asked for before, 311 x 151,936 x 2048
+// 1,198 us (721 in bf16, which moves 1.9 GB less), 5,130 x 128,256 x 2048 7,348 (6,937).
 // Not kept: in 128 x 160 tiles the next but one step's loads before the products, with a second barrier (even), the last step peeled off (dz 258 to 363: registers), tiles of 128 x 320 and
 // 256 x 320 for dz (even, and 8 % faster at 151,936 but 37 % slower at 32,000); 256 workgroups that walk over tiles, the next tile's loads under way during an epilogue (dz 1.4 % faster,
 // products 3.5 % slower); the K-major offsets of the ring formed ahead (products 4.5 % slower); dL/dh with the operands' roles exchanged, bands of 4, pieces of 2^27 to 2^30 values (even).
@@ -34,6 +36,7 @@ namespace {
 using namespace logprob_grad;
 using ring_nt::bf16x8;
 using ring_nt::f32x4;
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kXcds = 8, kRound = 256;
@@ -168,7 +171,6 @@ __global__ __launch_bounds__(256) void gather_kernel(Gather a) {
 // A wavefront's results, 4 consecutive values of a row in a lane, as bf16: lanes of neighbouring quarters exchange halves of two blocks, so that each stores 16 bytes and the
 // 16 lanes' rows get 64 bytes at a time.  x, y: blocks i and i + 1 of the row; the lane's 8 values start at 16 (i + lq % 2) + 4 (lq & 2).
 __device__ __forceinline__ u32x4 exchange(f32x4 x, f32x4 y) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
     const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), b = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
     const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
@@ -418,7 +420,6 @@ __device__ __forceinline__ void store_rows(const Lane& me, const f32x4 (&acc)[C:
     }
 }
 
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void add_times(f32x4& x, float f, bf16x4 four) {
     const f32x4 y = __builtin_convertvector(four, f32x4);
 #pragma unroll
@@ -426,7 +427,7 @@ __device__ __forceinline__ void add_times(f32x4& x, float f, bf16x4 four) {
 }
 
 // dz is largest at a token's target by far, and that one rounding, 2^-8 at most, counts beside a result's own: in dL/dh_t, where no other token averages it out, and in the row of dL/dW
-// that it is the target of, unless many tokens share it.  What dz lost there is added in fp32.  To dL/dh_t it is one row of W, a token's for itself: 5,130 x 128,256 x 2048 6,905 us and
+// that it is the target of, where gradients of either sign average out as little.  What dz lost there is added in fp32.  To dL/dh_t it is one row of W, a token's for itself: 5,130 x 128,256 x 2048 6,905 us and
 // without 6,965, 8,777 x 4,096 x 1024 317 and 315, at worst 4,000 x 300 x 1088 39.8 and 37.8.  To dL/dW it is a hidden state for every token whose target a row is.  The resident form has
 // that for nothing; tiles have to find their tokens and fetch them one after the other, so there it is up to kResidentTokens, where the forms meet, and beyond a gradient is 2.4e-3 off
 // in norm instead of 1.7e-3 (up to 1,024 tokens: 640 x 32,000 x 2048 292 us and without 267, 500 x 18,920 x 3128 275 and 256, 510 x 391 x 128 25.9 and 13.2).  What an epilogue
@@ -841,7 +842,6 @@ __device__ __forceinline__ f32x4 slab_sum(const float* slabs, int64_t stride, in
     return x;
 }
 __global__ __launch_bounds__(256) void join_kernel(Grad a, int n_slabs, int blocks_h) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     const int vecs = a.d / 4, n_active = *a.n_active;
     if (static_cast<int>(blockIdx.x) < blocks_h) {
         const int64_t total = static_cast<int64_t>(n_active) * vecs;

@@ -21,6 +21,9 @@ inline int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 // steps, a step where the chip is full (of every one of the `per_unit` workgroups that a compute unit has at a time) and a step where it is not.  1,024 x 32,000 x 2048:
 // dz 111 / 154 / 148 / 197 / 220, products 245 / 249 / 246 / 293 / 446; 640 tokens of it: 103 / 91 / 107 / 122 / 137 and 175 / 158 / 166 / 193 / 276; 318 x 4,096 x 256:
 // 14.9 / 11.4 / 9.7 / 7.9 / 7.4 and 19.4 / 10.0 / 9.3 / 9.2 / 6.8; 16 x 151,936 x 2048 (LM head from memory, and its gradient to it): dz in 128 x 160 150, 128 x 64 132, 64 x 64 135.
+// Next to the edges of the forms, whole calls with d = 2048, as chosen and with another form taken out: 321 x 128,256 749 and 740 (without 128 x 128), 321 x 151,936 882 and 878 .. 886,
+// 384 x 32,000 187 and 187 .. 202, 384 x 151,936 905 and 881 (without 128 x 128), 311 x 128,256 612 and 660 (without 128 x 160); not at 192 tokens, where dL/dh in 128 x 64 costs 7 %
+// (192 x 128,256 510 and 474 without it, 192 x 151,936 611 and 576).
 enum Form { kRing, kMid160, kMid128, kMidFew, kMid64, kForms };
 struct Size {
     int bm, bn, bm_w, bn_w;         // of dz and dL/dh, and of dL/dW
@@ -35,7 +38,7 @@ constexpr int64_t kSlabFloats = kSlabTiles * int64_t{65536};
 static_assert(kSlabFloats / 2 <= kCachedElements, "a gradient that goes past the caches has no parts");
 // From so many blocks of 64 x 256 on, seven to a compute unit, the hidden states' way into the registers is worth it.  The launch of the products, resident and in tiles: 311 x 151,936 x 2048
 // (19,000 blocks) 457 us and 600, 16 tokens 260 and 335, 110 x 79,125 x 3264 228 and 272, 300 x 32,000 x 1024 (2,000) 54 and 61; 250 x 20,000 x 1000 (1,252) 38.4 and 34.8, 320 x 16,384 x 512
-// (512) 22.7 and 19.8.
+// (512) 22.7 and 19.8.  Whole calls of 320 tokens, as many as there are registers for: x 128,256 x 2048 610 and 699, x 151,936 x 2048 711 and 845; of 192 608 and 700.
 constexpr int kResidentBlocks = 1792;
 constexpr double kJoin = 3.5, kJoinBytes = 3e6;      // microseconds; bytes a microsecond
 

@@ -9,17 +9,18 @@
 // under way, hands them over through its own part of the LDS and stores.  No barrier.  What a lane holds is a unit: VEC elements and their partners, or 2 VEC
 // elements side by side of the rest of the head or of an interleaved one, loaded and stored by that lane alone, so an output may be its input.
 //
-// Bound by memory: 11,136 tokens of 32 + 8 heads of 128 42.5 us (228 MB, 5.4 TB/s; torch's copy of 4 GiB 4.9), prompts into the pool with their keys kept 46.8 us (4.95 TB/s),
-// 6,426 tokens with heads of 80, 40 of them turned, 21.1 us (3.9 TB/s: accesses of 8 bytes).  Few tokens: one launch, 3.5 to 4.6 us.
+// Bound by memory: 11,136 tokens of 32 + 8 heads of 128 42.5 us (228 MB, 5.4 TB/s; torch's copy of 4 GiB 4.6 to 5.0), prompts into the pool with their keys kept 46.8 us (4.95 TB/s),
+// 6,426 tokens with heads of 80, 40 of them turned, 21.1 us (3.9 TB/s: accesses of 8 bytes, of the part that is not turned, too).  Few tokens: one launch, 3.5 to 4.6 us.
 #include "common.h"
 
 namespace {
 
 constexpr int kWaves = 4;                 // of a workgroup
-// Units of a lane in flight, and wavefronts that a launch is cut into where tokens are fewer.  11,136 tokens, 32 + 8 heads of 128, from and to memory: 2 and 65,536 45.3 us
-// (5.0 TB/s), 4 and 8,192 46.8, loads through the caches 50.4; stores past the caches too: 41.2, but the attention behind it 8 longer.  Into the pool, where every wavefront looks
-// for its token's page: 6,426 tokens of 24 + 8 heads of 80, 3 and 8,192 23.8 us, 2 and 65,536 28.3, 4 and 65,536 35.6; accesses of 16 bytes at
-// multiples of 8 where the second half begins there, with a short last unit, 29.5.
+// Units of a lane in flight, and wavefronts that a launch is cut into where tokens are fewer.  11,136 tokens, 32 + 8 heads of 128, from and to memory: 2 and 65,536 42.6 us
+// (5.4 TB/s), 4 and 8,192 40.9, but half of the head turned, in pairs, 40.6 and 42.9; loads through the caches 46.4; stores past the caches too: 41.2, but the attention behind
+// it 8 longer.  Into the pool, where every wavefront looks for its token's page: 6,426 tokens of 24 + 8 heads of 80, 3 and 8,192 21.1 us, 2 and 65,536 25.8, 4 and 65,536 32.8; prompts with their keys kept 46.9, 51.9 and 72.0.  Accesses of 16
+// bytes at multiples of 8 where the second half begins there, with a short last unit, were a quarter slower (29.5 and 23.8 in a loop over one call).  Loads through the caches: the heads of
+// 80 18.7 us, whose 8 bytes a lane share lines, but the prompts 52.9.
 template <bool POOL> constexpr int kUnits = POOL ? 3 : 2;
 template <bool POOL> constexpr int kWavefronts = POOL ? 8192 : 65536;
 constexpr int kMaxHalf = 128;
